@@ -48,8 +48,9 @@ enum {
     KVC_DEV_BAD_HEADER = 2,    /* payload header does not match the plan / request            */
     KVC_DEV_BAD_CHUNK = 4,     /* coder directory or chunk body inconsistent                  */
     KVC_DEV_BAD_TABLE = 8,     /* code-length table is not a complete prefix code             */
-    KVC_DEV_SCAN_TIMEOUT = 16  /* internal: chunk-offset scan gave up waiting; the payload's
+    KVC_DEV_SCAN_TIMEOUT = 16, /* internal: chunk-offset scan gave up waiting; the payload's
                                   directory, header sizes and size word are not written       */
+    KVC_DEV_BAD_ROW = 32       /* kvc_cache_*: rows, tokens or indices of a sequence do not fit */
 };
 
 enum { KVC_F16 = 1, KVC_BF16 = 2 };
@@ -338,6 +339,118 @@ int kvc_policy_build(const kvc_profile *profiles, int32_t n, kvc_policy_segment 
                      int32_t *count);
 int kvc_policy_lookup(const kvc_policy_segment *table, int32_t count, double bandwidth, int32_t *profile,
                       int32_t *toward_more_bandwidth, int32_t *toward_less_bandwidth);
+
+/*
+ * ---- A cache held in the quantiser's codes --------------------------------------------------
+ *
+ * What a decode worker keeps of the K/V it received and of the tokens it makes: pages of 4- or 8-bit
+ * codes, written row by row (kvc_cache_store), read by attention as they are (kvc_cache_attend),
+ * read back into 16-bit rows for the next movement (kvc_cache_load); kvc_cache_keep moves the rows
+ * of accepted drafts together.  One pool of pages belongs to one layer.
+ *
+ * A row is one token's head_dim (128) values of one KV head.  Both K and V are quantised per token in
+ * groups of `group` channels (a row never waits for other tokens, and a rejected draft is simply
+ * overwritten): values are limited to +-65504 (NaN counts as 0); zero = fp16(min),
+ * scale = fp16((max - min) / (2^b - 1)), code = clamp(rint((x - zero) * (1 / scale)), 0, 2^b - 1), as in
+ * kvc_compress.  A code stands for code * scale + zero.  With transform = KVC_T_HADAMARD, for K whose
+ * channels differ much in size, K rows are stored as H x / 8 (rounded to the type), and attention rotates the
+ * queries: (H q / 16) . (H k / 8) = q . k.  V is not rotated.
+ *
+ *   dtype         KVC_F16 or KVC_BF16: type of rows, queries and results
+ *   bits_k/bits_v 4 or 8
+ *   transform     KVC_T_NONE or KVC_T_HADAMARD
+ *   group         32, 64 or 128 channels
+ *   block_tokens  tokens per page: a power of two, 16 to 4096
+ *   q_heads       a multiple of kv_heads; query head h reads KV head h / (q_heads / kv_heads)
+ *   head_dim      128
+ */
+typedef struct {
+    uint8_t dtype, bits_k, bits_v, transform;
+    int32_t group, block_tokens, kv_heads, q_heads, head_dim;
+} kvc_cache_config;
+
+typedef struct kvc_cache_plan_s kvc_cache_plan_t;      /* opaque, host memory */
+
+/*
+ * Validates a configuration and fixes the limits of the calls: tokens of a sequence, new rows of a
+ * sequence in one call (new tokens in kvc_cache_attend), sequences.  Touches no device; read-only
+ * afterwards, so several threads may use one plan.  KVC_ERR_ARG / KVC_ERR_UNSUPPORTED / KVC_ERR_CAPACITY
+ * as for kvc_plan; *out = NULL on error.
+ */
+int kvc_cache_plan(const kvc_cache_config *config, int64_t max_tokens, int32_t max_new, int32_t max_batch,
+                   kvc_cache_plan_t **out);
+void kvc_cache_plan_free(kvc_cache_plan_t *plan);
+
+/* Bytes of a page (all KV heads, K and V) and of the DEVICE scratch of kvc_cache_attend (may be 0). */
+size_t kvc_cache_page_bytes(const kvc_cache_plan_t *plan);
+size_t kvc_cache_workspace_size(const kvc_cache_plan_t *plan);
+
+/*
+ * The sequences of a call.  Their lengths are on the device, so that a captured graph can be replayed as they
+ * grow; n, max_new and max_tokens are bounds that fix the launch and must hold for what the device arrays say.
+ * Sequence s has tokens[s] tokens, the last new_start[s+1] - new_start[s] of which are its new ones:
+ * rows new_start[s] ... of the tensors that a call names.  Token t of it lives in page
+ * block_table[s * table_stride + t / block_tokens].
+ *   mask       attention only: NULL = a new token sees all tokens up to itself (consecutive tokens,
+ *              also a chunk of a prompt); otherwise `mask_words` 64-bit words per new row: bit j says
+ *              whether it sees new token j of its sequence (a tree of drafts: itself and its
+ *              ancestors).  Tokens before the new ones are seen by all.
+ * A sequence whose numbers do not fit (more than max_new new rows, tokens < new rows or > max_tokens,
+ * rows outside the tensors) is left out and gets KVC_DEV_BAD_ROW; a page outside [0, num_pages) is
+ * neither written nor read (attention skips its tokens) and sets KVC_DEV_BAD_BLOCK.
+ */
+typedef struct {
+    int32_t n, max_new;
+    int64_t max_tokens;
+    const int32_t *new_start;            /* DEVICE, n + 1 */
+    const int32_t *tokens;               /* DEVICE, n */
+    const int32_t *block_table;          /* DEVICE, n x table_stride, table_stride >= ceil(max_tokens / block_tokens) */
+    int64_t table_stride;
+    const uint64_t *mask;                /* DEVICE or NULL; mask_words >= ceil(max_new / 64) */
+    int32_t mask_words, num_pages;
+} kvc_cache_batch;
+
+/* K and V rows: element d of KV head h of row r at k + r * stride_row + h * stride_head + d; strides are multiples of 8. */
+typedef struct {
+    void *k, *v;                         /* DEVICE */
+    int64_t rows, stride_row, stride_head;
+} kvc_cache_rows;
+
+/* Queries and results: q_heads heads of `rows` new rows.  Strides are multiples of 8.  lse: optional, [rows][q_heads]. */
+typedef struct {
+    const void *q;                       /* DEVICE */
+    void *out;                           /* DEVICE */
+    float *lse;                          /* DEVICE or NULL: log(sum of exp(scores)), for joining with other attention */
+    int64_t rows, q_stride_row, q_stride_head, out_stride_row, out_stride_head;
+    float scale;                         /* of the scores, usually 1 / sqrt(head_dim) */
+} kvc_cache_queries;
+
+/*
+ * The calls.  `pages`: the pool, DEVICE, num_pages * kvc_cache_page_bytes(plan) bytes.  dev_status: DEVICE,
+ * n words; bits are OR-ed in and never cleared by a call, so that a loop can look at them now and then.
+ * Everything is enqueued on hip_stream; nothing is allocated, copied or waited for, and the calls may be captured
+ * into a graph.
+ *   kvc_cache_store   quantises the new rows into the sequences' pages
+ *   kvc_cache_load    the new rows as the pages hold them, rounded to the type (every token, with new_start
+ *                     counting all of them)
+ *   kvc_cache_keep    among the new rows of sequence s, rows keep[keep_start[s]] < keep[keep_start[s] + 1] < ...
+ *                     (numbers below its count of new rows) move to places 0, 1, ...; `keep` has keep_rows entries.
+ *                     Codes move as they are.  Indices that do not ascend or are out of range:
+ *                     KVC_DEV_BAD_ROW, and the sequence stays as it is
+ *   kvc_cache_attend  out = softmax(scale * q k^T) v over the tokens that a new token sees; a row that sees none
+ *                     gives zeros and lse = -infinity.  Scores, maxima and sums are held in 32 bits; weights and
+ *                     values enter the second product as fp16 numbers (one rounding each).
+ *                     workspace: DEVICE, kvc_cache_workspace_size bytes, may be NULL when that is 0; calls on
+ *                     one workspace must be in stream order
+ */
+int kvc_cache_store(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_rows *rows, void *pages,
+                    int32_t *dev_status, void *hip_stream);
+int kvc_cache_load(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_rows *rows, const void *pages,
+                   int32_t *dev_status, void *hip_stream);
+int kvc_cache_keep(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const int32_t *keep_start, const int32_t *keep,
+                   int64_t keep_rows, void *pages, int32_t *dev_status, void *hip_stream);
+int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_queries *queries,
+                     const void *pages, int32_t *dev_status, void *workspace, void *hip_stream);
 
 const char *kvc_status_string(int status);
 

@@ -30,12 +30,12 @@ SRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 OUT = os.path.join(HERE, "libkvc.so")
 WIDTHS = (2, 3, 4, 8)
-# (source, code width or None): the kernel sources are compiled once per code width, which spreads
-# the build over the cores; the slowest units come first
-JOBS = ([("kvc_huff_enc.hip", b) for b in WIDTHS] + [("kvc_quant.hip", b) for b in WIDTHS] +
+# (source, code width or None): the kernel sources are compiled once per code width (the attention once per
+# pair of them, 10 * bits_k + bits_v), which spreads the build over the cores; the slowest units come first
+JOBS = ([("kvc_attend.hip", b) for b in (44, 48, 84, 88)] + [("kvc_cache_rows.hip", None)] + [("kvc_huff_enc.hip", b) for b in WIDTHS] + [("kvc_quant.hip", b) for b in WIDTHS] +
         [("kvc_huff_dec.hip", b) for b in WIDTHS] +
         [("kvc_huff_tables.hip", None), ("kvc_selftest.hip", None), ("kvc_service.hip", None), ("kvc_probe.hip", None),
-         ("kvc_api.hip", None), ("kvc_policy.hip", None)])
+         ("kvc_api.hip", None), ("kvc_cache.hip", None), ("kvc_policy.hip", None)])
 # packed fp32 instructions are switched off for the device pass (flag for hipcc only); host functions may take 44 KB of stack, which
 # the calls need for the items of a full window (they run on threads of other programs)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

@@ -1,0 +1,211 @@
+// Host side of the quantised cache: plans, checks of the arguments, how the attention's work is divided.
+#include "kvc_cache_internal.h"
+#include "../../include/kvc.h"
+
+#include <new>
+
+struct kvc_cache_plan_s {
+    kvc_cache_config config;
+    int64_t max_tokens;
+    int32_t max_new, max_batch;
+    size_t page_bytes, workspace;
+};
+
+namespace kvc {
+
+constexpr long long kAttendGroups = 1024;    // workgroups that the tokens of few rows are spread over (four per compute unit)
+constexpr int kMostSplits = 256;
+constexpr int kLeastChunk = 256;             // tokens of a workgroup: two steps of its four waves at least
+constexpr size_t kPartBytes = (kDim + 2) * sizeof(float);
+
+// How a call divides the work: tiles of 16 query rows per wave, tokens per workgroup.
+struct AttendShape {
+    int tiles, row_blocks, splits, chunk;
+};
+static AttendShape attend_shape(const kvc_cache_config &f, int n, int max_new, int64_t max_tokens)
+{
+    AttendShape s;
+    const int64_t rows = (int64_t)max_new * (f.q_heads / f.kv_heads);
+    s.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    s.row_blocks = (int)((rows + 16 * s.tiles - 1) / (16 * s.tiles));
+    const int64_t groups = (int64_t)n * f.kv_heads * s.row_blocks;
+    int64_t splits = kAttendGroups / groups;
+    const int64_t most = (max_tokens + kLeastChunk - 1) / kLeastChunk;
+    splits = splits > most ? most : splits;
+    splits = splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits;
+    int64_t chunk = (max_tokens + splits - 1) / splits;
+    chunk = chunk < 1 ? 1 : chunk;
+    s.chunk = (int)((chunk + 127) / 128 * 128);
+    s.splits = (int)((max_tokens + s.chunk - 1) / s.chunk);
+    if (s.splits < 1) s.splits = 1;
+    return s;
+}
+
+static CacheTypes types_of(const kvc_cache_config &f)
+{
+    return CacheTypes{f.dtype, f.bits_k, f.bits_v, f.group, f.transform == KVC_T_HADAMARD};
+}
+
+static bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+// The checks that all calls share; fills the view.
+static int check_call(const kvc_cache_plan_t *plan, const kvc_cache_batch *b, void *pages, int32_t *status, int64_t rows, CacheView *c)
+{
+    if (!plan || !b) return KVC_ERR_ARG;
+    const kvc_cache_config &f = plan->config;
+    if (b->n < 0 || b->max_new < 0 || b->max_tokens < 0 || b->num_pages < 0 || b->table_stride < 0 || rows < 0) return KVC_ERR_ARG;
+    if (b->n > plan->max_batch || b->max_new > plan->max_new || b->max_tokens > plan->max_tokens) return KVC_ERR_CAPACITY;
+    if (b->n == 0 || b->max_new == 0 || b->max_tokens == 0) return KVC_OK;
+    if (!b->new_start || !b->tokens || !b->block_table || !pages || !status) return KVC_ERR_ARG;
+    if (!aligned(b->new_start, 4) || !aligned(b->tokens, 4) || !aligned(b->block_table, 4) || !aligned(status, 4) || !aligned(pages, 16) ||
+        !aligned(b->mask, 8)) return KVC_ERR_ARG;
+    if (b->table_stride < (b->max_tokens + f.block_tokens - 1) / f.block_tokens) return KVC_ERR_ARG;
+    if (b->mask && (int64_t)b->mask_words * 64 < b->max_new) return KVC_ERR_ARG;
+    c->pages = (uint8_t *)pages;
+    c->new_start = b->new_start;
+    c->tokens = b->tokens;
+    c->block_table = b->block_table;
+    c->mask = (const unsigned long long *)b->mask;
+    c->status = status;
+    c->table_stride = b->table_stride;
+    c->page_bytes = (long long)plan->page_bytes;
+    c->rows = rows;
+    c->mask_words = b->mask_words;
+    c->heads = f.kv_heads;
+    c->page_shift = __builtin_ctz((unsigned)f.block_tokens);
+    c->num_pages = b->num_pages;
+    c->max_new = b->max_new;
+    c->max_tokens = (int)b->max_tokens;
+    return KVC_OK;
+}
+
+static bool nothing(const kvc_cache_batch *b) { return b->n == 0 || b->max_new == 0 || b->max_tokens == 0; }
+
+static bool strides_ok(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
+
+static int rows_call(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_rows *r, void *pages, int32_t *status,
+                     void *stream, bool store)
+{
+    CacheView c;
+    if (!r) return KVC_ERR_ARG;
+    const int rc = check_call(plan, batch, pages, status, r->rows, &c);
+    if (rc != KVC_OK || nothing(batch)) return rc;
+    if ((r->rows && (!r->k || !r->v)) || !aligned(r->k, 16) || !aligned(r->v, 16) || !strides_ok(r->stride_row, r->stride_head)) return KVC_ERR_ARG;
+    launch_cache_rows(types_of(plan->config), c, store, (uint16_t *)r->k, (uint16_t *)r->v, r->stride_row, r->stride_head, batch->n,
+                      (hipStream_t)stream);
+    return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
+}
+
+}  // namespace kvc
+
+extern "C" int kvc_cache_plan(const kvc_cache_config *config, int64_t max_tokens, int32_t max_new, int32_t max_batch,
+                              kvc_cache_plan_t **out)
+{
+    using namespace kvc;
+    if (!out) return KVC_ERR_ARG;
+    *out = nullptr;
+    if (!config || max_tokens < 0 || max_new < 1 || max_batch < 1) return KVC_ERR_ARG;
+    const kvc_cache_config &f = *config;
+    if (f.dtype != KVC_F16 && f.dtype != KVC_BF16) return KVC_ERR_ARG;
+    if (f.group != 32 && f.group != 64 && f.group != 128) return KVC_ERR_ARG;
+    if (f.kv_heads < 1 || f.q_heads < 1 || f.q_heads % f.kv_heads || f.head_dim < 1 || f.block_tokens < 1) return KVC_ERR_ARG;
+    const bool widths = (f.bits_k == 4 || f.bits_k == 8) && (f.bits_v == 4 || f.bits_v == 8);
+    const bool pages = f.block_tokens >= kGranule && f.block_tokens <= 4096 && (f.block_tokens & (f.block_tokens - 1)) == 0;
+    if (!widths || !pages || f.head_dim != kDim || f.transform > KVC_T_HADAMARD || f.q_heads > 65536 || max_batch > 65535)
+        return KVC_ERR_UNSUPPORTED;
+    // (row and token numbers are ints in the kernels, rows of a head in the grid's second dimension)
+    if (max_tokens > 0x7fffff00ll || (int64_t)max_new * f.q_heads > 0x3fffffffll ||
+        (int64_t)f.kv_heads * (((int64_t)max_new * (f.q_heads / f.kv_heads) + 15) / 16) > 65535)
+        return KVC_ERR_CAPACITY;
+    kvc_cache_plan_t *p = new (std::nothrow) kvc_cache_plan_t;
+    if (!p) return KVC_ERR_CAPACITY;
+    p->config = f;
+    p->max_tokens = max_tokens;
+    p->max_new = max_new;
+    p->max_batch = max_batch;
+    p->page_bytes = (size_t)f.kv_heads * (f.block_tokens / kGranule) * granule_map(f.bits_k, f.bits_v, f.group).bytes;
+    // a call has at most kAttendGroups workgroups where it divides the tokens, with 64 rows each, and no more
+    // than kMostSplits results per row
+    const int64_t rows = (int64_t)max_batch * max_new * f.q_heads;
+    int64_t most = (max_tokens + kLeastChunk - 1) / kLeastChunk;
+    most = most > kMostSplits ? kMostSplits : most;
+    const int64_t parts = rows * most < kAttendGroups * 64 ? rows * most : kAttendGroups * 64;
+    p->workspace = most > 1 ? (size_t)parts * kPartBytes : 0;
+    *out = p;
+    return KVC_OK;
+}
+
+extern "C" void kvc_cache_plan_free(kvc_cache_plan_t *plan) { delete plan; }
+
+extern "C" size_t kvc_cache_page_bytes(const kvc_cache_plan_t *plan) { return plan ? plan->page_bytes : 0; }
+
+extern "C" size_t kvc_cache_workspace_size(const kvc_cache_plan_t *plan) { return plan ? plan->workspace : 0; }
+
+extern "C" int kvc_cache_store(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_rows *rows, void *pages,
+                               int32_t *dev_status, void *hip_stream)
+{
+    return kvc::rows_call(plan, batch, rows, pages, dev_status, hip_stream, true);
+}
+
+extern "C" int kvc_cache_load(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_rows *rows, const void *pages,
+                              int32_t *dev_status, void *hip_stream)
+{
+    return kvc::rows_call(plan, batch, rows, (void *)pages, dev_status, hip_stream, false);
+}
+
+extern "C" int kvc_cache_keep(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const int32_t *keep_start, const int32_t *keep,
+                              int64_t keep_rows, void *pages, int32_t *dev_status, void *hip_stream)
+{
+    using namespace kvc;
+    CacheView c;
+    const int rc = check_call(plan, batch, pages, dev_status, INT64_MAX, &c);
+    if (rc != KVC_OK || nothing(batch)) return rc;
+    if (!keep_start || (keep_rows && !keep) || keep_rows < 0 || keep_rows > 0x7fffffffll || !aligned(keep_start, 4) || !aligned(keep, 4)) return KVC_ERR_ARG;
+    launch_cache_keep(types_of(plan->config), c, keep_start, keep, (int)keep_rows, batch->n, (hipStream_t)hip_stream);
+    return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
+}
+
+extern "C" int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_queries *queries,
+                                const void *pages, int32_t *dev_status, void *workspace, void *hip_stream)
+{
+    using namespace kvc;
+    if (!queries) return KVC_ERR_ARG;
+    const kvc_cache_queries &u = *queries;
+    AttendArgs a;
+    const int rc = check_call(plan, batch, (void *)pages, dev_status, u.rows, &a.c);
+    if (rc != KVC_OK || nothing(batch)) return rc;
+    if ((u.rows && (!u.q || !u.out)) || !aligned(u.q, 16) || !aligned(u.out, 16) || !aligned(u.lse, 4) || !strides_ok(u.q_stride_row, u.q_stride_head) ||
+        !strides_ok(u.out_stride_row, u.out_stride_head) || !(u.scale >= -3.0e38f && u.scale <= 3.0e38f)) return KVC_ERR_ARG;
+    const kvc_cache_config &f = plan->config;
+    const AttendShape s = attend_shape(f, batch->n, batch->max_new, batch->max_tokens);
+    a.part = nullptr;
+    a.part_ml = nullptr;
+    if (s.splits > 1) {
+        const int64_t parts = (int64_t)batch->n * batch->max_new * f.q_heads * s.splits;
+        if ((size_t)parts * kPartBytes > plan->workspace) return KVC_ERR_CAPACITY;
+        if (!workspace || !aligned(workspace, 16)) return KVC_ERR_ARG;
+        a.part = (float *)workspace;
+        a.part_ml = a.part + parts * kDim;
+    }
+    a.q = (const uint16_t *)u.q;
+    a.out = (uint16_t *)u.out;
+    a.lse = u.lse;
+    a.q_row = u.q_stride_row;
+    a.q_head = u.q_stride_head;
+    a.o_row = u.out_stride_row;
+    a.o_head = u.out_stride_head;
+    a.scale = u.scale * 1.44269504088896341f;
+    a.per_kv = f.q_heads / f.kv_heads;
+    a.row_blocks = s.row_blocks;
+    a.splits = s.splits;
+    a.chunk = s.chunk;
+    a.dtype = f.dtype;
+    const CacheTypes t = types_of(f);
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    if (f.bits_k == 4 && f.bits_v == 4) launch_attend<44>(t, a, s.tiles, batch->n, stream);
+    else if (f.bits_k == 4) launch_attend<48>(t, a, s.tiles, batch->n, stream);
+    else if (f.bits_v == 4) launch_attend<84>(t, a, s.tiles, batch->n, stream);
+    else launch_attend<88>(t, a, s.tiles, batch->n, stream);
+    if (s.splits > 1) launch_attend_join(a, s.tiles, batch->n, stream);
+    return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
+}

@@ -1,0 +1,47 @@
+// Host-side declarations shared by the translation units of the quantised cache.
+#pragma once
+
+#include "kvc_cache.h"
+
+namespace kvc {
+
+template <int N> struct IntConst {
+    static constexpr int value = N;
+};
+
+struct CacheTypes {
+    int dtype, bits_k, bits_v, group;
+    bool rotate;                   // K rows and queries
+};
+
+void launch_cache_rows(const CacheTypes &t, const CacheView &c, bool store, uint16_t *k, uint16_t *v, long long stride_row,
+                       long long stride_head, int n, hipStream_t stream);
+void launch_cache_keep(const CacheTypes &t, const CacheView &c, const int *keep_start, const int *keep, int max_keep, int n,
+                       hipStream_t stream);
+
+// Arguments of the attention kernels.
+struct AttendArgs {
+    CacheView c;
+    const uint16_t *q;
+    uint16_t *out;
+    float *lse;                    // or null
+    float *part;                   // splits > 1: sums, [sequence][new][query head][split][128]
+    float *part_ml;                // ... and (maximum, sum of weights)
+    long long q_row, q_head, o_row, o_head;        // strides in elements
+    float scale;                   // of the scores, times log2(e)
+    int per_kv;                    // query heads per KV head
+    int row_blocks;                // of 16 * tiles query rows, in the longest sequence
+    int splits, chunk;             // tokens of a sequence per workgroup (a multiple of 128)
+    int dtype;
+};
+
+// The attention of one pair of code widths (10 * bits_k + bits_v) with 1, 2 or 4 tiles of 16 query rows per wave, and the kernel that
+// joins the results of several workgroups per row.
+template <int BITS> void launch_attend(const CacheTypes &t, const AttendArgs &a, int tiles, int n, hipStream_t stream);
+template <> void launch_attend<44>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);
+template <> void launch_attend<48>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);
+template <> void launch_attend<84>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);
+template <> void launch_attend<88>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);
+void launch_attend_join(const AttendArgs &a, int tiles, int n, hipStream_t stream);
+
+}  // namespace kvc

@@ -13,12 +13,13 @@ LIB_PATH = os.path.join(_HERE, "libkvc.so")
 F16, BF16 = 1, 2
 CODEC_NONE, CODEC_HUFF8 = 0, 1
 OK = 0
-DEV_BAD_BLOCK, DEV_BAD_HEADER, DEV_BAD_CHUNK, DEV_BAD_TABLE, DEV_SCAN_TIMEOUT = 1, 2, 4, 8, 16
+DEV_BAD_BLOCK, DEV_BAD_HEADER, DEV_BAD_CHUNK, DEV_BAD_TABLE, DEV_SCAN_TIMEOUT, DEV_BAD_ROW = 1, 2, 4, 8, 16, 32
 
 SYMBOLS = ["kvc_plan", "kvc_plan_free", "kvc_payload_size", "kvc_workspace_size", "kvc_compress",
            "kvc_decompress", "kvc_payload_inspect", "kvc_check_block_table", "kvc_status_string",
            "kvc_trace", "kvc_selftest", "kvc_table_bytes", "kvc_workspace_init", "kvc_compress_static", "kvc_stream_probe", "kvc_profile_throughput", "kvc_benefit_threshold", "kvc_policy_build",
-           "kvc_policy_lookup"]
+           "kvc_policy_lookup", "kvc_cache_plan", "kvc_cache_plan_free", "kvc_cache_page_bytes", "kvc_cache_workspace_size",
+           "kvc_cache_store", "kvc_cache_load", "kvc_cache_keep", "kvc_cache_attend"]
 
 
 class Strategy(C.Structure):
@@ -46,6 +47,27 @@ class Request(C.Structure):
                 ("stride_token", C.c_int64), ("stride_block", C.c_int64),
                 ("block_table", C.c_void_p), ("block_tokens", C.c_int32),
                 ("num_phys_blocks", C.c_int32)]
+
+
+class CacheConfig(C.Structure):
+    _fields_ = [("dtype", C.c_uint8), ("bits_k", C.c_uint8), ("bits_v", C.c_uint8), ("transform", C.c_uint8),
+                ("group", C.c_int32), ("block_tokens", C.c_int32), ("kv_heads", C.c_int32), ("q_heads", C.c_int32),
+                ("head_dim", C.c_int32)]
+
+
+class CacheSequences(C.Structure):
+    _fields_ = [("n", C.c_int32), ("max_new", C.c_int32), ("max_tokens", C.c_int64), ("new_start", C.c_void_p),
+                ("tokens", C.c_void_p), ("block_table", C.c_void_p), ("table_stride", C.c_int64), ("mask", C.c_void_p),
+                ("mask_words", C.c_int32), ("num_pages", C.c_int32)]
+
+
+class CacheRows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("rows", C.c_int64), ("stride_row", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class CacheQueries(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("rows", C.c_int64), ("q_stride_row", C.c_int64),
+                ("q_stride_head", C.c_int64), ("out_stride_row", C.c_int64), ("out_stride_head", C.c_int64), ("scale", C.c_float)]
 
 
 class KvcError(RuntimeError):
@@ -99,6 +121,19 @@ def load():
                                        C.POINTER(C.c_int32)]
         L.kvc_policy_lookup.argtypes = [C.POINTER(PolicySegment), C.c_int32, C.c_double, C.POINTER(C.c_int32),
                                         C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+        L.kvc_cache_plan.argtypes = [C.POINTER(CacheConfig), C.c_int64, C.c_int32, C.c_int32, C.POINTER(C.c_void_p)]
+        L.kvc_cache_plan_free.argtypes = [C.c_void_p]
+        L.kvc_cache_plan_free.restype = None
+        L.kvc_cache_page_bytes.argtypes = [C.c_void_p]
+        L.kvc_cache_page_bytes.restype = C.c_size_t
+        L.kvc_cache_workspace_size.argtypes = [C.c_void_p]
+        L.kvc_cache_workspace_size.restype = C.c_size_t
+        for f in (L.kvc_cache_store, L.kvc_cache_load):
+            f.argtypes = [C.c_void_p, C.POINTER(CacheSequences), C.POINTER(CacheRows), C.c_void_p, C.c_void_p, C.c_void_p]
+        L.kvc_cache_keep.argtypes = [C.c_void_p, C.POINTER(CacheSequences), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                     C.c_void_p]
+        L.kvc_cache_attend.argtypes = [C.c_void_p, C.POINTER(CacheSequences), C.POINTER(CacheQueries), C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_void_p]
         L.kvc_status_string.argtypes = [C.c_int]
         L.kvc_status_string.restype = C.c_char_p
         _lib = L
@@ -313,3 +348,124 @@ class Buffers:
         """Host copy (numpy uint8) of request i's payload, cut to its true size."""
         n = int(self.out_bytes[i].item())
         return self.payload[self.offsets[i]: self.offsets[i] + n].cpu().numpy()
+
+
+# ---- the quantised cache ------------------------------------------------------------------------
+
+class CachePlan:
+    """kvc_cache_plan / kvc_cache_plan_free: configuration and limits of a cache held in the quantiser's codes."""
+
+    def __init__(self, dtype, kv_heads, q_heads, head_dim=128, bits_k=4, bits_v=4, group=32, block_tokens=16, transform=0,
+                 max_batch=1, max_tokens=0, max_new=1):
+        self.config = CacheConfig(dtype, bits_k, bits_v, transform, group, block_tokens, kv_heads, q_heads, head_dim)
+        self.max_tokens, self.max_new, self.max_batch = max_tokens, max_new, max_batch
+        self._h = C.c_void_p()
+        rc = load().kvc_cache_plan(C.byref(self.config), max_tokens, max_new, max_batch, C.byref(self._h))
+        if rc != OK:
+            raise KvcError("kvc_cache_plan", rc)
+
+    def __del__(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.kvc_cache_plan_free(self._h)
+            self._h = None
+
+    def page_bytes(self):
+        return load().kvc_cache_page_bytes(self._h)
+
+    def workspace_size(self):
+        return load().kvc_cache_workspace_size(self._h)
+
+
+class CacheBatch:
+    """The sequences of a call (kvc_cache_batch).  new_start [n + 1], tokens [n], block_table [n, pages per sequence]: int32
+    device tensors; max_new and max_tokens: host bounds of what they say; mask: int64 device tensor [new rows, words] or None."""
+
+    def __init__(self, new_start, tokens, block_table, max_new, max_tokens, num_pages, mask=None):
+        import torch
+        if not (new_start.dtype == tokens.dtype == block_table.dtype == torch.int32):
+            raise TypeError("new_start, tokens and block_table are int32 tensors")
+        n = tokens.shape[0]
+        if new_start.shape != (n + 1,) or block_table.dim() != 2 or block_table.shape[0] != n or not new_start.is_contiguous() or \
+                not tokens.is_contiguous() or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+            raise ValueError("new_start [n + 1], tokens [n] and the rows of block_table [n, pages] have to be contiguous")
+        words = 0
+        if mask is not None:
+            if mask.dtype != torch.int64 or mask.dim() != 2 or not mask.is_contiguous():
+                raise ValueError("mask is a contiguous int64 tensor [new rows, words]")
+            words = mask.shape[1]
+        self.keep_alive = (new_start, tokens, block_table, mask)
+        stride = block_table.stride(0) if n > 1 else block_table.shape[1]
+        self.struct = CacheSequences(n, max_new, max_tokens, new_start.data_ptr(), tokens.data_ptr(), block_table.data_ptr(), stride,
+                                     mask.data_ptr() if mask is not None else None, words, num_pages)
+        self.mask_rows = None if mask is None else mask.shape[0]
+        self._ref = C.byref(self.struct)
+
+
+class Cache:
+    """One layer's pool of pages with its status words and the attention's workspace, allocated through torch (the workspace may be
+    shared between layers that run in stream order)."""
+
+    def __init__(self, plan, num_pages, device="cuda", workspace=None):
+        import torch
+        self.plan, self.num_pages = plan, num_pages
+        self.dtype = torch.float16 if plan.config.dtype == F16 else torch.bfloat16
+        self.pages = torch.zeros(max(num_pages * plan.page_bytes(), 16), dtype=torch.uint8, device=device)
+        self.status = torch.zeros(plan.max_batch, dtype=torch.int32, device=device)
+        self.workspace = workspace if workspace is not None else \
+            torch.empty(max(plan.workspace_size(), 16), dtype=torch.uint8, device=device)
+        if self.workspace.numel() * self.workspace.element_size() < plan.workspace_size():
+            raise ValueError("the workspace is smaller than kvc_cache_workspace_size")
+        self._pages, self._status, self._workspace = self.pages.data_ptr(), self.status.data_ptr(), self.workspace.data_ptr()
+
+    def _check(self, batch, tensors, heads):
+        if batch.struct.num_pages > self.num_pages:
+            raise ValueError("the batch names more pages than the pool has")
+        for x in tensors:
+            if x.dtype is not self.dtype or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.plan.config.head_dim or x.stride(2) != 1:
+                raise ValueError("rows are [rows, %d, %d] tensors of the plan's type with contiguous channels" % (heads, self.plan.config.head_dim))
+
+    def _rows(self, batch, k, v):
+        self._check(batch, (k, v), self.plan.config.kv_heads)
+        if k.shape != v.shape or k.stride() != v.stride():
+            raise ValueError("k and v have one shape and one layout")
+        return CacheRows(k.data_ptr(), v.data_ptr(), k.shape[0], k.stride(0), k.stride(1))
+
+    def store(self, batch, k, v, stream=None):
+        """kvc_cache_store: k, v [new rows, kv_heads, 128]."""
+        rc = _lib.kvc_cache_store(self.plan._h, batch._ref, C.byref(self._rows(batch, k, v)), self._pages, self._status, stream)
+        if rc != OK:
+            raise KvcError("kvc_cache_store", rc)
+
+    def load(self, batch, k, v, stream=None):
+        """kvc_cache_load into k, v [new rows, kv_heads, 128]."""
+        rc = _lib.kvc_cache_load(self.plan._h, batch._ref, C.byref(self._rows(batch, k, v)), self._pages, self._status, stream)
+        if rc != OK:
+            raise KvcError("kvc_cache_load", rc)
+
+    def keep(self, batch, keep_start, keep, stream=None):
+        """kvc_cache_keep: keep_start [n + 1] and keep, int32 device tensors."""
+        import torch
+        if keep_start.dtype != torch.int32 or keep.dtype != torch.int32 or keep_start.numel() < batch.struct.n + 1 or \
+                not keep_start.is_contiguous() or not keep.is_contiguous():
+            raise ValueError("keep_start [n + 1] and keep are contiguous int32 tensors")
+        self._check(batch, (), 0)
+        rc = _lib.kvc_cache_keep(self.plan._h, batch._ref, keep_start.data_ptr(), keep.data_ptr(), keep.numel(), self._pages, self._status,
+                                 stream)
+        if rc != OK:
+            raise KvcError("kvc_cache_keep", rc)
+
+    def attend(self, batch, q, out, scale, lse=None, stream=None):
+        """kvc_cache_attend: q, out [new rows, q_heads, 128]; lse: optional contiguous float32 [new rows, q_heads]."""
+        self._check(batch, (q, out), self.plan.config.q_heads)
+        rows = q.shape[0]
+        if out.shape[0] != rows or (batch.mask_rows is not None and batch.mask_rows < rows):
+            raise ValueError("out and mask have a row for every row of q")
+        if lse is not None:
+            import torch
+            if lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
+                raise ValueError("lse is a contiguous float32 tensor [new rows, q_heads]")
+        u = CacheQueries(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, rows, q.stride(0), q.stride(1),
+                         out.stride(0), out.stride(1), scale)
+        rc = _lib.kvc_cache_attend(self.plan._h, batch._ref, C.byref(u), self._pages, self._status, self._workspace, stream)
+        if rc != OK:
+            raise KvcError("kvc_cache_attend", rc)
