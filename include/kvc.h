@@ -372,8 +372,8 @@ typedef struct {
 typedef struct kvc_cache_plan_s kvc_cache_plan_t;      /* opaque, host memory */
 
 /*
- * Validates a configuration and fixes the limits of the calls: tokens of a sequence, new rows of a
- * sequence in one call (new tokens in kvc_cache_attend), sequences.  Touches no device; read-only
+ * Validates a configuration and fixes the limits of the calls: tokens of a sequence, new tokens of a
+ * sequence in one kvc_cache_attend (the other calls take any number), sequences of a call.  Touches no device; read-only
  * afterwards, so several threads may use one plan.  KVC_ERR_ARG / KVC_ERR_UNSUPPORTED / KVC_ERR_CAPACITY
  * as for kvc_plan; *out = NULL on error.
  */

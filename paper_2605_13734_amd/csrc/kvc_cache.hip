@@ -14,6 +14,7 @@ struct kvc_cache_plan_s {
 namespace kvc {
 
 constexpr long long kAttendGroups = 1024;    // workgroups that the tokens of few rows are spread over (four per compute unit)
+constexpr long long kWideGroups = 512;       // ... of many rows (two per compute unit, which is all that LDS has room for)
 constexpr int kMostSplits = 256;
 constexpr int kLeastChunk = 256;             // tokens of a workgroup: two steps of its four waves at least
 constexpr size_t kPartBytes = (kDim + 2) * sizeof(float);
@@ -26,10 +27,10 @@ static AttendShape attend_shape(const kvc_cache_config &f, int n, int max_new, i
 {
     AttendShape s;
     const int64_t rows = (int64_t)max_new * (f.q_heads / f.kv_heads);
-    s.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    s.tiles = rows <= 16 ? 1 : rows <= 64 ? 2 : kWideTiles;
     s.row_blocks = (int)((rows + 16 * s.tiles - 1) / (16 * s.tiles));
     const int64_t groups = (int64_t)n * f.kv_heads * s.row_blocks;
-    int64_t splits = kAttendGroups / groups;
+    int64_t splits = (s.tiles == kWideTiles ? kWideGroups : kAttendGroups) / groups;
     const int64_t most = (max_tokens + kLeastChunk - 1) / kLeastChunk;
     splits = splits > most ? most : splits;
     splits = splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits;
@@ -48,13 +49,14 @@ static CacheTypes types_of(const kvc_cache_config &f)
 
 static bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
-// The checks that all calls share; fills the view.
-static int check_call(const kvc_cache_plan_t *plan, const kvc_cache_batch *b, void *pages, int32_t *status, int64_t rows, CacheView *c)
+// The checks that all calls share; fills the view.  most_new: the call's bound of new rows.
+static int check_call(const kvc_cache_plan_t *plan, const kvc_cache_batch *b, void *pages, int32_t *status, int64_t rows, int64_t most_new,
+                      CacheView *c)
 {
     if (!plan || !b) return KVC_ERR_ARG;
     const kvc_cache_config &f = plan->config;
     if (b->n < 0 || b->max_new < 0 || b->max_tokens < 0 || b->num_pages < 0 || b->table_stride < 0 || rows < 0) return KVC_ERR_ARG;
-    if (b->n > plan->max_batch || b->max_new > plan->max_new || b->max_tokens > plan->max_tokens) return KVC_ERR_CAPACITY;
+    if (b->n > plan->max_batch || b->max_new > most_new || b->max_tokens > plan->max_tokens) return KVC_ERR_CAPACITY;
     if (b->n == 0 || b->max_new == 0 || b->max_tokens == 0) return KVC_OK;
     if (!b->new_start || !b->tokens || !b->block_table || !pages || !status) return KVC_ERR_ARG;
     if (!aligned(b->new_start, 4) || !aligned(b->tokens, 4) || !aligned(b->block_table, 4) || !aligned(status, 4) || !aligned(pages, 16) ||
@@ -88,7 +90,7 @@ static int rows_call(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch,
 {
     CacheView c;
     if (!r) return KVC_ERR_ARG;
-    const int rc = check_call(plan, batch, pages, status, r->rows, &c);
+    const int rc = check_call(plan, batch, pages, status, r->rows, INT32_MAX, &c);
     if (rc != KVC_OK || nothing(batch)) return rc;
     if ((r->rows && (!r->k || !r->v)) || !aligned(r->k, 16) || !aligned(r->v, 16) || !strides_ok(r->stride_row, r->stride_head)) return KVC_ERR_ARG;
     launch_cache_rows(types_of(plan->config), c, store, (uint16_t *)r->k, (uint16_t *)r->v, r->stride_row, r->stride_head, batch->n,
@@ -113,10 +115,8 @@ extern "C" int kvc_cache_plan(const kvc_cache_config *config, int64_t max_tokens
     const bool pages = f.block_tokens >= kGranule && f.block_tokens <= 4096 && (f.block_tokens & (f.block_tokens - 1)) == 0;
     if (!widths || !pages || f.head_dim != kDim || f.transform > KVC_T_HADAMARD || f.q_heads > 65536 || max_batch > 65535)
         return KVC_ERR_UNSUPPORTED;
-    // (row and token numbers are ints in the kernels, rows of a head in the grid's second dimension)
-    if (max_tokens > 0x7fffff00ll || (int64_t)max_new * f.q_heads > 0x3fffffffll ||
-        (int64_t)f.kv_heads * (((int64_t)max_new * (f.q_heads / f.kv_heads) + 15) / 16) > 65535)
-        return KVC_ERR_CAPACITY;
+    // (row and token numbers are ints in the kernels, and so are the places of a launch)
+    if (max_tokens > 0x7fffff00ll || (int64_t)max_new * f.q_heads > 0x3fffffffll) return KVC_ERR_CAPACITY;
     kvc_cache_plan_t *p = new (std::nothrow) kvc_cache_plan_t;
     if (!p) return KVC_ERR_CAPACITY;
     p->config = f;
@@ -124,12 +124,12 @@ extern "C" int kvc_cache_plan(const kvc_cache_config *config, int64_t max_tokens
     p->max_new = max_new;
     p->max_batch = max_batch;
     p->page_bytes = (size_t)f.kv_heads * (f.block_tokens / kGranule) * granule_map(f.bits_k, f.bits_v, f.group).bytes;
-    // a call has at most kAttendGroups workgroups where it divides the tokens, with 64 rows each, and no more
+    // a call has at most kAttendGroups workgroups where it divides the tokens, with kWideRows rows each, and no more
     // than kMostSplits results per row
     const int64_t rows = (int64_t)max_batch * max_new * f.q_heads;
     int64_t most = (max_tokens + kLeastChunk - 1) / kLeastChunk;
     most = most > kMostSplits ? kMostSplits : most;
-    const int64_t parts = rows * most < kAttendGroups * 64 ? rows * most : kAttendGroups * 64;
+    const int64_t parts = rows * most < kAttendGroups * kWideRows ? rows * most : kAttendGroups * kWideRows;
     p->workspace = most > 1 ? (size_t)parts * kPartBytes : 0;
     *out = p;
     return KVC_OK;
@@ -158,7 +158,7 @@ extern "C" int kvc_cache_keep(const kvc_cache_plan_t *plan, const kvc_cache_batc
 {
     using namespace kvc;
     CacheView c;
-    const int rc = check_call(plan, batch, pages, dev_status, INT64_MAX, &c);
+    const int rc = check_call(plan, batch, pages, dev_status, INT64_MAX, INT32_MAX, &c);
     if (rc != KVC_OK || nothing(batch)) return rc;
     if (!keep_start || (keep_rows && !keep) || keep_rows < 0 || keep_rows > 0x7fffffffll || !aligned(keep_start, 4) || !aligned(keep, 4)) return KVC_ERR_ARG;
     launch_cache_keep(types_of(plan->config), c, keep_start, keep, (int)keep_rows, batch->n, (hipStream_t)hip_stream);
@@ -172,7 +172,7 @@ extern "C" int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_ba
     if (!queries) return KVC_ERR_ARG;
     const kvc_cache_queries &u = *queries;
     AttendArgs a;
-    const int rc = check_call(plan, batch, (void *)pages, dev_status, u.rows, &a.c);
+    const int rc = check_call(plan, batch, (void *)pages, dev_status, u.rows, plan ? plan->max_new : 0, &a.c);
     if (rc != KVC_OK || nothing(batch)) return rc;
     if ((u.rows && (!u.q || !u.out)) || !aligned(u.q, 16) || !aligned(u.out, 16) || !aligned(u.lse, 4) || !strides_ok(u.q_stride_row, u.q_stride_head) ||
         !strides_ok(u.out_stride_row, u.out_stride_head) || !(u.scale >= -3.0e38f && u.scale <= 3.0e38f)) return KVC_ERR_ARG;
@@ -200,6 +200,7 @@ extern "C" int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_ba
     a.splits = s.splits;
     a.chunk = s.chunk;
     a.dtype = f.dtype;
+    a.rotate = f.transform == KVC_T_HADAMARD;
     const CacheTypes t = types_of(f);
     const hipStream_t stream = (hipStream_t)hip_stream;
     if (f.bits_k == 4 && f.bits_v == 4) launch_attend<44>(t, a, s.tiles, batch->n, stream);

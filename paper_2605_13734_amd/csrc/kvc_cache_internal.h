@@ -32,11 +32,13 @@ struct AttendArgs {
     int per_kv;                    // query heads per KV head
     int row_blocks;                // of 16 * tiles query rows, in the longest sequence
     int splits, chunk;             // tokens of a sequence per workgroup (a multiple of 128)
-    int dtype;
+    int dtype, rotate;
 };
 
-// The attention of one pair of code widths (10 * bits_k + bits_v) with 1, 2 or 4 tiles of 16 query rows per wave, and the kernel that
-// joins the results of several workgroups per row.
+constexpr int kWideRows = 128, kWideTiles = kWideRows / 16;
+
+// The attention of one pair of code widths (10 * bits_k + bits_v) with 1 or 2 tiles of 16 query rows per workgroup or (kWideTiles) 128
+// rows, and the kernel that joins the results of several workgroups per row.
 template <int BITS> void launch_attend(const CacheTypes &t, const AttendArgs &a, int tiles, int n, hipStream_t stream);
 template <> void launch_attend<44>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);
 template <> void launch_attend<48>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);

@@ -353,7 +353,8 @@ class Buffers:
 # ---- the quantised cache ------------------------------------------------------------------------
 
 class CachePlan:
-    """kvc_cache_plan / kvc_cache_plan_free: configuration and limits of a cache held in the quantiser's codes."""
+    """kvc_cache_plan / kvc_cache_plan_free: configuration and limits of a cache held in the quantiser's codes.  max_new: new
+    tokens of a sequence in one attention."""
 
     def __init__(self, dtype, kv_heads, q_heads, head_dim=128, bits_k=4, bits_v=4, group=32, block_tokens=16, transform=0,
                  max_batch=1, max_tokens=0, max_new=1):

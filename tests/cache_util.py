@@ -45,7 +45,7 @@ class World:
         self.tokens = torch.tensor(self.total, dtype=torch.int32, device=device)
         limits = limits or {}
         self.plan = kvc.CachePlan(kvc.BF16 if bf16 else kvc.F16, kv_heads, kv_heads * per_kv, DIM, bits_k, bits_v, group, block_tokens,
-                                  transform, max_batch=n, max_tokens=limits.get("tokens", self.most), max_new=self.most)
+                                  transform, max_batch=n, max_tokens=limits.get("tokens", self.most), max_new=self.most_new)
         self.cache = kvc.Cache(self.plan, self.num_pages, device)
         self.cache.pages.fill_(0xff)            # (what nobody wrote is NaN as a scale or zero)
 

@@ -36,7 +36,7 @@ def test_plans(lib):
         with pytest.raises(kvc.KvcError) as e:
             plan(**kw)
         assert e.value.status == -2, kw
-    for kw in [dict(max_tokens=1 << 31), dict(max_new=1 << 28), dict(kv_heads=64, q_heads=64, max_new=1 << 15)]:
+    for kw in [dict(max_tokens=1 << 31), dict(max_new=1 << 28), dict(kv_heads=64, q_heads=64, max_new=1 << 25)]:
         with pytest.raises(kvc.KvcError) as e:
             plan(**kw)
         assert e.value.status == -3, kw
@@ -82,7 +82,7 @@ class Args:
                 "attend": lambda: lib.kvc_cache_attend(self.p._h, b, C.byref(self.queries), self.pages, self.status, self.workspace, None)}
 
 
-BATCH = [(dict(n=-1), -1), (dict(n=4), -3), (dict(max_new=5), -3), (dict(max_new=-1), -1), (dict(max_tokens=1001), -3), (dict(max_tokens=-1), -1),
+BATCH = [(dict(n=-1), -1), (dict(n=4), -3), (dict(max_new=-1), -1), (dict(max_tokens=1001), -3), (dict(max_tokens=-1), -1),
          (dict(new_start=None), -1), (dict(tokens=None), -1), (dict(block_table=None), -1), (dict(new_start=0x1002), -1),
          (dict(table_stride=62), -1), (dict(table_stride=-1), -1), (dict(num_pages=-1), -1), (dict(mask=0x9000, mask_words=0), -1),
          (dict(mask=0x9004, mask_words=1), -1)]
@@ -95,6 +95,13 @@ def test_sequences_that_are_refused(lib, change, want):
         for k, v in change.items():
             setattr(a.batch, k, v)
         assert a.calls(lib)[name]() == want, name
+
+
+def test_new_tokens_of_an_attention(lib):
+    """The plan bounds them for the attention alone."""
+    a = Args(plan())
+    a.batch.max_new = 5
+    assert a.calls(lib)["attend"]() == -3
 
 
 def test_tensors_that_are_refused(lib):
