@@ -4,7 +4,7 @@
 //
 // A workgroup has 16 * TILES query rows of one KV head (a row: one new token and one of the query heads that share the KV head)
 // and a run of the sequence's tokens, of which its four waves take 32 at a time in turn; the waves' results are joined in
-// LDS.  Where rows are few the tokens of a sequence are spread over several workgroups, whose results a second kernel joins.
+// LDS.  The tokens of long sequences are spread over several workgroups, whose results the last of them joins.
 //
 // Scores: the matrix product runs over the codes themselves, with 16 tokens as rows and 16 query rows as columns.  A code, masked
 // out of its word together with a second one, is a half-precision subnormal, code * 2^-24 (or 2^-20), which the matrix
@@ -29,7 +29,7 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 32;                    // tokens per wave and step
-constexpr int kWaves = 4;
+constexpr int kManyWaves = 4;
 constexpr float kSlack = 8.0f;               // the maximum may grow by 2^8 before the sums are rescaled
 constexpr float kBias = 6.0f;                // weights are kept as 2^(6 + score - maximum) <= 2^14
 // A score that is not seen is kLowest before the factor, which is kept at 2^-60 or more (products stay below 2^40: scores below 2^-20
@@ -78,10 +78,13 @@ template <int BITS_K, int BITS_V, int GROUP> struct RawGranule {
     u32x2 ks[groups];                        // scales of 4 tokens
     uint32_t kz[(groups + 1) / 2];           // zeros of one token
 
-    __device__ __forceinline__ void load_codes(const uint8_t *p, const LanePlaces<BITS_K, BITS_V, GROUP> &at)
+    __device__ __forceinline__ void load_keys(const uint8_t *p, const LanePlaces<BITS_K, BITS_V, GROUP> &at)
     {
 #pragma unroll
         for (int h = 0; h < BITS_K / 4; ++h) k[h] = *(const u32x4 *)(p + at.k + h * 1024u);
+    }
+    __device__ __forceinline__ void load_values(const uint8_t *p, const LanePlaces<BITS_K, BITS_V, GROUP> &at)
+    {
 #pragma unroll
         for (int h = 0; h < BITS_V / 4; ++h) v[h] = *(const u32x4 *)(p + at.v + h * 1024u);
         vp = *(const u32x4 *)(p + at.vp);
@@ -122,16 +125,24 @@ template <int BITS> __device__ __forceinline__ half8 key_operand(const u32x4 *k,
     return __builtin_bit_cast(half8, u32x4{p[0], p[1], p[2], p[3]});
 }
 
+// (x & mask) | bits in one instruction (the compiler takes two, each with a literal)
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits)
+{
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(mask), "v"(bits));
+    return r;
+}
+
 // Channel 8 i + c of tokens t0, t1 (the words of their octets): code * scale + zero in both halves.
 template <int BITS> __device__ __forceinline__ uint32_t value_pair(uint32_t pair, int c, half2v scale, half2v zero)
 {
     uint32_t bits;
     _Float16 offset;
     if (BITS == 4 && (c & 1)) {
-        bits = (pair & 0x00f000f0u) | 0x54005400u;            // 64 + code
+        bits = and_or(pair, 0x00f000f0u, 0x54005400u);        // 64 + code
         offset = (_Float16)64.0f;
     } else {
-        bits = (BITS == 4 ? pair & 0x000f000fu : pair) | 0x64006400u;       // 1024 + code
+        bits = BITS == 4 ? and_or(pair, 0x000f000fu, 0x64006400u) : pair | 0x64006400u;       // 1024 + code
         offset = (_Float16)1024.0f;
     }
     const half2v code = __builtin_bit_cast(half2v, bits) - half2v{offset, offset};
@@ -182,18 +193,43 @@ template <int BITS_K, int GROUP, bool ROTATE> struct QueryTile {
     float factor;                            // scores in base 2 = products * factor (not negative)
     int draft;                               // the row's new token
 
-    __device__ __forceinline__ void load(const AttendArgs &a, const Sequence &seq, int head, int row, int rows)
+    __device__ __forceinline__ void fetch(const AttendArgs &a, const Sequence &seq, int head, int row, int rows)
     {
-        constexpr int groups = kDim / GROUP;
-        const int lane = lane_id(), q = lane >> 4;
+        const int q = lane_id() >> 4;
         const bool there = row < rows;
         draft = there ? row / a.per_kv : 0;
         const uint16_t *from = a.q + (long long)(seq.row0 + draft) * a.q_row + (long long)(head * a.per_kv + row % a.per_kv) * a.q_head + 8 * q;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) part[g] = there ? *(const half8 *)(from + 32 * g) : half8{};
+    }
+    // Prepared queries through LDS: what one wave has made, for all waves of the workgroup.
+    static constexpr int kPlaces = 4 * PARTS + 1;
+    __device__ __forceinline__ void put(u32x4 (*to)[64]) const
+    {
+        const int lane = lane_id();
+#pragma unroll
+        for (int g = 0; g < 4 * PARTS; ++g) to[g][lane] = __builtin_bit_cast(u32x4, part[g]);
+        const u32x2 s = __builtin_bit_cast(u32x2, sums);
+        to[4 * PARTS][lane] = u32x4{s[0], s[1], __float_as_uint(factor), (uint32_t)draft};
+    }
+    __device__ __forceinline__ void get(const u32x4 (*from)[64])
+    {
+        const int lane = lane_id();
+#pragma unroll
+        for (int g = 0; g < 4 * PARTS; ++g) part[g] = __builtin_bit_cast(half8, from[g][lane]);
+        const u32x4 w = from[4 * PARTS][lane];
+        sums = __builtin_bit_cast(half4, u32x2{w[0], w[1]});
+        factor = __uint_as_float(w[2]);
+        draft = (int)w[3];
+    }
+    __device__ __forceinline__ void prepare(const AttendArgs &a)
+    {
+        constexpr int groups = kDim / GROUP;
+        const int lane = lane_id(), q = lane >> 4;
         float x[4][8];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            u32x4 r = {0, 0, 0, 0};
-            if (there) r = *(const u32x4 *)(from + 32 * g);
+            const u32x4 r = __builtin_bit_cast(u32x4, part[g]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[g][e] = a.dtype == DT_F16 ? elem_f32<DT_F16>(r, e) : elem_f32<DT_BF16>(r, e);
         }
@@ -271,31 +307,37 @@ template <int BITS_K, int GROUP, bool ROTATE> struct QueryTile {
     }
 };
 
-// Scores of one granule and tile from the codes: products per group, scales in 32 bits, zeros by one more product.
-template <int GROUP, typename Query>
-__device__ __forceinline__ void scores_of(const half8 key[4], half4 zeros, const u32x2 *ks, const Query &query, float score[4])
-{
-    constexpr int groups = kDim / GROUP;
-    f32x4 dot[groups];
+// Scores of one granule and tile from the codes: products per group and one of the zeros ...
+template <int GROUP> struct Products {
+    static constexpr int groups = kDim / GROUP;
+    f32x4 dot[groups], offset;
+
+    template <typename Query> __device__ __forceinline__ void make(const half8 key[4], half4 zeros, const Query &query)
+    {
 #pragma unroll
-    for (int g = 0; g < groups; ++g) dot[g] = f32x4{0, 0, 0, 0};
+        for (int g = 0; g < groups; ++g) dot[g] = f32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int p = 0; p < Query::PARTS; ++p)
+        for (int p = 0; p < Query::PARTS; ++p)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-            dot[g * groups / 4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[g], query.part[4 * p + g], dot[g * groups / 4], 0, 0, 0);
-    const f32x4 offset = __builtin_amdgcn_mfma_f32_16x16x16f16(zeros, query.sums, f32x4{0, 0, 0, 0}, 0, 0, 0);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        float sum = 0.0f;
+            for (int g = 0; g < 4; ++g)
+                dot[g * groups / 4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[g], query.part[4 * p + g], dot[g * groups / 4], 0, 0, 0);
+        offset = __builtin_amdgcn_mfma_f32_16x16x16f16(zeros, query.sums, f32x4{0, 0, 0, 0}, 0, 0, 0);
+    }
+    // ... and the scales in 32 bits (a half of a register each, read as it is).
+    __device__ __forceinline__ void scores(const u32x2 *ks, float score[4]) const
+    {
+        float sum[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int g = 0; g < groups; ++g) {
-            const half2v scales = __builtin_bit_cast(half2v, (uint32_t)ks[g][e >> 1]);
-            sum = __builtin_fmaf((float)scales[e & 1], dot[g][e], sum);      // (reads the half of the register as it is)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sum[e] = __builtin_fmaf((float)__builtin_bit_cast(half2v, (uint32_t)ks[g][e >> 1])[e & 1], dot[g][e], sum[e]);
+            __builtin_amdgcn_sched_barrier(0x7fe);           // (four sums in turn: nothing but vector arithmetic stays in place)
         }
-        score[e] = __builtin_fmaf(sum, 16777216.0f, offset[e]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) score[e] = __builtin_fmaf(sum[e], 16777216.0f, offset[e]);
     }
-}
+};
 
 // Running softmax of one tile: maximum (base 2, the same in the row's four lanes), sum of weights, and the sums of weighted values,
 // channel 32 q + 8 e + ch of row i in out[ch][e].
@@ -326,24 +368,31 @@ template <int PARTS> struct RowState {
 #pragma unroll
             for (int ch = 0; ch < 8; ++ch) out[ch] *= shrink;
         }
-        const float down = kBias - top;
+        const float down = kBias - top, one_f32 = opaque_one();
         constexpr _Float16 one = (_Float16)1.0f;
         constexpr half8 ones = {one, one, one, one, one, one, one, one};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(score[e], factor, down));
-            weight[0][e] = (_Float16)w;
-            if (PARTS == 1) norm[0] += w;
-            if (PARTS == 2) weight[PARTS - 1][e] = (_Float16)__builtin_fmaf((float)weight[0][e], -1.0f, w);
+        for (int e = 0; e < 8; e += 2) {
+            const f32x2_t w = {__builtin_amdgcn_exp2f(__builtin_fmaf(score[e], factor, down)),
+                               __builtin_amdgcn_exp2f(__builtin_fmaf(score[e + 1], factor, down))};
+            const half2v high = __builtin_convertvector(w, half2v);
+            weight[0][e] = high[0];
+            weight[0][e + 1] = high[1];
+            if (PARTS == 1) norm[0] += w[0] + w[1];
+            else {                           // (the halves are read as they are)
+                const f32x2_t rest = {__builtin_fmaf((float)high[0], -one_f32, w[0]), __builtin_fmaf((float)high[1], -one_f32, w[1])};
+                const half2v low = __builtin_convertvector(rest, half2v);
+                weight[PARTS - 1][e] = low[0];
+                weight[PARTS - 1][e + 1] = low[1];
+            }
         }
         if (PARTS == 1) return;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) norm = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, weight[p], norm, 0, 0, 0);
     }
-    __device__ __forceinline__ void add(int ch, half8 values, const half8 weight[PARTS])
+    __device__ __forceinline__ void add(int ch, half8 values, const half8 &weight)
     {
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) out[ch] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, weight[p], out[ch], 0, 0, 0);
+        out[ch] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, weight, out[ch], 0, 0, 0);
     }
 };
 
@@ -372,33 +421,29 @@ __device__ __forceinline__ u32x4 only_there(u32x4 vp, bool page, int first_token
     return u32x4{vp[0] & low, vp[1] & high, vp[2] & low, vp[3] & high};
 }
 
-// Operands of the product over tokens for channels 8 i + ch, ch = 0..7, one after the other: f(ch, operand).
+// Operands of the product over tokens for channels 8 i + ch, two at a time (what follows on a product has another one in between):
+// f(ch, operand of ch, operand of ch + 1), ch even.
 template <int BITS_V, typename Raw, typename F> __device__ __forceinline__ void value_operands(const Raw *r, F f)
 {
 #pragma unroll
-    for (int half = 0; half < BITS_V / 4; ++half)
+    for (int ch = 0; ch < 8; ch += 2) {
+        u32x4 w[2];
 #pragma unroll
-        for (int byte = 0; byte < 4; ++byte) {
-            uint32_t pair[4];
+        for (int which = 0; which < 2; ++which)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                pair[e] = __builtin_amdgcn_perm(r[e >> 1].v[half][2 * (e & 1) + 1], r[e >> 1].v[half][2 * (e & 1)],
-                                                0x0c040c00u + (uint32_t)byte * 0x00010001u);
-#pragma unroll
-            for (int nibble = 0; nibble < 8 / BITS_V; ++nibble) {
-                const int ch = BITS_V == 4 ? 2 * byte + nibble : 4 * half + byte;
-                u32x4 w;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    w[e] = value_pair<BITS_V>(pair[e], ch, __builtin_bit_cast(half2v, (uint32_t)r[e >> 1].vp[e & 1]),
-                                              __builtin_bit_cast(half2v, (uint32_t)r[e >> 1].vp[2 + (e & 1)]));
-                f(ch, __builtin_bit_cast(half8, w));
+            for (int e = 0; e < 4; ++e) {
+                const int word = BITS_V == 4 ? 0 : ch >> 2, byte = BITS_V == 4 ? ch >> 1 : (ch + which) & 3;
+                const uint32_t pair = __builtin_amdgcn_perm(r[e >> 1].v[word][2 * (e & 1) + 1], r[e >> 1].v[word][2 * (e & 1)],
+                                                            0x0c040c00u + (uint32_t)byte * 0x00010001u);
+                w[which][e] = value_pair<BITS_V>(pair, ch + which, __builtin_bit_cast(half2v, (uint32_t)r[e >> 1].vp[e & 1]),
+                                                 __builtin_bit_cast(half2v, (uint32_t)r[e >> 1].vp[2 + (e & 1)]));
             }
-        }
+        f(ch, __builtin_bit_cast(half8, w[0]), __builtin_bit_cast(half8, w[1]));
+    }
 }
 
-// Pages of a wave's coming steps of 32 tokens: step n is granules first + 2 (kWaves n + wave) and the one behind it.
-struct PageWindow {
+// Pages of a wave's coming steps of 32 tokens: step n is granules first + 2 (WAVES n + wave) and the one behind it.
+template <int WAVES> struct PageWindow {
     int entries, ahead;                      // lane l: the page of granule l & 1 of step ahead + (l >> 1)
 
     __device__ __forceinline__ void start() { ahead = -32; }
@@ -407,7 +452,7 @@ struct PageWindow {
     {
         if (n == ahead + 32) {
             ahead = n;
-            const int lane = lane_id(), j = first + 2 * (kWaves * (n + (lane >> 1)) + wave) + (lane & 1);
+            const int lane = lane_id(), j = first + 2 * (WAVES * (n + (lane >> 1)) + wave) + (lane & 1);
             entries = page_of(c, s, j < last ? j : last);        // (behind the end: the last one's page, and a place in it)
             if (entries < 0) atomicOr(c.status + s, KVC_DEV_BAD_BLOCK);
         }
@@ -415,64 +460,384 @@ struct PageWindow {
     }
 };
 
+// ---- which tokens of which sequence a workgroup has ---------------------------------------------------
+
+// A part of a sequence: `count` parts of `chunk` tokens each, this is number `index`.  Parts of a sequence with several of them leave
+// their results in slots slot0 ... slot0 + count - 1 (times the heads and blocks of rows).
+struct Part {
+    int s, index, count, slot0;
+    long long chunk;
+};
+
+// Sum over the wave's lanes up to and with this one.
+__device__ __forceinline__ unsigned sum_upto(unsigned x)
+{
+    // inside rows of 16, then the last lanes of the rows before (two steps)
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);       // row_shr:1
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);       // row_shr:2
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);       // row_shr:4
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);       // row_shr:8
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);       // row_bcast:15
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);       // row_bcast:31
+    return x;
+}
+__device__ __forceinline__ float max_of_row(float x)         // over the 16 lanes
+{
+    x = fmaxf(x, dpp_f32<DPP_QUAD_XOR1>(x));
+    x = fmaxf(x, dpp_f32<DPP_QUAD_XOR2>(x));
+    x = fmaxf(x, dpp_f32<DPP_HALF_MIRROR>(x));
+    return fmaxf(x, dpp_f32<DPP_MIRROR>(x));
+}
+__device__ __forceinline__ float sum_of_row(float x)
+{
+    x += dpp_f32<DPP_QUAD_XOR1>(x);
+    x += dpp_f32<DPP_QUAD_XOR2>(x);
+    x += dpp_f32<DPP_HALF_MIRROR>(x);
+    return x + dpp_f32<DPP_MIRROR>(x);
+}
+
+// Part u of the call, in all waves.  The lengths are on the device, so the division is made here, from the lengths of up to 256 sequences
+// in units of STEP tokens.  The measure is a piece length: the shortest with which the pieces of all sequences fit the chip at
+// once (per head and block of rows); or, with more sequences than that, twice an even share, so that only the longest are cut.
+// A sequence is then cut into equal pieces of that length at most; nothing is cut where that would save less than joining costs
+// (a.joining units).  With more than 256 sequences a piece is a whole one.  False: there is no part u, or nothing in it.
+template <int STEP> __device__ __forceinline__ bool find_part(const AttendArgs &a, int u, Part &p, Sequence &seq)
+{
+    const CacheView &c = a.c;
+    if (!a.divide) {
+        if (u >= a.n) return false;
+        p = Part{u, 0, 1, 0, 1ll << 40};
+        seq = sequence_of(c, u);
+        return true;
+    }
+    const int lane = lane_id();
+    Sequence of[4];
+    int units[4], busy = 0, longest = 0;
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        units[k] = 0;
+        if (64 * k < a.n) {
+            const int s = 64 * k + lane;
+            if (s < a.n) {
+                of[k].row0 = c.new_start[s];
+                of[k].fresh = (int)((unsigned)c.new_start[s + 1] - (unsigned)of[k].row0);
+                of[k].tokens = c.tokens[s];
+                const bool fit = fits(c, of[k]);
+                if (fit && of[k].fresh) units[k] = (int)(((unsigned)of[k].tokens + STEP - 1u) / STEP);
+                if (!fit && blockIdx.x == 0 && threadIdx.x < 64) atomicOr(c.status + s, KVC_DEV_BAD_ROW);     // (no workgroup comes to it)
+            }
+            sum += (float)units[k];
+            longest = units[k] > longest ? units[k] : longest;
+            busy += __popcll(__ballot(units[k] > 0));
+        }
+    }
+    if (busy == 0) return false;
+    longest = __builtin_amdgcn_readfirstlane((int)row_max(max_of_row((float)longest)));
+    // in units; joining takes time by the number of pieces, so that piece + a.joining_piece * longest / piece is to be small
+    int piece = __builtin_amdgcn_readfirstlane((int)__builtin_amdgcn_sqrtf(a.joining_piece * (float)longest)) + 1;
+    if (a.n == 1) {
+        const int even = (longest + a.parts - 1) / a.parts;
+        piece = even > piece ? even : piece;
+    } else {
+        sum = row_sum(sum_of_row(sum));
+        if (busy > a.parts) {
+            const int even = __builtin_amdgcn_readfirstlane((int)(2.0f * sum / (float)a.parts)) + 1;
+            piece = even > piece ? even : piece;
+        } else if (longest > piece) {
+            // between an even share and one that leaves room for a shorter last piece of every sequence, by bisection
+            const int even = __builtin_amdgcn_readfirstlane((int)(sum * 0.9999f / (float)a.parts));
+            piece = even > piece ? even : piece;
+            int most = longest;
+            if (busy < a.parts) {
+                const int roomy = __builtin_amdgcn_readfirstlane((int)(sum * 1.0001f / (float)(a.parts - busy))) + 1;
+                most = roomy < most ? roomy : most;
+            }
+            while (piece < most) {
+                const int middle = (piece + most) >> 1;
+                float made = 0.0f;           // (below 2^24: exact)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (64 * k < a.n) made += (float)(((unsigned)units[k] + (unsigned)middle - 1u) / (unsigned)middle);
+                if (row_sum(sum_of_row(made)) <= (float)a.parts) most = middle;
+                else piece = middle + 1;
+            }
+        }
+    }
+    if (piece + a.joining > longest) piece = longest;
+    // pieces of the sequences before, and slots of those of them that are cut (both below 2^16)
+    unsigned before = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (64 * k < a.n) {
+            const unsigned parts = units[k] ? ((unsigned)units[k] + (unsigned)piece - 1u) / (unsigned)piece : 0u;
+            const unsigned upto = before + sum_upto(parts | (parts > 1 ? parts << 16 : 0u));
+            const unsigned long long behind = __ballot((int)(upto & 0xffffu) > u);
+            if (behind) {
+                const int owner = __builtin_ctzll(behind);
+                const unsigned mine = __builtin_amdgcn_readlane((int)parts, owner), end = __builtin_amdgcn_readlane((int)upto, owner);
+                const unsigned whole = __builtin_amdgcn_readlane(units[k], owner);
+                p.s = 64 * k + owner;
+                p.count = (int)mine;
+                p.index = u - (int)((end & 0xffffu) - mine);
+                p.slot0 = (int)((end >> 16) - (mine > 1 ? mine : 0u));
+                p.chunk = (long long)((whole + mine - 1) / mine) * STEP;
+                seq.row0 = __builtin_amdgcn_readlane(of[k].row0, owner);
+                seq.fresh = __builtin_amdgcn_readlane(of[k].fresh, owner);
+                seq.tokens = __builtin_amdgcn_readlane(of[k].tokens, owner);
+                return true;
+            }
+            before = __builtin_amdgcn_readlane((int)upto, 63);
+        }
+    }
+    return false;
+}
+
+// ---- results of several workgroups --------------------------------------------------------------------
+
+// What workgroups leave for each other are pairs of numbers, stored as single words of agent scope: such a store goes through to memory,
+// and loads of that scope (bit 4 of a buffer load's last argument, sc1) pass by what the XCD's own L2 may have.
+// (A release of agent scope writes back a whole L2 per workgroup, 139 instead of 45 us for one token over 128k, and an acquire
+// takes 1.5 to 2.5 us.)
+__device__ __forceinline__ void leave(float *p, float a, float b)
+{
+    const unsigned long long v = (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32;
+    __hip_atomic_store((unsigned long long *)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+struct LeftRows {
+    __amdgpu_buffer_rsrc_t words;
+
+    __device__ __forceinline__ LeftRows(const float *p, long long floats)
+    {
+        words = __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(unsigned)(floats * 4), 0x27000);
+    }
+    __device__ __forceinline__ f32x4 four(unsigned at) const
+    {
+        return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(words, (int)(at * 4u), 0, 16));
+    }
+    __device__ __forceinline__ f32x2_t two(unsigned at) const
+    {
+        return __builtin_bit_cast(f32x2_t, __builtin_amdgcn_raw_buffer_load_b64(words, (int)(at * 4u), 0, 16));
+    }
+};
+
+// True in all threads of the workgroup that is the last of `count` to get here (the counter is left at zero, as it was found).  What all
+// of them have left before is then there to be taken: every wave waits for its stores to arrive before the workgroup counts.
+__device__ __forceinline__ bool last_to_arrive(int *counter, int count)
+{
+    __shared__ int order;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) order = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (order != count - 1) return false;
+    asm volatile("" ::: "memory");           // (nothing is loaded before this)
+    if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+}
+
+// Channels that lane i of sixteen has of a row that it leaves: pairs 2 i + 32 j, j = 0..3, so that the lanes' pairs lie next to each
+// other.
+constexpr int pair_at(int i, int j) { return 2 * i + 32 * j; }
+
+// Joins the parts of `rows` query rows (128 at most): part k of row r has its sums at (first + k * stride + r) * kDim of `part` and
+// (maximum, sum of weights) at twice that place of `ml`.  Sixteen lanes with eight channels each per row, or several times
+// sixteen that take turns with the parts, eight parts requested at a time, the first together with the maxima; `space` is LDS
+// for every sixteen lanes.  done(row, i, values of channels 8 i ..., maximum, sum).
+template <int THREADS, typename F>
+__device__ __forceinline__ void join_parts(const LeftRows &part, const LeftRows &ml, unsigned first, unsigned stride, int rows, int count,
+                                           float (*space)[kDim + 4], F done)
+{
+    constexpr int sets = THREADS / 16;
+    const int set = (int)threadIdx.x >> 4, i = (int)threadIdx.x & 15;
+    int side = 1;                            // rows at a time: a power of two
+    while (side < rows && 2 * side <= sets) side *= 2;
+    const int per_row = sets / side;         // (sets beyond side * per_row do nothing)
+    for (int base = 0; base < rows; base += side) {
+        const int r = base + set % side, turn = set / side;
+        const bool mine = r < rows && turn < per_row && turn < count;
+        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, highest = kLowest, total = 0.0f;
+        f32x2_t s[8];
+        f32x4 lo[8], hi[8];
+        auto request = [&](int k0) {
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                const int k = k0 + n * per_row < count ? k0 + n * per_row : k0;
+                const unsigned at = first + (unsigned)k * stride + (unsigned)r;
+                s[n] = ml.two(2 * at);
+                lo[n] = part.four(at * kDim + 8 * i);
+                hi[n] = part.four(at * kDim + 8 * i + 4);
+            }
+        };
+        if (mine) {
+            request(turn);
+            // sixteen lanes look at sixteen parts at a time
+#pragma unroll 4
+            for (int k = i; k < count; k += 16) highest = fmaxf(highest, ml.two(2 * (first + (unsigned)k * stride + (unsigned)r))[0]);
+        }
+        highest = max_of_row(highest);
+        if (mine) {
+            for (int k0 = turn; k0 < count; k0 += 8 * per_row) {
+                if (k0 > turn) request(k0);
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    const float share = k0 + n * per_row < count ? __builtin_amdgcn_exp2f(s[n][0] - highest) : 0.0f;
+                    total = __builtin_fmaf(s[n][1], share, total);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = __builtin_fmaf(lo[n][e], share, x[e]);
+                        x[4 + e] = __builtin_fmaf(hi[n][e], share, x[4 + e]);
+                    }
+                }
+            }
+        }
+        if (per_row > 1) {                   // (the same in all threads)
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) space[set][8 * i + e] = x[e];
+            if (i == 0) space[set][kDim] = total;
+            __syncthreads();
+            if (turn == 0) {
+                for (int k = 1; k < per_row; ++k) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] += space[set + k * side][8 * i + e];
+                    total += space[set + k * side][kDim];
+                }
+            }
+        }
+        if (mine && turn == 0) done(r, i, x, highest, total);
+    }
+}
+
+// Where the results of a block of query rows go.
+struct Results {
+    const AttendArgs &a;
+    const Sequence &seq;
+    int head, first;
+
+    __device__ __forceinline__ uint16_t *row(int row, int &d, int &query_head) const
+    {
+        d = (first + row) / a.per_kv;
+        query_head = head * a.per_kv + (first + row) % a.per_kv;
+        return a.out + (long long)(seq.row0 + d) * a.o_row + (long long)query_head * a.o_head;
+    }
+    __device__ __forceinline__ void lse(int d, int query_head, float highest, float total) const
+    {
+        if (a.lse) a.lse[(long long)(seq.row0 + d) * (a.c.heads * a.per_kv) + query_head] = lse_of(highest, total);
+    }
+    // eight channels in a row; `speaks`: the lane writes the row's lse
+    template <int DT> __device__ __forceinline__ void octet(int r, int channel, const float x[8], bool speaks, float highest, float total) const
+    {
+        int d, query_head;
+        uint16_t *to = row(r, d, query_head);
+        const float share = total > 0.0f ? 1.0f / total : 0.0f;
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = x[e] * share;
+        *(u32x4 *)(to + channel) = pack_row<DT>(y);
+        if (speaks) lse(d, query_head, highest, total);
+    }
+};
+
 // ---- few rows: the waves of a workgroup share rows and divide tokens --------------------------------
 
+// As many waves as the registers leave room for in a compute unit: three per SIMD, or two.
+constexpr int few_waves(int tiles, bool rotate) { return tiles == 1 && !rotate ? 12 : 8; }
+
 template <int BITS_K, int BITS_V, int GROUP, int TILES, bool ROTATE, int PARTS>
-__global__ __launch_bounds__(64 * kWaves, TILES == 1 ? 2 : 1) void attend_kernel(AttendArgs a)
+__global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROTATE) / 4) void attend_kernel(AttendArgs a)
 {
     constexpr GranuleMap map = granule_map(BITS_K, BITS_V, GROUP);
+    constexpr int waves = few_waves(TILES, ROTATE);
     typedef RawGranule<BITS_K, BITS_V, GROUP> Raw;
-    __shared__ __attribute__((aligned(16))) float sums[kWaves][16][kDim + 4];
-    __shared__ float tops[kWaves][16 * TILES], norms[kWaves][16 * TILES];
+    __shared__ __attribute__((aligned(16))) float sums[waves][16][kDim + 4];
+    __shared__ float tops[waves][16 * TILES], norms[waves][16 * TILES];
 
     const CacheView &c = a.c;
-    const int s = blockIdx.z, split = (int)(blockIdx.x % (unsigned)a.splits), place = (int)(blockIdx.x / (unsigned)a.splits);
-    const int head = place % c.heads, block = place / c.heads;
     const int lane = lane_id(), wave = wave_id(), q = lane >> 4, i = lane & 15;
-    const Sequence seq = sequence_of(c, s);
+    const int each = c.heads * a.row_blocks, u = (int)(blockIdx.x / (unsigned)each), rest = (int)(blockIdx.x % (unsigned)each);
+    const int head = rest % c.heads, block = rest / c.heads;
+    Part part;
+    Sequence seq;
+    if (!find_part<kStep * waves>(a, u, part, seq)) return;
+    const int s = part.s;
     const int first = block * 16 * TILES, rows = seq.fresh * a.per_kv;
     if (first >= rows) return;
     const int limit = tokens_seen(c, seq, block, 16 * TILES, a.per_kv), past = seq.tokens - seq.fresh;
-    const long long start = (long long)split * a.chunk;
-    if (start >= limit) return;
-    const int begin = (int)start;
-    const int end = start + a.chunk < limit ? begin + a.chunk : limit;
+    const int count = (int)((limit + part.chunk - 1) / part.chunk);      // (of this block of rows)
+    if (part.index >= count) return;
+    const int begin = (int)(part.index * part.chunk);
+    const int end = begin + part.chunk < limit ? (int)(begin + part.chunk) : limit;
 
     // overflow of half-precision arithmetic ends at 65504 instead of infinity (bit 23 of the mode register)
     __builtin_amdgcn_s_setreg((0 << 11) | (23 << 6) | 1, 1);
 
-    QueryTile<BITS_K, GROUP, ROTATE> query[TILES];
-    RowState<PARTS> state[TILES];
+    // ---- tokens: the wave's step n is 32 tokens from begin + 32 * (waves * n + wave); the first are requested before the queries
+    const int steps = (end - begin + kStep - 1) / kStep;
+    const int mine = steps > wave ? (steps - wave + waves - 1) / waves : 0;
     LanePlaces<BITS_K, BITS_V, GROUP> at;
     at.set();
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-        query[t].load(a, seq, head, first + 16 * t + i, rows);
-        state[t].clear();
-    }
-
-    // ---- tokens: the wave's step n is 32 tokens from begin + 32 * (4 n + wave)
-    const int steps = (end - begin + kStep - 1) / kStep;
-    const int mine = steps > wave ? (steps - wave + kWaves - 1) / kWaves : 0;
-    PageWindow window;
+    PageWindow<waves> window;
     window.start();
-    auto load = [&](Raw *r, bool *there, int n) {
+    // The granules of a step: where they are, and whether their pages are there.
+    struct Step {
+        const uint8_t *at[2];
+        bool there[2];
+    };
+    auto find = [&](int n) {
+        Step f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int page = window.page(c, s, begin >> 4, wave, (end - 1) >> 4, n, h);
-            there[h] = page >= 0;
-            const uint8_t *p = c.pages + granule_at(c, page < 0 ? 0 : page, (begin >> 4) + 2 * (kWaves * n + wave) + h, head, map.bytes);
-            r[h].load_codes(p, at);
-            r[h].load_scales(p, at);
+            f.there[h] = page >= 0;
+            f.at[h] = c.pages + granule_at(c, page < 0 ? 0 : page, (begin >> 4) + 2 * (waves * n + wave) + h, head, map.bytes);
+        }
+        return f;
+    };
+    auto load_keys = [&](Raw *r, const Step &f) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            r[h].load_keys(f.at[h], at);
+            r[h].load_scales(f.at[h], at);
         }
     };
-    auto step = [&](Raw *r, const bool *there, int n) {
-        const int token = begin + kStep * (kWaves * n + wave);
-        const bool all = token + kStep <= past && token + kStep <= end && there[0] && there[1];
-        if (!all) {
+    auto load_values = [&](Raw *r, const Step &f) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) r[h].vp = only_there(r[h].vp, there[h], token + 16 * h, seq.tokens);
+        for (int h = 0; h < 2; ++h) r[h].load_values(f.at[h], at);
+    };
+    typedef QueryTile<BITS_K, GROUP, ROTATE> Query;
+    static_assert(sizeof(u32x4) * 64 * Query::kPlaces * TILES <= sizeof(sums), "the queries go through the room of the sums");
+    u32x4(*shared_queries)[64] = (u32x4(*)[64])sums;
+    Query query[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+        if (wave == t) query[t].fetch(a, seq, head, first + 16 * t + i, rows);
+    Raw now[2];
+    Step now_at = {}, next_at = {};
+    if (mine > 0) {
+        now_at = find(0);
+        load_keys(now, now_at);
+        load_values(now, now_at);
+    }
+    RowState<PARTS> state[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+        if (wave == t) {                     // one wave per tile prepares it for all of them
+            query[t].prepare(a);
+            query[t].put(shared_queries + t * Query::kPlaces);
         }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+        query[t].get(shared_queries + t * Query::kPlaces);
+        state[t].clear();
+    }
+    __syncthreads();                         // (before the room is the sums' again)
+    // Scores and weights of step n, from r's keys ...
+    auto weigh = [&](Raw *r, const Step &f, int n, half8 (*weight)[PARTS]) {
+        const int token = begin + kStep * (waves * n + wave);
+        const bool all = token + kStep <= past && token + kStep <= end && f.there[0] && f.there[1];
         float score[TILES][8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -480,29 +845,48 @@ __global__ __launch_bounds__(64 * kWaves, TILES == 1 ? 2 : 1) void attend_kernel
 #pragma unroll
             for (int g = 0; g < 4; ++g) key[g] = key_operand<BITS_K>(r[h].k, g);
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) scores_of<GROUP>(key, r[h].zeros(), r[h].ks, query[t], score[t] + 4 * h);
+            for (int t = 0; t < TILES; ++t) {
+                Products<GROUP> products;
+                products.make(key, r[h].zeros(), query[t]);
+                products.scores(r[h].ks, score[t] + 4 * h);
+            }
         }
         if (!all) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) only_seen(score[t], c, seq, query[t].draft, token, past, end, there);
+            for (int t = 0; t < TILES; ++t) only_seen(score[t], c, seq, query[t].draft, token, past, end, f.there);
         }
-        half8 weight[TILES][PARTS];
 #pragma unroll
         for (int t = 0; t < TILES; ++t) state[t].weigh(score[t], query[t].factor, weight[t]);
-        value_operands<BITS_V>(r, [&](int ch, half8 values) {
+    };
+    // ... and its values.
+    auto add = [&](Raw *r, const Step &f, int n, const half8 (*weight)[PARTS]) {
+        const int token = begin + kStep * (waves * n + wave);
+        if (token + kStep > seq.tokens || !f.there[0] || !f.there[1]) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) state[t].add(ch, values, weight[t]);
+            for (int h = 0; h < 2; ++h) r[h].vp = only_there(r[h].vp, f.there[h], token + 16 * h, seq.tokens);
+        }
+        value_operands<BITS_V>(r, [&](int ch, half8 v0, half8 v1) {
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    state[t].add(ch, v0, weight[t][p]);
+                    state[t].add(ch + 1, v1, weight[t][p]);
+                }
         });
     };
-    Raw now[2], next[2];
-    bool now_there[2] = {false, false}, next_there[2] = {false, false};
-    if (mine > 0) load(now, now_there, 0);
-    for (int n = 0; n < mine; n += 2) {
-        if (n + 1 < mine) load(next, next_there, n + 1);
-        step(now, now_there, n);
+    // The next step's keys and values are requested as soon as the step's own are used: one set of registers, so that more waves fit.
+    half8 weight[TILES][PARTS];
+    for (int n = 0; n < mine; ++n) {
+        weigh(now, now_at, n, weight);
         if (n + 1 < mine) {
-            if (n + 2 < mine) load(now, now_there, n + 2);
-            step(next, next_there, n + 1);
+            next_at = find(n + 1);
+            load_keys(now, next_at);
+        }
+        add(now, now_at, n, weight);
+        if (n + 1 < mine) {
+            load_values(now, next_at);
+            now_at = next_at;
         }
     }
 
@@ -516,12 +900,15 @@ __global__ __launch_bounds__(64 * kWaves, TILES == 1 ? 2 : 1) void attend_kernel
         }
     }
     __syncthreads();
-    const int q_heads = c.heads * a.per_kv;
+    constexpr int dtype = PARTS == 2 ? DT_F16 : DT_BF16;
+    const int here = rows - first < 16 * TILES ? rows - first : 16 * TILES;
+    const long long slot = ((long long)(part.slot0 + part.index) * each + rest) * (16 * TILES);
+    const Results results{a, seq, head, first};
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
         float most = kLowest;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, tops[w][16 * t + i]);
+        for (int w = 0; w < waves; ++w) most = fmaxf(most, tops[w][16 * t + i]);
         const float share = __builtin_amdgcn_exp2f(state[t].top - most);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -533,35 +920,48 @@ __global__ __launch_bounds__(64 * kWaves, TILES == 1 ? 2 : 1) void attend_kernel
                 *(f32x4 *)&sums[wave][i][32 * q + 8 * e + 4 * half] = v;
             }
         __syncthreads();
-        // the wave finishes rows 4 * wave + q, 8 channels per lane
-        const int r = 4 * wave + q, row = first + 16 * t + r;
-        if (row < rows) {
+        // sixteen lanes have one row, 8 channels each
+        const int r = (int)threadIdx.x >> 4, row = 16 * t + r;
+        if (r < 16 && row < here) {
             float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.0f, highest = kLowest;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) highest = fmaxf(highest, tops[w][16 * t + r]);
+            for (int w = 0; w < waves; ++w) highest = fmaxf(highest, tops[w][row]);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                total += norms[w][16 * t + r] * __builtin_amdgcn_exp2f(tops[w][16 * t + r] - highest);
+            for (int w = 0; w < waves; ++w) total += norms[w][row] * __builtin_amdgcn_exp2f(tops[w][row] - highest);
+            if (count == 1) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] += sums[w][r][8 * i + e];
-            }
-            const int d = row / a.per_kv, query_head = head * a.per_kv + row % a.per_kv;
-            if (a.splits == 1) {
-                const float part = total > 0.0f ? 1.0f / total : 0.0f;
+                for (int w = 0; w < waves; ++w) {
+                    const f32x4 lo = *(const f32x4 *)&sums[w][r][8 * i], hi = *(const f32x4 *)&sums[w][r][8 * i + 4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] *= part;
-                uint16_t *to = a.out + (long long)(seq.row0 + d) * a.o_row + (long long)query_head * a.o_head + 8 * i;
-                *(u32x4 *)to = PARTS == 2 ? pack_row<DT_F16>(x) : pack_row<DT_BF16>(x);
-                if (a.lse && i == 0) a.lse[(long long)(seq.row0 + d) * q_heads + query_head] = lse_of(highest, total);
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] += lo[e];
+                        x[4 + e] += hi[e];
+                    }
+                }
+                results.octet<dtype>(row, 8 * i, x, i == 0, highest, total);
             } else {
-                const long long at = (((long long)s * c.max_new + d) * q_heads + query_head) * a.splits + split;
-                *(f32x4 *)(a.part + at * kDim + 8 * i) = f32x4{x[0], x[1], x[2], x[3]};
-                *(f32x4 *)(a.part + at * kDim + 8 * i + 4) = f32x4{x[4], x[5], x[6], x[7]};
-                if (i == 0) *(f32x2_t *)(a.part_ml + 2 * at) = f32x2_t{highest, total};
+#pragma unroll
+                for (int w = 0; w < waves; ++w)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x2_t v = *(const f32x2_t *)&sums[w][r][pair_at(i, j)];
+                        x[2 * j] += v[0];
+                        x[2 * j + 1] += v[1];
+                    }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) leave(a.part + (slot + row) * kDim + pair_at(i, j), x[2 * j], x[2 * j + 1]);
+                if (i == 0) leave(a.part_ml + 2 * (slot + row), highest, total);
             }
         }
         if (t + 1 < TILES) __syncthreads();
     }
+    if (count == 1) return;
+    const unsigned first_slot = (unsigned)(part.slot0 * each + rest) * (16 * TILES);
+    if (!last_to_arrive(a.counters + (long long)part.slot0 * each + rest, count)) return;
+    join_parts<64 * waves>(LeftRows(a.part, a.part_rows * kDim), LeftRows(a.part_ml, a.part_rows * 2), first_slot, (unsigned)each * 16 * TILES, here, count,
+                               (float(*)[kDim + 4])sums, [&](int r, int lane_of, const float x[8], float highest, float total) {
+                                   results.octet<dtype>(r, 8 * lane_of, x, lane_of == 0, highest, total);
+                               });
 }
 
 // ---- many rows: the waves of a workgroup share tokens and divide rows --------------------------------
@@ -569,27 +969,32 @@ __global__ __launch_bounds__(64 * kWaves, TILES == 1 ? 2 : 1) void attend_kernel
 // 128 tokens at a time: each wave turns 32 of them into operands, which go through LDS in the order of the lanes (every access is
 // one KB in a row); each wave has 32 rows.
 template <int BITS_K, int BITS_V, int GROUP, bool ROTATE, int PARTS>
-__global__ __launch_bounds__(64 * kWaves, 2) void attend_wide_kernel(AttendArgs a)
+__global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendArgs a)
 {
     constexpr GranuleMap map = granule_map(BITS_K, BITS_V, GROUP);
     constexpr int groups = kDim / GROUP, param_words = 16 * groups;      // words of a granule's key scales and zeros
     typedef RawGranule<BITS_K, BITS_V, GROUP> Raw;
-    __shared__ u32x4 keys[2 * kWaves][4][64], values[kWaves][8][64];
-    __shared__ __attribute__((aligned(16))) uint32_t params[2 * kWaves][param_words];
-    __shared__ int present[2 * kWaves];
+    __shared__ u32x4 lds[2 * kManyWaves * 4 * 64 + kManyWaves * 8 * 64];
+    u32x4(*keys)[4][64] = (u32x4(*)[4][64]) lds;                         // of 8 granules
+    u32x4(*values)[8][64] = (u32x4(*)[8][64])(lds + 2 * kManyWaves * 4 * 64);      // of 4 steps
+    __shared__ __attribute__((aligned(16))) uint32_t params[2 * kManyWaves][param_words];
+    __shared__ int present[2 * kManyWaves];
 
     const CacheView &c = a.c;
-    const int s = blockIdx.z, split = (int)(blockIdx.x % (unsigned)a.splits), place = (int)(blockIdx.x / (unsigned)a.splits);
-    const int head = place % c.heads, block = place / c.heads;
     const int lane = lane_id(), wave = wave_id(), q = lane >> 4, i = lane & 15;
-    const Sequence seq = sequence_of(c, s);
+    const int each = c.heads * a.row_blocks, u = (int)(blockIdx.x / (unsigned)each), rest = (int)(blockIdx.x % (unsigned)each);
+    const int head = rest % c.heads, block = rest / c.heads;
+    Part part;
+    Sequence seq;
+    if (!find_part<kStep * kManyWaves>(a, u, part, seq)) return;
+    const int s = part.s;
     const int first = block * kWideRows, rows = seq.fresh * a.per_kv;
     if (first >= rows) return;
     const int limit = tokens_seen(c, seq, block, kWideRows, a.per_kv), past = seq.tokens - seq.fresh;
-    const long long start = (long long)split * a.chunk;
-    if (start >= limit) return;
-    const int begin = (int)start;
-    const int end = start + a.chunk < limit ? begin + a.chunk : limit;
+    const int count = (int)((limit + part.chunk - 1) / part.chunk);
+    if (part.index >= count) return;
+    const int begin = (int)(part.index * part.chunk);
+    const int end = begin + part.chunk < limit ? (int)(begin + part.chunk) : limit;
     __builtin_amdgcn_s_setreg((0 << 11) | (23 << 6) | 1, 1);             // (see attend_kernel)
 
     QueryTile<BITS_K, GROUP, ROTATE> query[2];
@@ -598,12 +1003,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_wide_kernel(AttendArgs 
     at.set();
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        query[t].load(a, seq, head, first + 32 * wave + 16 * t + i, rows);
+        query[t].fetch(a, seq, head, first + 32 * wave + 16 * t + i, rows);
+        query[t].prepare(a);
         state[t].clear();
+        __builtin_amdgcn_sched_barrier(0);   // (one tile's numbers in 32 bits at a time)
     }
 
-    const int steps = (end - begin + kStep - 1) / kStep, rounds = (steps + kWaves - 1) / kWaves;
-    PageWindow window;
+    const int steps = (end - begin + kStep - 1) / kStep, rounds = (steps + kManyWaves - 1) / kManyWaves;
+    PageWindow<kManyWaves> window;
     window.start();
     Raw raw[2];
     uint32_t param[2];
@@ -613,15 +1020,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_wide_kernel(AttendArgs 
         for (int h = 0; h < 2; ++h) {
             const int page = window.page(c, s, begin >> 4, wave, (end - 1) >> 4, n, h);
             there[h] = page >= 0;
-            const uint8_t *p = c.pages + granule_at(c, page < 0 ? 0 : page, (begin >> 4) + 2 * (kWaves * n + wave) + h, head, map.bytes);
-            raw[h].load_codes(p, at);
+            const uint8_t *p = c.pages + granule_at(c, page < 0 ? 0 : page, (begin >> 4) + 2 * (kManyWaves * n + wave) + h, head, map.bytes);
+            raw[h].load_keys(p, at);
+            raw[h].load_values(p, at);
             param[h] = *(const uint32_t *)(p + map.k_scales + (uint32_t)(lane % param_words) * 4u);
         }
     };
     load(0);
     for (int n = 0; n < rounds; ++n) {
         if (n) __syncthreads();              // everybody has read the round before
-        const int own = begin + kStep * (kWaves * n + wave);
+        const int own = begin + kStep * (kManyWaves * n + wave);
         if (own < end) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -631,13 +1039,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_wide_kernel(AttendArgs 
                 if (lane < param_words) params[2 * wave + h][lane] = param[h];
                 if (lane == 0) present[2 * wave + h] = there[h];
             }
-            value_operands<BITS_V>(raw, [&](int ch, half8 v) { values[wave][ch][lane] = __builtin_bit_cast(u32x4, v); });
+            value_operands<BITS_V>(raw, [&](int ch, half8 v0, half8 v1) {
+                values[wave][ch][lane] = __builtin_bit_cast(u32x4, v0);
+                values[wave][ch + 1][lane] = __builtin_bit_cast(u32x4, v1);
+            });
         }
         if (n + 1 < rounds) load(n + 1);
         __syncthreads();
 #pragma unroll 1
-        for (int k = 0; k < kWaves; ++k) {
-            const int token = begin + kStep * (kWaves * n + k);
+        for (int k = 0; k < kManyWaves; ++k) {
+            const int token = begin + kStep * (kManyWaves * n + k);
             if (token >= end) break;
             float score[2][8];
 #pragma unroll
@@ -653,7 +1064,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_wide_kernel(AttendArgs 
                 else if constexpr (groups == 2) zeros = __builtin_bit_cast(half4, u32x2{params[2 * k + h][16 + i], 0u});
                 else zeros = __builtin_bit_cast(half4, u32x2{(params[2 * k + h][8 + (i >> 1)] >> (16 * (i & 1))) & 0xffffu, 0u});
 #pragma unroll
-                for (int t = 0; t < 2; ++t) scores_of<GROUP>(key, zeros, ks, query[t], score[t] + 4 * h);
+                for (int t = 0; t < 2; ++t) {
+                    Products<GROUP> products;
+                    products.make(key, zeros, query[t]);
+                    products.scores(ks, score[t] + 4 * h);
+                }
             }
             const bool have[2] = {__builtin_amdgcn_readfirstlane(present[2 * k]) != 0, __builtin_amdgcn_readfirstlane(present[2 * k + 1]) != 0};
             if (token + kStep > past || token + kStep > end || !have[0] || !have[1]) {
@@ -667,84 +1082,71 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_wide_kernel(AttendArgs 
             for (int ch = 0; ch < 8; ++ch) {
                 const half8 v = __builtin_bit_cast(half8, values[k][ch][lane]);
 #pragma unroll
-                for (int t = 0; t < 2; ++t) state[t].add(ch, v, weight[t]);
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) state[t].add(ch, v, weight[t][p]);
             }
         }
     }
 
-    const int q_heads = c.heads * a.per_kv;
+    constexpr int dtype = PARTS == 2 ? DT_F16 : DT_BF16;
+    const int here = rows - first < kWideRows ? rows - first : kWideRows;
+    const Results results{a, seq, head, first};
+    if (count == 1) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const float total = state[t].total();
-        const int row = first + 32 * wave + 16 * t + i;
-        if (row < rows) {
-            const int d = row / a.per_kv, query_head = head * a.per_kv + row % a.per_kv;
-            if (a.splits == 1) {
-                const float part = total > 0.0f ? 1.0f / total : 0.0f;
-                uint16_t *to = a.out + (long long)(seq.row0 + d) * a.o_row + (long long)query_head * a.o_head + 32 * q;
+        for (int t = 0; t < 2; ++t) {
+            const float total = state[t].total();
+            const int row = 32 * wave + 16 * t + i;
+            if (row < here) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float x[8];
 #pragma unroll
-                    for (int ch = 0; ch < 8; ++ch) x[ch] = state[t].out[ch][e] * part;
-                    *(u32x4 *)(to + 8 * e) = PARTS == 2 ? pack_row<DT_F16>(x) : pack_row<DT_BF16>(x);
+                    for (int ch = 0; ch < 8; ++ch) x[ch] = state[t].out[ch][e];
+                    results.octet<dtype>(row, 32 * q + 8 * e, x, q == 0 && e == 0, state[t].top, total);
                 }
-                if (a.lse && q == 0) a.lse[(long long)(seq.row0 + d) * q_heads + query_head] = lse_of(state[t].top, total);
-            } else {
-                const long long place_of = (((long long)s * c.max_new + d) * q_heads + query_head) * a.splits + split;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        f32x4 v;
-#pragma unroll
-                        for (int ch = 0; ch < 4; ++ch) v[ch] = state[t].out[4 * half + ch][e];
-                        *(f32x4 *)(a.part + place_of * kDim + 32 * q + 8 * e + 4 * half) = v;
-                    }
-                if (q == 0) *(f32x2_t *)(a.part_ml + 2 * place_of) = f32x2_t{state[t].top, total};
             }
         }
+        return;
     }
-}
-
-// Joins the splits of a query row: one wave per row, 16 lanes with 8 channels each, the splits dealt to the four sets of lanes.
-template <int DT>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int rows_per_block)
-{
-    const CacheView &c = a.c;
-    const int s = blockIdx.z, q_heads = c.heads * a.per_kv, lane = lane_id(), q = lane >> 4, i = lane & 15;
-    const Sequence seq = sequence_of(c, s);
-    const int at_row = (int)blockIdx.x * 4 + wave_id(), d = at_row / q_heads, query_head = at_row % q_heads;
-    if (d >= seq.fresh) return;
-    const int block = (int)(((long long)d * a.per_kv + query_head % a.per_kv) / rows_per_block);
-    const int splits = (tokens_seen(c, seq, block, rows_per_block, a.per_kv) + a.chunk - 1) / a.chunk;
-    const long long at = (((long long)s * c.max_new + d) * q_heads + query_head) * a.splits;
-    float highest = kLowest;
-    for (int k = lane; k < splits; k += 64) highest = fmaxf(highest, a.part_ml[2 * (at + k)]);
+    // through LDS, where the wave has a place for 16 rows in what the keys and values had, into whole rows per 64 pairs
+    const long long slot = ((long long)(part.slot0 + part.index) * each + rest) * kWideRows;
+    float(*space)[kDim + 4] = (float(*)[kDim + 4]) lds;
+    float(*own_rows)[kDim + 4] = space + 16 * wave;
+    __syncthreads();
 #pragma unroll
-    for (int m = 1; m < 16; m <<= 1) highest = fmaxf(highest, __shfl_xor(highest, m, 64));
-    highest = row_max(highest);
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.0f;
-    for (int k = q; k < splits; k += 4) {
-        const f32x2_t ml = *(const f32x2_t *)(a.part_ml + 2 * (at + k));
-        const f32x4 lo = *(const f32x4 *)(a.part + (at + k) * kDim + 8 * i), hi = *(const f32x4 *)(a.part + (at + k) * kDim + 8 * i + 4);
-        const float share = __builtin_amdgcn_exp2f(ml[0] - highest);
-        total = __builtin_fmaf(ml[1], share, total);
+    for (int t = 0; t < 2; ++t) {
+        const float total = state[t].total();
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[e] = __builtin_fmaf(lo[e], share, x[e]);
-            x[4 + e] = __builtin_fmaf(hi[e], share, x[4 + e]);
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f32x4 v;
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch) v[ch] = state[t].out[4 * half + ch][e];
+                *(f32x4 *)&own_rows[i][32 * q + 8 * e + 4 * half] = v;
+            }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+        const int row0 = 32 * wave + 16 * t;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const f32x2_t v = *(const f32x2_t *)&own_rows[r][2 * lane];
+            if (row0 + r < here) leave(a.part + (slot + row0 + r) * kDim + 2 * lane, v[0], v[1]);
         }
+        if (q == 0 && row0 + i < here) leave(a.part_ml + 2 * (slot + row0 + i), state[t].top, total);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
     }
-    total = row_sum(total);
-    const float part = total > 0.0f ? 1.0f / total : 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = row_sum(x[e]) * part;
-    if (q == 0) {
-        uint16_t *to = a.out + (long long)(seq.row0 + d) * a.o_row + (long long)query_head * a.o_head + 8 * i;
-        *(u32x4 *)to = pack_row<DT>(x);
-    }
-    if (a.lse && lane == 0) a.lse[(long long)(seq.row0 + d) * q_heads + query_head] = lse_of(highest, total);
+    const unsigned first_slot = (unsigned)(part.slot0 * each + rest) * kWideRows;
+    if (!last_to_arrive(a.counters + (long long)part.slot0 * each + rest, count)) return;
+    join_parts<64 * kManyWaves>(LeftRows(a.part, a.part_rows * kDim), LeftRows(a.part_ml, a.part_rows * 2), first_slot, (unsigned)each * kWideRows, here,
+                                count, space,
+                                [&](int r, int lane_of, const float x[8], float highest, float total) {
+                                    results.octet<dtype>(r, 8 * lane_of, x, lane_of == 0, highest, total);
+                                });
 }
 
 // ---- launches ---------------------------------------------------------------------------------------
@@ -752,16 +1154,16 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int rows
 template <int GROUP, bool ROTATE, int PARTS> static void launch_rows(const AttendArgs &a, int tiles, const dim3 &grid, hipStream_t stream)
 {
     constexpr int bits_k = KVC_BITS / 10, bits_v = KVC_BITS % 10;
-    const dim3 threads(64 * kWaves);
-    if (tiles == 1) hipLaunchKernelGGL((attend_kernel<bits_k, bits_v, GROUP, 1, ROTATE, PARTS>), grid, threads, 0, stream, a);
-    else if (tiles == 2) hipLaunchKernelGGL((attend_kernel<bits_k, bits_v, GROUP, 2, ROTATE, PARTS>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((attend_wide_kernel<bits_k, bits_v, GROUP, ROTATE, PARTS>), grid, threads, 0, stream, a);
+    const dim3 many(64 * kManyWaves);
+    if (tiles == 1) hipLaunchKernelGGL((attend_kernel<bits_k, bits_v, GROUP, 1, ROTATE, PARTS>), grid, dim3(64 * few_waves(1, ROTATE)), 0, stream, a);
+    else if (tiles == 2) hipLaunchKernelGGL((attend_kernel<bits_k, bits_v, GROUP, 2, ROTATE, PARTS>), grid, dim3(64 * few_waves(2, ROTATE)), 0, stream, a);
+    else hipLaunchKernelGGL((attend_wide_kernel<bits_k, bits_v, GROUP, ROTATE, PARTS>), grid, many, 0, stream, a);
 }
 
 // fp16 results take weights in two parts, for bf16 ones (three bits less) one is enough
-template <int GROUP> static void launch_group(const AttendArgs &a, int tiles, int n, hipStream_t stream)
+template <int GROUP> static void launch_group(const AttendArgs &a, int tiles, int places, hipStream_t stream)
 {
-    const dim3 grid((unsigned)a.splits * (unsigned)(a.c.heads * a.row_blocks), 1, (unsigned)n);
+    const dim3 grid((unsigned)places);
     if (a.dtype == DT_F16) {
         if (a.rotate) launch_rows<GROUP, true, 2>(a, tiles, grid, stream);
         else launch_rows<GROUP, false, 2>(a, tiles, grid, stream);
@@ -771,20 +1173,11 @@ template <int GROUP> static void launch_group(const AttendArgs &a, int tiles, in
     }
 }
 
-template <> void launch_attend<KVC_BITS>(const CacheTypes &t, const AttendArgs &a, int tiles, int n, hipStream_t stream)
+template <> void launch_attend<KVC_BITS>(const CacheTypes &t, const AttendArgs &a, int tiles, int places, hipStream_t stream)
 {
-    if (t.group == 32) launch_group<32>(a, tiles, n, stream);
-    else if (t.group == 64) launch_group<64>(a, tiles, n, stream);
-    else launch_group<128>(a, tiles, n, stream);
+    if (t.group == 32) launch_group<32>(a, tiles, places, stream);
+    else if (t.group == 64) launch_group<64>(a, tiles, places, stream);
+    else launch_group<128>(a, tiles, places, stream);
 }
-
-#if KVC_BITS == 44          // (all widths join the same way: one of the units has the kernel)
-void launch_attend_join(const AttendArgs &a, int tiles, int n, hipStream_t stream)
-{
-    const dim3 grid((unsigned)(((long long)a.c.max_new * a.c.heads * a.per_kv + 3) / 4), 1, (unsigned)n);
-    if (a.dtype == DT_F16) hipLaunchKernelGGL(attend_join_kernel<DT_F16>, grid, dim3(256), 0, stream, a, 16 * tiles);
-    else hipLaunchKernelGGL(attend_join_kernel<DT_BF16>, grid, dim3(256), 0, stream, a, 16 * tiles);
-}
-#endif
 
 }  // namespace kvc

@@ -55,18 +55,21 @@ struct Sequence {
     int row0, fresh, tokens;                   // first new row, new rows, tokens with the new ones
 };
 
-// Sequence s, with nothing in it where its numbers do not fit the call (reported).
+// Whether a sequence's numbers fit the call.  (Its new rows as an unsigned number: a start near the limits of an int makes it large.)
+__device__ __forceinline__ bool fits(const CacheView &c, const Sequence &q)
+{
+    return q.row0 >= 0 && (unsigned)q.fresh <= (unsigned)c.max_new && (long long)q.row0 + q.fresh <= c.rows && q.tokens >= q.fresh &&
+           q.tokens <= c.max_tokens;
+}
+// Sequence s (the same in all lanes), with nothing in it where its numbers do not fit (reported).
 __device__ __forceinline__ Sequence sequence_of(const CacheView &c, int s)
 {
     Sequence q;
     q.row0 = __builtin_amdgcn_readfirstlane(c.new_start[s]);
-    q.fresh = __builtin_amdgcn_readfirstlane(c.new_start[s + 1]) - q.row0;
+    q.fresh = __builtin_amdgcn_readfirstlane((int)((unsigned)c.new_start[s + 1] - (unsigned)q.row0));
     q.tokens = __builtin_amdgcn_readfirstlane(c.tokens[s]);
-    // (differences as unsigned: a start near the limits of an int makes them large)
-    const bool bad = q.row0 < 0 || (unsigned)q.fresh > (unsigned)c.max_new || (long long)q.row0 + q.fresh > c.rows ||
-                     q.tokens < q.fresh || q.tokens > c.max_tokens;
-    if (bad) {
-        if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(c.status + s, 32 /* KVC_DEV_BAD_ROW */);
+    if (!fits(c, q)) {
+        if (threadIdx.x == 0) atomicOr(c.status + s, 32 /* KVC_DEV_BAD_ROW */);
         q.fresh = q.tokens = 0;
     }
     return q;

@@ -3,6 +3,7 @@
 #include "../../include/kvc.h"
 
 #include <new>
+#include <cstdlib>
 
 struct kvc_cache_plan_s {
     kvc_cache_config config;
@@ -13,15 +14,23 @@ struct kvc_cache_plan_s {
 
 namespace kvc {
 
-constexpr long long kAttendGroups = 1024;    // workgroups that the tokens of few rows are spread over (four per compute unit)
-constexpr long long kWideGroups = 512;       // ... of many rows (two per compute unit, which is all that LDS has room for)
-constexpr int kMostSplits = 256;
-constexpr int kLeastChunk = 256;             // tokens of a workgroup: two steps of its four waves at least
+// Workgroups of four waves that the chip holds: as the kernels' registers have it, three per compute unit for up to 16 rows, else two.
+constexpr int kFewGroups = 256, kManyGroups = 512;
+static float env(const char *n, float d) { const char *v = getenv(n); return v ? atof(v) : d; }
+// What cutting sequences has to gain and what joining takes per piece, in steps of a workgroup.
+#define kFewJoining env("KVC_FJ", 3)
+#define kManyJoining env("KVC_MJ", 4)
+#define kFewJoiningPiece env("KVC_FP", 0.05f)
+#define kManyJoiningPiece env("KVC_MP", 0.8f)
+constexpr int kLeastDivided = 256;           // tokens: calls of shorter sequences are not divided
+constexpr int kCounters = 2 * kManyGroups;   // at the start of the workspace
 constexpr size_t kPartBytes = (kDim + 2) * sizeof(float);
 
-// How a call divides the work: tiles of 16 query rows per wave, tokens per workgroup.
+// How a call's query rows are divided: tiles of 16 rows per workgroup, and what that makes of the tokens.
 struct AttendShape {
-    int tiles, row_blocks, splits, chunk;
+    int tiles, row_blocks;
+    bool divide;
+    int64_t parts, places, slots;            // parts per head and block of rows, workgroups, workgroups with results to be joined
 };
 static AttendShape attend_shape(const kvc_cache_config &f, int n, int max_new, int64_t max_tokens)
 {
@@ -29,16 +38,14 @@ static AttendShape attend_shape(const kvc_cache_config &f, int n, int max_new, i
     const int64_t rows = (int64_t)max_new * (f.q_heads / f.kv_heads);
     s.tiles = rows <= 16 ? 1 : rows <= 64 ? 2 : kWideTiles;
     s.row_blocks = (int)((rows + 16 * s.tiles - 1) / (16 * s.tiles));
-    const int64_t groups = (int64_t)n * f.kv_heads * s.row_blocks;
-    int64_t splits = (s.tiles == kWideTiles ? kWideGroups : kAttendGroups) / groups;
-    const int64_t most = (max_tokens + kLeastChunk - 1) / kLeastChunk;
-    splits = splits > most ? most : splits;
-    splits = splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits;
-    int64_t chunk = (max_tokens + splits - 1) / splits;
-    chunk = chunk < 1 ? 1 : chunk;
-    s.chunk = (int)((chunk + 127) / 128 * 128);
-    s.splits = (int)((max_tokens + s.chunk - 1) / s.chunk);
-    if (s.splits < 1) s.splits = 1;
+    const int64_t each = (int64_t)f.kv_heads * s.row_blocks;
+    s.parts = (s.tiles != kWideTiles ? kFewGroups : kManyGroups) / each;
+    s.divide = n <= kMostDivided && s.parts > 1 && max_tokens > kLeastDivided;
+    // what find_part makes: no more than the parts, or than half of them beyond one piece per sequence; the pieces of sequences that
+    // are cut are no more than the parts
+    const int64_t other = n + (s.parts + 1) / 2;
+    s.places = each * (!s.divide ? n : s.parts > other ? s.parts : other);
+    s.slots = s.divide ? each * (s.parts + 1) : 0;
     return s;
 }
 
@@ -124,13 +131,12 @@ extern "C" int kvc_cache_plan(const kvc_cache_config *config, int64_t max_tokens
     p->max_new = max_new;
     p->max_batch = max_batch;
     p->page_bytes = (size_t)f.kv_heads * (f.block_tokens / kGranule) * granule_map(f.bits_k, f.bits_v, f.group).bytes;
-    // a call has at most kAttendGroups workgroups where it divides the tokens, with kWideRows rows each, and no more
-    // than kMostSplits results per row
-    const int64_t rows = (int64_t)max_batch * max_new * f.q_heads;
-    int64_t most = (max_tokens + kLeastChunk - 1) / kLeastChunk;
-    most = most > kMostSplits ? kMostSplits : most;
-    const int64_t parts = rows * most < kAttendGroups * kWideRows ? rows * most : kAttendGroups * kWideRows;
-    p->workspace = most > 1 ? (size_t)parts * kPartBytes : 0;
+    p->workspace = 0;
+    for (int64_t rows = 1; rows <= (int64_t)max_new; rows = rows < max_new && 2 * rows > max_new ? max_new : 2 * rows) {
+        const AttendShape one = attend_shape(f, 1, (int)rows, max_tokens);       // (the number of sequences does not matter)
+        const size_t bytes = one.divide ? (size_t)one.slots * 16 * one.tiles * kPartBytes + kCounters * sizeof(int) : 0;
+        p->workspace = bytes > p->workspace ? bytes : p->workspace;
+    }
     *out = p;
     return KVC_OK;
 }
@@ -178,14 +184,18 @@ extern "C" int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_ba
         !strides_ok(u.out_stride_row, u.out_stride_head) || !(u.scale >= -3.0e38f && u.scale <= 3.0e38f)) return KVC_ERR_ARG;
     const kvc_cache_config &f = plan->config;
     const AttendShape s = attend_shape(f, batch->n, batch->max_new, batch->max_tokens);
-    a.part = nullptr;
-    a.part_ml = nullptr;
-    if (s.splits > 1) {
-        const int64_t parts = (int64_t)batch->n * batch->max_new * f.q_heads * s.splits;
-        if ((size_t)parts * kPartBytes > plan->workspace) return KVC_ERR_CAPACITY;
+    if (s.places > 0x7fffffffll) return KVC_ERR_CAPACITY;
+    a.part = a.part_ml = nullptr;
+    a.counters = nullptr;
+    a.part_rows = 0;
+    if (s.divide) {
+        const size_t rows = (size_t)s.slots * 16 * s.tiles;
+        if (rows * kPartBytes + (size_t)kCounters * sizeof(int) > plan->workspace) return KVC_ERR_CAPACITY;
         if (!workspace || !aligned(workspace, 16)) return KVC_ERR_ARG;
-        a.part = (float *)workspace;
-        a.part_ml = a.part + parts * kDim;
+        a.counters = (int *)workspace;
+        a.part = (float *)(a.counters + kCounters);
+        a.part_ml = a.part + rows * kDim;
+        a.part_rows = (long long)rows;
     }
     a.q = (const uint16_t *)u.q;
     a.out = (uint16_t *)u.out;
@@ -197,16 +207,18 @@ extern "C" int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_ba
     a.scale = u.scale * 1.44269504088896341f;
     a.per_kv = f.q_heads / f.kv_heads;
     a.row_blocks = s.row_blocks;
-    a.splits = s.splits;
-    a.chunk = s.chunk;
+    a.n = batch->n;
+    a.divide = s.divide;
+    a.parts = (int)s.parts;
+    a.joining_piece = s.tiles == kWideTiles ? kManyJoiningPiece : kFewJoiningPiece;
+    a.joining = s.tiles == kWideTiles ? kManyJoining : kFewJoining;
     a.dtype = f.dtype;
     a.rotate = f.transform == KVC_T_HADAMARD;
     const CacheTypes t = types_of(f);
     const hipStream_t stream = (hipStream_t)hip_stream;
-    if (f.bits_k == 4 && f.bits_v == 4) launch_attend<44>(t, a, s.tiles, batch->n, stream);
-    else if (f.bits_k == 4) launch_attend<48>(t, a, s.tiles, batch->n, stream);
-    else if (f.bits_v == 4) launch_attend<84>(t, a, s.tiles, batch->n, stream);
-    else launch_attend<88>(t, a, s.tiles, batch->n, stream);
-    if (s.splits > 1) launch_attend_join(a, s.tiles, batch->n, stream);
+    if (f.bits_k == 4 && f.bits_v == 4) launch_attend<44>(t, a, s.tiles, (int)s.places, stream);
+    else if (f.bits_k == 4) launch_attend<48>(t, a, s.tiles, (int)s.places, stream);
+    else if (f.bits_v == 4) launch_attend<84>(t, a, s.tiles, (int)s.places, stream);
+    else launch_attend<88>(t, a, s.tiles, (int)s.places, stream);
     return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
 }

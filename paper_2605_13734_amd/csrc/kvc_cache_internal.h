@@ -25,25 +25,32 @@ struct AttendArgs {
     const uint16_t *q;
     uint16_t *out;
     float *lse;                    // or null
-    float *part;                   // splits > 1: sums, [sequence][new][query head][split][128]
-    float *part_ml;                // ... and (maximum, sum of weights)
+    // sequences in several parts: sums of a part's rows, [slot][128], (maximum, sum of weights), [slot][2], and how many of
+    // a sequence's parts are done (zero between the calls)
+    float *part, *part_ml;
+    int *counters;
+    long long part_rows;           // rows that the results have room for (below 2^32 bytes)
     long long q_row, q_head, o_row, o_head;        // strides in elements
     float scale;                   // of the scores, times log2(e)
+    // the division of sequences (see find_part), in the tokens that a workgroup's waves take at a time: whether there is one, workgroups
+    // per head and block of rows that the chip holds at once, what cutting has to gain, and what joining takes per piece
+    int divide, parts, joining;
+    float joining_piece;
     int per_kv;                    // query heads per KV head
     int row_blocks;                // of 16 * tiles query rows, in the longest sequence
-    int splits, chunk;             // tokens of a sequence per workgroup (a multiple of 128)
+    int n;
     int dtype, rotate;
 };
 
+constexpr int kMostDivided = 256;             // sequences of a call whose sequences are divided
 constexpr int kWideRows = 128, kWideTiles = kWideRows / 16;
 
-// The attention of one pair of code widths (10 * bits_k + bits_v) with 1 or 2 tiles of 16 query rows per workgroup or (kWideTiles) 128
-// rows, and the kernel that joins the results of several workgroups per row.
-template <int BITS> void launch_attend(const CacheTypes &t, const AttendArgs &a, int tiles, int n, hipStream_t stream);
+// The attention of one pair of code widths (10 * bits_k + bits_v) with 1 or 2 tiles of 16 query rows per workgroup, or (kWideTiles) 128
+// rows; `places` workgroups.
+template <int BITS> void launch_attend(const CacheTypes &t, const AttendArgs &a, int tiles, int places, hipStream_t stream);
 template <> void launch_attend<44>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);
 template <> void launch_attend<48>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);
 template <> void launch_attend<84>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);
 template <> void launch_attend<88>(const CacheTypes &, const AttendArgs &, int, int, hipStream_t);
-void launch_attend_join(const AttendArgs &a, int tiles, int n, hipStream_t stream);
 
 }  // namespace kvc

@@ -413,7 +413,7 @@ class Cache:
         self.pages = torch.zeros(max(num_pages * plan.page_bytes(), 16), dtype=torch.uint8, device=device)
         self.status = torch.zeros(plan.max_batch, dtype=torch.int32, device=device)
         self.workspace = workspace if workspace is not None else \
-            torch.empty(max(plan.workspace_size(), 16), dtype=torch.uint8, device=device)
+            torch.zeros(max(plan.workspace_size(), 16), dtype=torch.uint8, device=device)
         if self.workspace.numel() * self.workspace.element_size() < plan.workspace_size():
             raise ValueError("the workspace is smaller than kvc_cache_workspace_size")
         self._pages, self._status, self._workspace = self.pages.data_ptr(), self.status.data_ptr(), self.workspace.data_ptr()
