@@ -398,7 +398,7 @@ class CacheBatch:
         stride = block_table.stride(0) if n > 1 else block_table.shape[1]
         self.struct = CacheSequences(n, max_new, max_tokens, new_start.data_ptr(), tokens.data_ptr(), block_table.data_ptr(), stride,
                                      mask.data_ptr() if mask is not None else None, words, num_pages)
-        self.mask_rows = None if mask is None else mask.shape[0]
+        self.mask_rows, self.num_pages = None if mask is None else mask.shape[0], num_pages
         self._ref = C.byref(self.struct)
 
 
@@ -417,29 +417,35 @@ class Cache:
         if self.workspace.numel() * self.workspace.element_size() < plan.workspace_size():
             raise ValueError("the workspace is smaller than kvc_cache_workspace_size")
         self._pages, self._status, self._workspace = self.pages.data_ptr(), self.status.data_ptr(), self.workspace.data_ptr()
+        f, lib = plan.config, load()
+        self._kv_heads, self._q_heads, self._dim, self._plan = f.kv_heads, f.q_heads, f.head_dim, plan._h
+        self._store, self._load, self._attend = lib.kvc_cache_store, lib.kvc_cache_load, lib.kvc_cache_attend
 
-    def _check(self, batch, tensors, heads):
-        if batch.struct.num_pages > self.num_pages:
-            raise ValueError("the batch names more pages than the pool has")
-        for x in tensors:
-            if x.dtype is not self.dtype or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.plan.config.head_dim or x.stride(2) != 1:
-                raise ValueError("rows are [rows, %d, %d] tensors of the plan's type with contiguous channels" % (heads, self.plan.config.head_dim))
+    def _layout(self, x, heads):
+        """(rows, strides) of a tensor of rows; the checks are the few that a call of microseconds can afford."""
+        rows, h, d = x.shape
+        strides = x.stride()
+        if x.dtype is not self.dtype or h != heads or d != self._dim or strides[2] != 1:
+            raise ValueError("rows are [rows, %d, %d] tensors of the plan's type with contiguous channels" % (heads, self._dim))
+        return rows, strides
 
     def _rows(self, batch, k, v):
-        self._check(batch, (k, v), self.plan.config.kv_heads)
-        if k.shape != v.shape or k.stride() != v.stride():
+        if batch.num_pages > self.num_pages:
+            raise ValueError("the batch names more pages than the pool has")
+        rows, strides = self._layout(k, self._kv_heads)
+        if self._layout(v, self._kv_heads) != (rows, strides):
             raise ValueError("k and v have one shape and one layout")
-        return CacheRows(k.data_ptr(), v.data_ptr(), k.shape[0], k.stride(0), k.stride(1))
+        return CacheRows(k.data_ptr(), v.data_ptr(), rows, strides[0], strides[1])
 
     def store(self, batch, k, v, stream=None):
         """kvc_cache_store: k, v [new rows, kv_heads, 128]."""
-        rc = _lib.kvc_cache_store(self.plan._h, batch._ref, C.byref(self._rows(batch, k, v)), self._pages, self._status, stream)
+        rc = self._store(self._plan, batch._ref, self._rows(batch, k, v), self._pages, self._status, stream)
         if rc != OK:
             raise KvcError("kvc_cache_store", rc)
 
     def load(self, batch, k, v, stream=None):
         """kvc_cache_load into k, v [new rows, kv_heads, 128]."""
-        rc = _lib.kvc_cache_load(self.plan._h, batch._ref, C.byref(self._rows(batch, k, v)), self._pages, self._status, stream)
+        rc = self._load(self._plan, batch._ref, self._rows(batch, k, v), self._pages, self._status, stream)
         if rc != OK:
             raise KvcError("kvc_cache_load", rc)
 
@@ -449,24 +455,27 @@ class Cache:
         if keep_start.dtype != torch.int32 or keep.dtype != torch.int32 or keep_start.numel() < batch.struct.n + 1 or \
                 not keep_start.is_contiguous() or not keep.is_contiguous():
             raise ValueError("keep_start [n + 1] and keep are contiguous int32 tensors")
-        self._check(batch, (), 0)
-        rc = _lib.kvc_cache_keep(self.plan._h, batch._ref, keep_start.data_ptr(), keep.data_ptr(), keep.numel(), self._pages, self._status,
+        if batch.num_pages > self.num_pages:
+            raise ValueError("the batch names more pages than the pool has")
+        rc = _lib.kvc_cache_keep(self._plan, batch._ref, keep_start.data_ptr(), keep.data_ptr(), keep.numel(), self._pages, self._status,
                                  stream)
         if rc != OK:
             raise KvcError("kvc_cache_keep", rc)
 
     def attend(self, batch, q, out, scale, lse=None, stream=None):
         """kvc_cache_attend: q, out [new rows, q_heads, 128]; lse: optional contiguous float32 [new rows, q_heads]."""
-        self._check(batch, (q, out), self.plan.config.q_heads)
-        rows = q.shape[0]
-        if out.shape[0] != rows or (batch.mask_rows is not None and batch.mask_rows < rows):
+        if batch.num_pages > self.num_pages:
+            raise ValueError("the batch names more pages than the pool has")
+        rows, q_strides = self._layout(q, self._q_heads)
+        out_rows, out_strides = self._layout(out, self._q_heads)
+        if out_rows != rows or (batch.mask_rows is not None and batch.mask_rows < rows):
             raise ValueError("out and mask have a row for every row of q")
         if lse is not None:
             import torch
             if lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
                 raise ValueError("lse is a contiguous float32 tensor [new rows, q_heads]")
-        u = CacheQueries(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, rows, q.stride(0), q.stride(1),
-                         out.stride(0), out.stride(1), scale)
-        rc = _lib.kvc_cache_attend(self.plan._h, batch._ref, C.byref(u), self._pages, self._status, self._workspace, stream)
+        u = CacheQueries(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, rows, q_strides[0], q_strides[1],
+                         out_strides[0], out_strides[1], scale)
+        rc = self._attend(self._plan, batch._ref, u, self._pages, self._status, self._workspace, stream)
         if rc != OK:
             raise KvcError("kvc_cache_attend", rc)
