@@ -49,12 +49,6 @@ __global__ __launch_bounds__(256) void cache_store_kernel(CacheView c, const uin
     const int past = seq.tokens - seq.fresh;
     const long long j = (past >> 4) + (long long)(blockIdx.x / quads);
     if (seq.fresh == 0 || head >= c.heads || j * kGranule >= seq.tokens) return;
-    const int page = __builtin_amdgcn_readfirstlane(page_of(c, s, j));
-    if (page < 0) {
-        if (lane_id() == 0) atomicOr(c.status + s, KVC_DEV_BAD_BLOCK);
-        return;
-    }
-    uint8_t *to = c.pages + granule_at(c, page, j, head, map.bytes);
     // (the rotation's lanes hold their octets in an order of their own; V then takes the same order)
     const int col = lane_octet(ROTATE), rsub = lane_id() >> 4;
     u32x4 rk[4], rv[4];
@@ -69,6 +63,12 @@ __global__ __launch_bounds__(256) void cache_store_kernel(CacheView c, const uin
             rv[p] = *(const u32x4 *)(v + at);
         }
     }
+    const int page = __builtin_amdgcn_readfirstlane(page_of(c, s, j));        // (behind the rows' requests)
+    if (page < 0) {
+        if (lane_id() == 0) atomicOr(c.status + s, KVC_DEV_BAD_BLOCK);
+        return;
+    }
+    uint8_t *to = c.pages + granule_at(c, page, j, head, map.bytes);
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const int t = 4 * p + rsub;
