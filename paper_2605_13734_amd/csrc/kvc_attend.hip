@@ -1040,6 +1040,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
         }
     };
     load(0);
+    const bool busy = first + 32 * wave < rows;              // (a wave without rows still makes operands)
     for (int n = 0; n < rounds; ++n) {
         if (n) __syncthreads();              // everybody has read the round before
         const int own = begin + kStep * (kManyWaves * n + wave);
@@ -1062,7 +1063,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
 #pragma unroll 1
         for (int k = 0; k < kManyWaves; ++k) {
             const int token = begin + kStep * (kManyWaves * n + k);
-            if (token >= end) break;
+            if (token >= end || !busy) break;
             float score[2][8];
             half8 keyy[2][4];
 #pragma unroll
