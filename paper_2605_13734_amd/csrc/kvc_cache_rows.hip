@@ -61,6 +61,7 @@ __device__ __forceinline__ void store_granule(const u32x4 rk[4], const u32x4 rv[
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const int t = 4 * p + rsub;
+        if (4 * p + 4 <= first || 4 * p >= end) continue;    // (the same in all lanes: a single row is a quarter of the work)
         float x[8];
         uint32_t mk, mv;
         values_of<DT, LIMIT>(rk[p], x);
@@ -116,14 +117,15 @@ __global__ __launch_bounds__(256) void cache_store_kernel(CacheView c, const uin
         return;
     }
     uint8_t *to = c.pages + granule_at(c, page, j, head, map.bytes);
+    const long long token = j * kGranule;
+    const int first = token < past ? (int)(past - token) : 0, end = seq.tokens - token < kGranule ? (int)(seq.tokens - token) : kGranule;
     bool limit = false;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
+        if (4 * p + 4 <= first || 4 * p >= end) continue;
         if (ROTATE) rk[p] = hadamard_row<DT, true>(rk[p], false);
         limit |= out_of_order<DT>(rk[p]) || out_of_order<DT>(rv[p]);
     }
-    const long long token = j * kGranule;
-    const int first = token < past ? (int)(past - token) : 0, end = seq.tokens - token < kGranule ? (int)(seq.tokens - token) : kGranule;
     // A whole granule goes through LDS and out in pieces of 16 bytes per lane, past the caches as its rows came; part of one, and rows
     // with values to be limited, row by row, the parameters two bytes at a time.  (32k tokens of 8 heads, 176 MB: 41.6 us, through the
     // caches 44.8; rotated 48.1 and 51.8.)
@@ -181,10 +183,13 @@ __global__ __launch_bounds__(256) void cache_load_kernel(CacheView c, uint16_t *
     }
     const uint8_t *from = c.pages + granule_at(c, page, j, head, map.bytes);
     const int col = lane_id() & 15, rsub = lane_id() >> 4, g = col / (GROUP / 8);
+    const long long start = j * kGranule;
+    const int first = start < past ? (int)(past - start) : 0, end = seq.tokens - start < kGranule ? (int)(seq.tokens - start) : kGranule;
     u32x2 ck[4], cv[4];
     uint32_t sk[4], zk[4], sv[4], zv[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
+        if (4 * p + 4 <= first || 4 * p >= end) continue;
         const int t = 4 * p + rsub;              // (rows that nobody wrote are read as well, and not used)
         if (BITS_K == 4) ck[p] = u32x2{*(const uint32_t *)(from + k_code_at<4>(t, col)), 0};
         else ck[p] = *(const u32x2 *)(from + k_code_at<8>(t, col));
@@ -197,6 +202,7 @@ __global__ __launch_bounds__(256) void cache_load_kernel(CacheView c, uint16_t *
     }
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
+        if (4 * p + 4 <= first || 4 * p >= end) continue;
         const long long token = j * kGranule + 4 * p + rsub;
         float x[8], y[8];
         restore_octet<BITS_K>(ck[p], f16_bits_to_f32(sk[p]), f16_bits_to_f32(zk[p]), x);
