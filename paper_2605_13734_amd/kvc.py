@@ -12,6 +12,7 @@ LIB_PATH = os.path.join(_HERE, "libkvc.so")
 
 F16, BF16 = 1, 2
 CODEC_NONE, CODEC_HUFF8 = 0, 1
+T_NONE, T_HADAMARD, T_DELTA = 0, 1, 2
 OK = 0
 DEV_BAD_BLOCK, DEV_BAD_HEADER, DEV_BAD_CHUNK, DEV_BAD_TABLE, DEV_SCAN_TIMEOUT, DEV_BAD_ROW = 1, 2, 4, 8, 16, 32
 
