@@ -356,6 +356,8 @@ int kvc_policy_lookup(const kvc_policy_segment *table, int32_t count, double ban
  * channels differ much in size, K rows are stored as H x / 8 (rounded to the type), and attention rotates the
  * queries: (H q / 16) . (H k / 8) = q . k.  V is not rotated.
  *
+ * Arrays of 32-bit words (lengths, tables, indices, status) have to be 4-byte aligned, masks 8-byte, all else 16-byte.
+ *
  *   dtype         KVC_F16 or KVC_BF16: type of rows, queries and results
  *   bits_k/bits_v 4 or 8
  *   transform     KVC_T_NONE or KVC_T_HADAMARD
@@ -438,10 +440,14 @@ typedef struct {
  *                     Codes move as they are.  Indices that do not ascend or are out of range:
  *                     KVC_DEV_BAD_ROW, and the sequence stays as it is
  *   kvc_cache_attend  out = softmax(scale * q k^T) v over the tokens that a new token sees; a row that sees none
- *                     gives zeros and lse = -infinity.  Scores, maxima and sums are held in 32 bits; weights and
- *                     values enter the second product as fp16 numbers (one rounding each).
- *                     workspace: DEVICE, kvc_cache_workspace_size bytes, may be NULL when that is 0; calls on
- *                     one workspace must be in stream order
+ *                     gives zeros and lse = -infinity (so does one whose scores are all below -2^59).  Scores, maxima and sums are held in 32 bits; weights and
+ *                     values enter the second product as fp16 numbers (values with one rounding; weights with one where
+ *                     results are bf16, as two numbers where they are fp16).
+ *                     workspace: DEVICE, kvc_cache_workspace_size bytes, all zero before the first call that
+ *                     uses it (calls leave what has to be zero as they find it), may be NULL when that is 0;
+ *                     several plans may share one of the largest size; calls on one workspace must be in
+ *                     stream order.  Up to 256 sequences of a call are cut into pieces where that fills the
+ *                     chip; equal inputs give equal bits
  */
 int kvc_cache_store(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_rows *rows, void *pages,
                     int32_t *dev_status, void *hip_stream);

@@ -129,12 +129,11 @@ extern "C" int kvc_cache_plan(const kvc_cache_config *config, int64_t max_tokens
     p->max_new = max_new;
     p->max_batch = max_batch;
     p->page_bytes = (size_t)f.kv_heads * (f.block_tokens / kGranule) * granule_map(f.bits_k, f.bits_v, f.group).bytes;
-    p->workspace = 0;
-    for (int64_t rows = 1; rows <= (int64_t)max_new; rows = rows < max_new && 2 * rows > max_new ? max_new : 2 * rows) {
-        const AttendShape one = attend_shape(f, 1, (int)rows, max_tokens);       // (the number of sequences does not matter)
-        const size_t bytes = one.divide ? (size_t)one.slots * 16 * one.tiles * kPartBytes + kCounters * sizeof(int) : 0;
-        p->workspace = bytes > p->workspace ? bytes : p->workspace;
-    }
+    // the counters, and as many results as a call of up to max_new rows can have (attend_shape: each * (parts + 1) with each * parts of
+    // the groups at most and two parts or more)
+    const int tiles = attend_shape(f, 1, max_new, max_tokens).tiles;
+    const size_t slots = (size_t)(tiles == kWideTiles ? kManyGroups : kFewGroups) * 3 / 2;
+    p->workspace = max_tokens > kLeastDivided ? slots * 16 * tiles * kPartBytes + kCounters * sizeof(int) : 0;
     *out = p;
     return KVC_OK;
 }

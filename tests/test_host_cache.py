@@ -63,6 +63,21 @@ def test_workspace(lib):
     assert 0 < small.workspace_size() <= long.workspace_size() <= wide.workspace_size() < 64 << 20
 
 
+@pytest.mark.parametrize("kv_heads,per_kv,max_new", [(8, 8, 64), (3, 5, 40), (1, 1, 300), (40, 2, 9), (128, 1, 1), (7, 16, 100)])
+def test_workspace_is_enough_for_every_call_of_a_plan(lib, kv_heads, per_kv, max_new):
+    """Calls with fewer sequences or new tokens than the plan has are accepted (they end at the device that is not there)."""
+    if torch.cuda.is_available():
+        pytest.skip("would launch")
+    p = plan(kv_heads=kv_heads, q_heads=kv_heads * per_kv, max_new=max_new, max_tokens=1 << 20, max_batch=300)
+    for n in (1, 2, 31, 256, 257, 300):
+        for new in sorted(set(range(1, max_new + 1, 7)) | {1, 2, 3, 4, 5, 8, 16, 17, max_new}):
+            if new > max_new:
+                continue
+            a = Args(p)
+            a.batch.n, a.batch.max_new, a.batch.max_tokens, a.batch.table_stride = n, new, 1 << 20, 1 << 16
+            assert a.calls(lib)["attend"]() == -6, (n, new)
+
+
 class Args:
     """Arguments of a call that is well formed but for what a test changes (addresses are never followed)."""
 
