@@ -13,7 +13,8 @@ struct kvc_cache_plan_s {
 
 namespace kvc {
 
-// Workgroups of four waves that the chip holds: as the kernels' registers have it, three per compute unit for up to 16 rows, else two.
+// Workgroups that the chip holds, as the kernels' registers have it: one of 8 or 12 waves per compute unit for up to 64 rows, two of 4 waves
+// for more (64 drafts over 8k tokens, 8 heads, divided among 512 / 768 / 1024: 305 us, and more with either of the others).
 constexpr int kFewGroups = 256, kManyGroups = 512;
 // What cutting sequences has to gain, in steps of a workgroup's waves, and what joining takes per piece (128 rows: 64 KB, read by one
 // workgroup).  One sequence, steps that cutting has to gain 0 / 3 / 5 for few rows: 1k tokens 12.1 / 11.3 / 11.4 us; per piece 0 / 0.2 /
@@ -23,6 +24,8 @@ constexpr float kFewJoiningPiece = 0.05f, kManyJoiningPiece = 0.3f;
 constexpr int kLeastDivided = 256;           // tokens: calls of shorter sequences are not divided
 constexpr int kCounters = 2 * kManyGroups;   // at the start of the workspace
 constexpr size_t kPartBytes = (kDim + 2) * sizeof(float);
+constexpr int64_t kMostThreads = 0xffffffffll;       // of a launch, per dimension
+constexpr int kMostAttending = 768;                  // threads of an attention's workgroup at most
 
 // How a call's query rows are divided: tiles of 16 rows per workgroup, and what that makes of the tokens.
 struct AttendShape {
@@ -81,7 +84,7 @@ static int check_call(const kvc_cache_plan_t *plan, const kvc_cache_batch *b, vo
     c->heads = f.kv_heads;
     c->page_shift = __builtin_ctz((unsigned)f.block_tokens);
     c->num_pages = b->num_pages;
-    c->max_new = b->max_new;
+    c->max_new = b->max_new < b->max_tokens ? b->max_new : (int)b->max_tokens;       // (new rows are tokens)
     c->max_tokens = (int)b->max_tokens;
     return KVC_OK;
 }
@@ -98,6 +101,7 @@ static int rows_call(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch,
     const int rc = check_call(plan, batch, pages, status, r->rows, INT32_MAX, &c);
     if (rc != KVC_OK || nothing(batch)) return rc;
     if ((r->rows && (!r->k || !r->v)) || !aligned(r->k, 16) || !aligned(r->v, 16) || !strides_ok(r->stride_row, r->stride_head)) return KVC_ERR_ARG;
+    if (row_places(c) > kMostThreads / 256) return KVC_ERR_CAPACITY;
     launch_cache_rows(types_of(plan->config), c, store, (uint16_t *)r->k, (uint16_t *)r->v, r->stride_row, r->stride_head, batch->n,
                       (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
@@ -180,8 +184,8 @@ extern "C" int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_ba
     if ((u.rows && (!u.q || !u.out)) || !aligned(u.q, 16) || !aligned(u.out, 16) || !aligned(u.lse, 4) || !strides_ok(u.q_stride_row, u.q_stride_head) ||
         !strides_ok(u.out_stride_row, u.out_stride_head) || !(u.scale >= -3.0e38f && u.scale <= 3.0e38f)) return KVC_ERR_ARG;
     const kvc_cache_config &f = plan->config;
-    const AttendShape s = attend_shape(f, batch->n, batch->max_new, batch->max_tokens);
-    if (s.places > 0x7fffffffll) return KVC_ERR_CAPACITY;
+    const AttendShape s = attend_shape(f, batch->n, a.c.max_new, batch->max_tokens);
+    if (s.places > kMostThreads / kMostAttending) return KVC_ERR_CAPACITY;
     a.part = a.part_ml = nullptr;
     a.counters = nullptr;
     a.part_rows = 0;

@@ -14,6 +14,8 @@ struct CacheTypes {
     bool rotate;                   // K rows and queries
 };
 
+// Workgroups of 256 threads per sequence of a call that stores or loads rows.
+long long row_places(const CacheView &c);
 void launch_cache_rows(const CacheTypes &t, const CacheView &c, bool store, uint16_t *k, uint16_t *v, long long stride_row,
                        long long stride_head, int n, hipStream_t stream);
 void launch_cache_keep(const CacheTypes &t, const CacheView &c, const int *keep_start, const int *keep, int max_keep, int n,

@@ -312,12 +312,13 @@ template <typename F> static void with_store_types(const CacheTypes &t, F f)
     else by_group(IntConst<8>(), IntConst<8>());
 }
 
+// granules that max_new consecutive tokens can lie in, by four heads
+long long row_places(const CacheView &c) { return ((long long)c.max_new + 2 * kGranule - 2) / kGranule * ((c.heads + 3) / 4); }
+
 void launch_cache_rows(const CacheTypes &t, const CacheView &c, bool store, uint16_t *k, uint16_t *v, long long stride_row,
                        long long stride_head, int n, hipStream_t stream)
 {
-    // granules that max_new consecutive tokens can lie in
-    const unsigned granules = (unsigned)(((long long)c.max_new + 2 * kGranule - 2) / kGranule);
-    const dim3 grid(granules * (unsigned)((c.heads + 3) / 4), 1, (unsigned)n);
+    const dim3 grid((unsigned)row_places(c), 1, (unsigned)n);
     with_store_types(t, [&](auto bk, auto bv, auto g) {
         constexpr int BK = decltype(bk)::value, BV = decltype(bv)::value, G = decltype(g)::value;
         auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, c, k, v, stride_row, stride_head); };

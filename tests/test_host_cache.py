@@ -222,3 +222,16 @@ def test_oracle_attention():
     out, lse, _, _ = cache_ref.attention(np.ones((2, 1, 128)), k, v, seen, 0.01, 1)
     assert np.allclose(out[0], 2.0) and np.all(out[1] == 0) and lse[1, 0] == -np.inf
     assert np.isclose(lse[0, 0], 1.28 + np.log(2))
+
+
+def test_calls_too_large_for_a_launch(lib):
+    """What no launch can hold is refused before anything starts: 2^31 new rows of 64 heads, 5000 blocks of rows for 40 heads and more
+    sequences than are divided."""
+    p = plan(kv_heads=64, q_heads=64, max_tokens=0x7fffff00, max_new=1)
+    a = Args(p)
+    a.batch.max_new, a.batch.max_tokens, a.batch.table_stride = 0x7fffffff, 0x7fffff00, 1 << 27
+    assert a.calls(lib)["store"]() == -3 and a.calls(lib)["load"]() == -3
+    p = plan(kv_heads=40, q_heads=40, max_tokens=640000, max_new=640000, max_batch=300)
+    a = Args(p)
+    a.batch.n, a.batch.max_new, a.batch.max_tokens, a.batch.table_stride = 300, 640000, 640000, 40000
+    assert a.calls(lib)["attend"]() == -3
