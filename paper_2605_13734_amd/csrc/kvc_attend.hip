@@ -2,9 +2,10 @@
 //
 // Compiled once per pair of code widths (KVC_BITS = 10 * bits_k + bits_v).
 //
-// A workgroup has 16 * TILES query rows of one KV head (a row: one new token and one of the query heads that share the KV head)
-// and a run of the sequence's tokens, of which its four waves take 32 at a time in turn; the waves' results are joined in
-// LDS.  The tokens of long sequences are spread over several workgroups, whose results the last of them joins.
+// A row is one new token and one of the query heads that share a KV head; a workgroup has a block of rows of one KV head and a run of
+// the sequence's tokens.  Up to 64 rows per sequence and head go to attend_kernel (HBM's rate bounds it), more to
+// attend_wide_kernel (arithmetic does).  Where a call has fewer blocks than the chip has room for, the tokens of long sequences
+// are spread over several workgroups, whose results the last of them joins.
 //
 // Scores: the matrix product runs over the codes themselves, with 16 tokens as rows and 16 query rows as columns.  A code, masked
 // out of its word together with a second one, is a half-precision subnormal, code * 2^-24 (or 2^-20), which the matrix
@@ -755,7 +756,16 @@ struct Results {
 
 // ---- few rows: the waves of a workgroup share rows and divide tokens --------------------------------
 
-// As many waves as the registers leave room for in a compute unit: three per SIMD, or two.
+// One block of 16 * TILES rows (16 up to 16 rows, 32 up to 64), whose queries are in the registers of every wave; the waves take 32 tokens
+// at a time in turn and their results meet in LDS at the end.  So a code is read once per block, straight into the registers of the one
+// wave that uses it: with few rows a token brings 160 to 300 bytes per head and 512 operations per row, and HBM is the bound.
+// One token over 128k (8 KV heads, 4 query heads each, 4 bits, groups of 32, fp16; 168 MB): 42.9 us, 3.9 TB/s; what more tokens cost,
+// 5.5 TB/s (a large copy: 4.8, a large fill: 6.8), and some 12 us do not depend on them: dividing (2), pages and queries (3), the waves' join (2),
+// the workgroups' join (4 to 6).  Vector instructions take 49 % of the time there, matrix instructions 17 %.  4 sequences of 16k to
+// 32k tokens, 8-bit K, groups of 128 (92 MB): 26.0 us.  One token over 1k: 11.2 us, latencies one after the other.
+// Two tiles per block, 16 queries of 4 heads over 1k tokens: 15 us.
+// As many waves as the registers leave room for in a compute unit, three per SIMD or two: what is in flight is what hides the memory's
+// latency, one step's codes per wave.  (The same with four waves and three workgroups per unit was slower: more pieces to join.)
 constexpr int few_waves(int tiles, bool rotate) { return tiles == 1 && !rotate ? 12 : 8; }
 
 template <int BITS_K, int BITS_V, int GROUP, int TILES, bool ROTATE, int PARTS>
@@ -979,8 +989,18 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
 
 // ---- many rows: the waves of a workgroup share tokens and divide rows --------------------------------
 
-// 128 tokens at a time: each wave turns 32 of them into operands, which go through LDS in the order of the lanes (every access is
-// one KB in a row); each wave has 32 rows.
+// 128 rows, 32 for each of four waves.  128 tokens at a time: each wave turns 32 of them into operands, which go through LDS in the
+// order of the lanes (every access is one KB in a row: no bank conflicts), so masking codes and restoring values, some 200 vector
+// instructions per 32 tokens, is done once for 128 rows and not once per wave.
+// Arithmetic bounds it: per wave and 32 tokens 36 matrix instructions of 16 x 16 x 32 (16 for the scores, 4 of a smaller kind for the
+// zeros, 16 for the values; a second part of rotated queries adds 16, of the weights for fp16 results 20) and some 270 of vector arithmetic
+// (with groups of 32: 80 for scales and zeros, 32 exponentials and their arguments, 16 maxima, 16 sums, its share of the operands).
+// The two kinds hardly run side by side: 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 717 us, 761 TFLOP/s
+// (a large library product: 1135), vector instructions 62 % of the time and matrix instructions 38 %; trees of 64 drafts over 8 x 8k
+// (rotated 4 bits, groups of 32, fp16; 137 GFLOP, 275 with the second parts): 302 us, 55 % and 47 %.
+// Two workgroups per compute unit, as 256 registers per lane allow (with rotated queries and groups of 32, 64 to 152 bytes per lane do not
+// fit: addresses and numbers of the next load, once per 128 tokens, nothing between the products); the scores of the next 32 tokens ahead of this one's weights
+// gained nothing, nor did two steps of the loop at once.
 template <int BITS_K, int BITS_V, int GROUP, bool ROTATE, int PARTS>
 __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendArgs a)
 {
@@ -1065,15 +1085,14 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
             const int token = begin + kStep * (kManyWaves * n + k);
             if (token >= end || !busy) break;
             float score[2][8];
-            half8 keyy[2][4];
+            half8 key[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) keyy[h][g] = __builtin_bit_cast(half8, keys[2 * k + h][g][lane]);
+                for (int g = 0; g < 4; ++g) key[h][g] = __builtin_bit_cast(half8, keys[2 * k + h][g][lane]);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                half8 *key = keyy[h];
                 u32x2 ks[groups];
 #pragma unroll
                 for (int g = 0; g < groups; ++g) ks[g] = *(const u32x2 *)&params[2 * k + h][(q * groups + g) * 2];
@@ -1084,7 +1103,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     Products<GROUP> products;
-                    products.make(key, zeros, query[t]);
+                    products.make(key[h], zeros, query[t]);
                     products.scores(ks, score[t] + 4 * h);
                 }
             }

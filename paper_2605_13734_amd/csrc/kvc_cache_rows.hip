@@ -1,8 +1,9 @@
 // Rows of the quantised cache: quantised as they are written, read back, moved.
 //
-// All three are bound by HBM.  A wave has one granule (16 tokens) of one head, 16 lanes per row and 8 channels per lane,
-// four rows at a time; the four waves of a workgroup take neighbouring heads, whose rows lie next to each other in the caller's
-// tensors and whose granules lie one after the other in a page.
+// All three are bound by HBM where there are many rows, and by the latency of a few dependent loads (lengths, page, rows) where there are
+// few.  A wave has one granule (16 tokens) of one head, 16 lanes per row and 8 channels per lane, four rows at a time: a group's
+// minimum and maximum are found inside a row of lanes, a rotation too, and all of a granule's rows are requested at once.  The
+// four waves of a workgroup take neighbouring heads, whose rows lie next to each other in the caller's tensors.
 #include "kvc_cache.h"
 #include "kvc_cache_internal.h"
 #include "../../include/kvc.h"
@@ -85,6 +86,9 @@ __device__ __forceinline__ void store_granule(const u32x4 rk[4], const u32x4 rv[
     }
 }
 
+// zero = fp16(min), scale = fp16((max - min) / (2^b - 1)), code = clamp(rint((x - zero) / scale)) per row and group.
+// 32k tokens of 8 heads, 4 bits, groups of 32 (134 MB read, 42 written): 41.6 us, 4.2 TB/s (a large copy: 4.8), K rotated 48.
+// One token of each of 32 sequences: 3.9 us.
 template <int BITS_K, int BITS_V, int GROUP, int DT, bool ROTATE>
 __global__ __launch_bounds__(256) void cache_store_kernel(CacheView c, const uint16_t *k, const uint16_t *v, long long stride_row,
                                                           long long stride_head)
@@ -165,6 +169,9 @@ template <int DT> __device__ __forceinline__ u32x4 rounded_octet(const float x[8
     return out;
 }
 
+// code * scale + zero in 32 bits, a rotated row turned back, rounded once.  32k tokens of 8 heads, 4 bits, groups of 32, K rotated (42 MB
+// read, 134 written): 38 to 43 us, 4.1 to 4.6 TB/s; four sequences of 16k to 32k tokens of 4 heads, 8-bit K, groups of 64 (302 MB): 61.7 us,
+// 4.9 TB/s (a large copy: 4.8).  1k tokens of 8 heads: 4.7 us.
 template <int BITS_K, int BITS_V, int GROUP, int DT, bool ROTATE>
 __global__ __launch_bounds__(256) void cache_load_kernel(CacheView c, uint16_t *k, uint16_t *v, long long stride_row, long long stride_head)
 {
@@ -218,7 +225,8 @@ __global__ __launch_bounds__(256) void cache_load_kernel(CacheView c, uint16_t *
 
 // Row keep[i] of a sequence's new rows moves to place i.  The indices ascend, so place i is never behind its source: of every 16
 // rows all are read before the first is written, and what later rows come from is behind everything written so far.  A wave has
-// one head; nothing is decoded.
+// one head; nothing is decoded.  A few rows per sequence, so latency bounds it (indices, pages, rows, one after the other): 32 sequences
+// of 17 to 32 drafts 4.9 us, one of 15 3.7 us.
 template <int BITS_K, int BITS_V, int GROUP>
 __global__ __launch_bounds__(256) void cache_keep_kernel(CacheView c, const int *keep_start, const int *keep, int max_keep)
 {
