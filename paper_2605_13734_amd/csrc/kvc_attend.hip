@@ -761,7 +761,7 @@ struct Results {
 // wave that uses it: with few rows a token brings 160 to 300 bytes per head and 512 operations per row, and HBM is the bound.
 // One token over 128k (8 KV heads, 4 query heads each, 4 bits, groups of 32, fp16; 168 MB): 42.9 us, 3.9 TB/s; what more tokens cost,
 // 5.5 TB/s (a large copy: 4.8, a large fill: 6.8), and some 12 us do not depend on them: dividing (2), pages and queries (3), the waves' join (2),
-// the workgroups' join (4 to 6).  Vector instructions take 49 % of the time there, matrix instructions 17 %.  4 sequences of 16k to
+// the workgroups' join (4 to 6).  Vector instructions take 46 % of the time there, matrix instructions 18 %.  4 sequences of 16k to
 // 32k tokens, 8-bit K, groups of 128 (92 MB): 26.0 us.  One token over 1k: 11.2 us, latencies one after the other.
 // Two tiles per block, 16 queries of 4 heads over 1k tokens: 15 us.
 // As many waves as the registers leave room for in a compute unit, three per SIMD or two: what is in flight is what hides the memory's
@@ -992,12 +992,14 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
 // 128 rows, 32 for each of four waves.  128 tokens at a time: each wave turns 32 of them into operands, which go through LDS in the
 // order of the lanes (every access is one KB in a row: no bank conflicts), so masking codes and restoring values, some 200 vector
 // instructions per 32 tokens, is done once for 128 rows and not once per wave.
-// Arithmetic bounds it: per wave and 32 tokens 36 matrix instructions of 16 x 16 x 32 (16 for the scores, 4 of a smaller kind for the
-// zeros, 16 for the values; a second part of rotated queries adds 16, of the weights for fp16 results 20) and some 270 of vector arithmetic
-// (with groups of 32: 80 for scales and zeros, 32 exponentials and their arguments, 16 maxima, 16 sums, its share of the operands).
-// The two kinds hardly run side by side: 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 717 us, 761 TFLOP/s
-// (a large library product: 1135), vector instructions 62 % of the time and matrix instructions 38 %; trees of 64 drafts over 8 x 8k
-// (rotated 4 bits, groups of 32, fp16; 137 GFLOP, 275 with the second parts): 302 us, 55 % and 47 %.
+// Arithmetic bounds it: per wave and 32 tokens 36 matrix instructions (16 of 16 x 16 x 32 for the scores, 4 smaller ones for the zeros, 16
+// for the values; a second part of rotated queries adds 16, of the weights for fp16 results 20) and some 180 (bf16, groups of 64) to
+// 250 (fp16, groups of 32) of vector arithmetic: scales and zeros 48 or 80, 16 exponentials and their arguments, the sums, the
+// second parts, a quarter of the operands' making.  The two kinds share the registers' ports: for two waves per SIMD 16 products of
+// one kind and 64 multiply-adds take 235 and 188 ns alone and 432 together; only exponentials run beside products for nothing.
+// 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 692 us, 788 TFLOP/s (a large library product:
+// 1135), vector instructions 55 % of the time and matrix instructions 40 %; trees of 64 drafts over 8 x 8k (rotated 4 bits, groups of 32,
+// fp16; 137 GFLOP, 275 with the second parts): 297 us, 45 % and 49 %.
 // Two workgroups per compute unit, as 256 registers per lane allow (with rotated queries and groups of 32, 64 to 152 bytes per lane do not
 // fit: addresses and numbers of the next load, once per 128 tokens, nothing between the products); the scores of the next 32 tokens ahead of this one's weights
 // gained nothing, nor did two steps of the loop at once.
