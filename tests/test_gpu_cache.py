@@ -154,6 +154,29 @@ def test_attention_of_trees(new, past, bits_v, transform, per_kv):
     attend(w, masks)
 
 
+@pytest.mark.parametrize("bits_k,bits_v,group", list(itertools.product((4, 8), (4, 8), (32, 64, 128))))
+@pytest.mark.parametrize("bf16,transform", [(False, 0), (True, 0), (False, 1), (True, 1)])
+@pytest.mark.parametrize("new", [7, 37])
+def test_attention_of_every_kind(bits_k, bits_v, group, bf16, transform, new):
+    """Blocks of 32 rows and of 128, each pair of widths, group, type and transform: a tree behind nothing and behind a context that is
+    cut, and one token."""
+    w = World([0, 900, 45], [new, new, 1], seed=new + group, kv_heads=1, per_kv=4, bf16=bf16, bits_k=bits_k, bits_v=bits_v, group=group,
+              transform=transform, block_tokens=32)
+    masks, _ = tree_masks(w.g, w.new)
+    w.fill()
+    attend(w, masks)
+
+
+@pytest.mark.parametrize("n,new,per_kv", [(256, 1, 3), (257, 1, 3), (256, 70, 2), (260, 66, 2)])
+def test_attention_of_the_most_sequences_that_are_cut(n, new, per_kv):
+    """256 sequences, the longest of them cut, and more, which are whole."""
+    past = [(37 * i) % 50 + (700 if i % 64 == 5 else 0) for i in range(n)]
+    w = World(past, [1 + (i * new) // n for i in range(n)], seed=n + new, kv_heads=1, per_kv=per_kv)
+    w.fill()
+    a = attend(w)
+    assert torch.equal(a, attend(w))
+
+
 def test_rows_that_see_nothing():
     """Empty mask rows: zeros and -infinity where there is no context, the context alone where there is one; and rows that see later
     drafts, or not themselves."""
