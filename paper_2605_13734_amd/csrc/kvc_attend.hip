@@ -995,14 +995,14 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
 // Arithmetic bounds it: per wave and 32 tokens 36 matrix instructions (16 of 16 x 16 x 32 for the scores, 4 smaller ones for the zeros, 16
 // for the values; a second part of rotated queries adds 16, of the weights for fp16 results 20) and some 180 (bf16, groups of 64) to
 // 250 (fp16, groups of 32) of vector arithmetic: scales and zeros 48 or 80, 16 exponentials and their arguments, the sums, the
-// second parts, a quarter of the operands' making.  The two kinds share the registers' ports: for two waves per SIMD 16 products of
+// second parts, a quarter of the operands' making.  The two kinds hardly run side by side: for two waves per SIMD 16 products of
 // one kind and 64 multiply-adds take 235 and 188 ns alone and 432 together; only exponentials run beside products for nothing.
 // 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 692 us, 788 TFLOP/s (a large library product:
 // 1135), vector instructions 55 % of the time and matrix instructions 40 %; trees of 64 drafts over 8 x 8k (rotated 4 bits, groups of 32,
 // fp16; 137 GFLOP, 275 with the second parts): 297 us, 45 % and 49 %.
-// Two workgroups per compute unit, as 256 registers per lane allow (with rotated queries and groups of 32, 64 to 152 bytes per lane do not
-// fit: addresses and numbers of the next load, once per 128 tokens, nothing between the products); the scores of the next 32 tokens ahead of this one's weights
-// gained nothing, nor did two steps of the loop at once.
+// Two workgroups per compute unit, as 256 registers per lane allow (with rotated queries and groups of 32 some 64 to 152 bytes per lane do
+// not fit: addresses and numbers of the next load, once per 128 tokens, nothing between the products).  The scores of the next 32
+// tokens ahead of this one's weights gained nothing, nor did two steps of the loop at once.
 template <int BITS_K, int BITS_V, int GROUP, bool ROTATE, int PARTS>
 __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendArgs a)
 {
