@@ -399,7 +399,9 @@ class CacheBatch:
         stride = block_table.stride(0) if n > 1 else block_table.shape[1]
         self.struct = CacheSequences(n, max_new, max_tokens, new_start.data_ptr(), tokens.data_ptr(), block_table.data_ptr(), stride,
                                      mask.data_ptr() if mask is not None else None, words, num_pages)
-        self.mask_rows, self.num_pages = None if mask is None else mask.shape[0], num_pages
+        self.mask_rows, self.num_pages, self.device = None if mask is None else mask.shape[0], num_pages, tokens.get_device()
+        if any(t is not None and t.get_device() != self.device for t in self.keep_alive):
+            raise ValueError("the tensors of a batch are on one device")
         self._ref = C.byref(self.struct)
 
 
@@ -415,8 +417,10 @@ class Cache:
         self.status = torch.zeros(plan.max_batch, dtype=torch.int32, device=device)
         self.workspace = workspace if workspace is not None else \
             torch.zeros(max(plan.workspace_size(), 16), dtype=torch.uint8, device=device)
-        if self.workspace.numel() * self.workspace.element_size() < plan.workspace_size():
-            raise ValueError("the workspace is smaller than kvc_cache_workspace_size")
+        self._device = self.pages.get_device()
+        if self.workspace.numel() * self.workspace.element_size() < plan.workspace_size() or not self.workspace.is_contiguous() or \
+                self.workspace.get_device() != self._device:
+            raise ValueError("the workspace has to be contiguous, on the cache's device and of kvc_cache_workspace_size bytes")
         self._pages, self._status, self._workspace = self.pages.data_ptr(), self.status.data_ptr(), self.workspace.data_ptr()
         f, lib = plan.config, load()
         self._kv_heads, self._q_heads, self._dim, self._plan = f.kv_heads, f.q_heads, f.head_dim, plan._h
@@ -426,13 +430,16 @@ class Cache:
         """(rows, strides) of a tensor of rows; the checks are the few that a call of microseconds can afford."""
         rows, h, d = x.shape
         strides = x.stride()
-        if x.dtype is not self.dtype or h != heads or d != self._dim or strides[2] != 1:
-            raise ValueError("rows are [rows, %d, %d] tensors of the plan's type with contiguous channels" % (heads, self._dim))
+        if x.dtype is not self.dtype or h != heads or d != self._dim or strides[2] != 1 or x.get_device() != self._device:
+            raise ValueError("rows are [rows, %d, %d] tensors of the plan's type and the cache's device with contiguous channels" %
+                             (heads, self._dim))
+        if rows == 1 or h == 1:              # the stride of one thing may be anything
+            strides = (strides[0] if rows > 1 else 0, strides[1] if h > 1 else 0, 1)
         return rows, strides
 
     def _rows(self, batch, k, v):
-        if batch.num_pages > self.num_pages:
-            raise ValueError("the batch names more pages than the pool has")
+        if batch.num_pages > self.num_pages or batch.device != self._device:
+            raise ValueError("the batch names more pages than the pool has, or is on another device")
         rows, strides = self._layout(k, self._kv_heads)
         if self._layout(v, self._kv_heads) != (rows, strides):
             raise ValueError("k and v have one shape and one layout")
@@ -454,10 +461,11 @@ class Cache:
         """kvc_cache_keep: keep_start [n + 1] and keep, int32 device tensors."""
         import torch
         if keep_start.dtype != torch.int32 or keep.dtype != torch.int32 or keep_start.numel() < batch.struct.n + 1 or \
-                not keep_start.is_contiguous() or not keep.is_contiguous():
-            raise ValueError("keep_start [n + 1] and keep are contiguous int32 tensors")
-        if batch.num_pages > self.num_pages:
-            raise ValueError("the batch names more pages than the pool has")
+                not keep_start.is_contiguous() or not keep.is_contiguous() or keep_start.get_device() != self._device or \
+                keep.get_device() != self._device:
+            raise ValueError("keep_start [n + 1] and keep are contiguous int32 tensors on the cache's device")
+        if batch.num_pages > self.num_pages or batch.device != self._device:
+            raise ValueError("the batch names more pages than the pool has, or is on another device")
         rc = _lib.kvc_cache_keep(self._plan, batch._ref, keep_start.data_ptr(), keep.data_ptr(), keep.numel(), self._pages, self._status,
                                  stream)
         if rc != OK:
@@ -465,15 +473,15 @@ class Cache:
 
     def attend(self, batch, q, out, scale, lse=None, stream=None):
         """kvc_cache_attend: q, out [new rows, q_heads, 128]; lse: optional contiguous float32 [new rows, q_heads]."""
-        if batch.num_pages > self.num_pages:
-            raise ValueError("the batch names more pages than the pool has")
+        if batch.num_pages > self.num_pages or batch.device != self._device:
+            raise ValueError("the batch names more pages than the pool has, or is on another device")
         rows, q_strides = self._layout(q, self._q_heads)
         out_rows, out_strides = self._layout(out, self._q_heads)
         if out_rows != rows or (batch.mask_rows is not None and batch.mask_rows < rows):
             raise ValueError("out and mask have a row for every row of q")
         if lse is not None:
             import torch
-            if lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
+            if lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.get_device() != self._device:
                 raise ValueError("lse is a contiguous float32 tensor [new rows, q_heads]")
         u = CacheQueries(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, rows, q_strides[0], q_strides[1],
                          out_strides[0], out_strides[1], scale)

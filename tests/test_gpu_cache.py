@@ -414,3 +414,43 @@ def test_offsets_beyond_32_bits():
     w.fill()
     check_rows(w)
     attend(w)
+
+
+def test_one_row_or_head_with_any_stride():
+    """A dimension of one thing has a stride that is never used: one row cut out of odd rows, one head with an odd stride."""
+    w = World([40], [1], seed=31, per_kv=4)
+    w.fill()
+    want = attend(w)
+    wide = torch.zeros(2, 8 * DIM + 3, dtype=w.dtype, device="cuda")
+    q = wide.as_strided((1, 8, DIM), (8 * DIM + 3, DIM, 1))
+    q.copy_(w.q)
+    out = torch.zeros_like(wide).as_strided((1, 8, DIM), (8 * DIM + 3, DIM, 1))
+    assert q.stride(0) % 8 and out.stride(0) % 8
+    w.cache.attend(w.batch(), q, out, SCALE, None, stream())
+    assert torch.equal(out, want) and not w.cache.status.any()
+    w = World([3], [9], seed=32, kv_heads=1)
+    w.fill()
+    k = torch.zeros(9, 1, DIM, dtype=w.dtype, device="cuda").as_strided((9, 1, DIM), (DIM, 5, 1))
+    v = torch.zeros_like(k).as_strided((9, 1, DIM), (DIM, 1, 1))
+    w.cache.load(w.batch(), k, v, stream())
+    hk, hv = w.held(0)
+    assert np.array_equal(k.double().cpu().numpy(), hk.read_back(False)[3:]) and np.array_equal(v.double().cpu().numpy(), hv.read_back(False)[3:])
+
+
+def test_tensors_of_the_host_are_refused():
+    """Addresses that the GPU cannot follow never reach a kernel."""
+    w = World([40], [2], seed=33)
+    w.fill()
+    out, host = torch.empty_like(w.q, device="cuda"), torch.empty_like(w.q)
+    rows = torch.zeros(2, 2, DIM, dtype=w.dtype, device="cuda")
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32)                        # noqa: E731
+    for call in (lambda: w.cache.attend(w.batch(), host, out, SCALE), lambda: w.cache.attend(w.batch(), out, host, SCALE),
+                 lambda: w.cache.attend(w.batch(), out, out.clone(), SCALE, torch.zeros(out.shape[:2])),
+                 lambda: w.cache.store(w.batch(), rows, rows.cpu()), lambda: w.cache.load(w.batch(), rows.cpu(), rows),
+                 lambda: w.cache.keep(w.batch(), i32(0, 1), i32(0).cuda()), lambda: w.cache.keep(w.batch(), i32(0, 1).cuda(), i32(0)),
+                 lambda: w.cache.store(kvc.CacheBatch(i32(0, 2), i32(42), torch.zeros(1, 3, dtype=torch.int32), 2, 42, 3), rows, rows),
+                 lambda: kvc.CacheBatch(i32(0, 2), i32(42).cuda(), torch.zeros(1, 3, dtype=torch.int32), 2, 42, 3),
+                 lambda: kvc.Cache(w.plan, 3, "cuda", workspace=torch.zeros(1 << 26, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            call()
+    assert not w.cache.status.any()
