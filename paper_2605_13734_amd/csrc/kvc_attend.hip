@@ -674,10 +674,12 @@ __device__ __forceinline__ void join_parts(const LeftRows &part, const LeftRows 
         float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, highest = kLowest, total = 0.0f;
         f32x2_t s[8];
         f32x4 lo[8], hi[8];
-        auto request = [&](int k0) {
+        // (part turn + n * per_row for n = n0 ... n0 + 7; turns behind the last part take that one, and no share of it)
+        auto request = [&](int n0) {
 #pragma unroll
             for (int n = 0; n < 8; ++n) {
-                const int k = k0 + n * per_row < count ? k0 + n * per_row : k0;
+                if ((n0 + n) * per_row >= count) break;
+                const int k = turn + (n0 + n) * per_row < count ? turn + (n0 + n) * per_row : count - 1;
                 const unsigned at = first + (unsigned)k * stride + (unsigned)r;
                 s[n] = ml.two(2 * at);
                 lo[n] = part.four(at * kDim + 8 * i);
@@ -685,18 +687,19 @@ __device__ __forceinline__ void join_parts(const LeftRows &part, const LeftRows 
             }
         };
         if (mine) {
-            request(turn);
+            request(0);
             // sixteen lanes look at sixteen parts at a time
 #pragma unroll 4
             for (int k = i; k < count; k += 16) highest = fmaxf(highest, ml.two(2 * (first + (unsigned)k * stride + (unsigned)r))[0]);
         }
         highest = max_of_row(highest);
         if (mine) {
-            for (int k0 = turn; k0 < count; k0 += 8 * per_row) {
-                if (k0 > turn) request(k0);
+            for (int n0 = 0; n0 * per_row < count; n0 += 8) {
+                if (n0) request(n0);
 #pragma unroll
                 for (int n = 0; n < 8; ++n) {
-                    const float share = k0 + n * per_row < count ? __builtin_amdgcn_exp2f(s[n][0] - highest) : 0.0f;
+                    if ((n0 + n) * per_row >= count) break;
+                    const float share = turn + (n0 + n) * per_row < count ? __builtin_amdgcn_exp2f(s[n][0] - highest) : 0.0f;
                     total = __builtin_fmaf(s[n][1], share, total);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -721,6 +724,51 @@ __device__ __forceinline__ void join_parts(const LeftRows &part, const LeftRows 
             }
         }
         if (mine && turn == 0) done(r, i, x, highest, total);
+    }
+}
+
+// The same where there are as many rows as sets of sixteen lanes or more, and 16 / M parts or fewer: a set has M rows at a time, all of
+// whose parts are requested together.
+template <int THREADS, int M, typename F>
+__device__ __forceinline__ void join_few_parts(const LeftRows &part, const LeftRows &ml, unsigned first, unsigned stride, int rows, int count, F done)
+{
+    constexpr int sets = THREADS / 16, most = 16 / M;
+    const int set = (int)threadIdx.x >> 4, i = (int)threadIdx.x & 15;
+    for (int base = 0; base < rows; base += sets * M) {
+        f32x2_t s[M][most];
+        f32x4 lo[M][most], hi[M][most];
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int k = 0; k < most; ++k) {
+                if (k >= count) break;
+                const int row = base + m * sets + set < rows ? base + m * sets + set : rows - 1;
+                const unsigned at = first + (unsigned)k * stride + (unsigned)row;
+                s[m][k] = ml.two(2 * at);
+                lo[m][k] = part.four(at * kDim + 8 * i);
+                hi[m][k] = part.four(at * kDim + 8 * i + 4);
+            }
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, highest = kLowest, total = 0.0f;
+#pragma unroll
+            for (int k = 0; k < most; ++k) {
+                if (k >= count) break;
+                highest = fmaxf(highest, s[m][k][0]);
+            }
+#pragma unroll
+            for (int k = 0; k < most; ++k) {
+                if (k >= count) break;
+                const float share = __builtin_amdgcn_exp2f(s[m][k][0] - highest);
+                total = __builtin_fmaf(s[m][k][1], share, total);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = __builtin_fmaf(lo[m][k][e], share, x[e]);
+                    x[4 + e] = __builtin_fmaf(hi[m][k][e], share, x[4 + e]);
+                }
+            }
+            if (base + m * sets + set < rows) done(base + m * sets + set, i, x, highest, total);
+        }
     }
 }
 
@@ -1189,11 +1237,15 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
     }
     const unsigned first_slot = (unsigned)(part.slot0 * each + rest) * kWideRows;
     if (!last_to_arrive(a.counters + (long long)part.slot0 * each + rest, count)) return;
-    join_parts<64 * kManyWaves>(LeftRows(a.part, a.part_rows * kDim), LeftRows(a.part_ml, a.part_rows * 2), first_slot, (unsigned)each * kWideRows, here,
-                                count, space,
-                                [&](int r, int lane_of, const float x[8], float highest, float total) {
-                                    results.octet<dtype>(r, 8 * lane_of, x, lane_of == 0, highest, total);
-                                });
+    const LeftRows sums_left(a.part, a.part_rows * kDim), ml_left(a.part_ml, a.part_rows * 2);
+    const unsigned stride = (unsigned)each * kWideRows;
+    const auto done = [&](int r, int lane_of, const float x[8], float highest, float total) {
+        results.octet<dtype>(r, 8 * lane_of, x, lane_of == 0, highest, total);
+    };
+    if (count <= 2) join_few_parts<64 * kManyWaves, 8>(sums_left, ml_left, first_slot, stride, here, count, done);
+    else if (count <= 4) join_few_parts<64 * kManyWaves, 4>(sums_left, ml_left, first_slot, stride, here, count, done);
+    else if (count <= 8) join_few_parts<64 * kManyWaves, 2>(sums_left, ml_left, first_slot, stride, here, count, done);
+    else join_parts<64 * kManyWaves>(sums_left, ml_left, first_slot, stride, here, count, space, done);
 }
 
 // ---- launches ---------------------------------------------------------------------------------------
