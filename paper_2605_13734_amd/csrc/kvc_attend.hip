@@ -513,6 +513,8 @@ __device__ __forceinline__ float sum_of_row(float x)
 // Part u of the call, in all waves.  The lengths are on the device, so the division is made here, from the lengths of up to 256 sequences
 // in units of STEP tokens.  The measure is a piece length: the shortest with which the pieces of all sequences fit the chip at
 // once (per head and block of rows); or, with more sequences than that, twice an even share, so that only the longest are cut.
+// Where two workgroups share a compute unit each is slower for it (by a.alone), so that up to that much longer pieces with which
+// every workgroup has a unit of its own are better.
 // A sequence is then cut into equal pieces of that length at most; nothing is cut where that would save less than joining costs
 // (a.joining units).  With more than 256 sequences a piece is a whole one.  False: there is no part u, or nothing in it.
 template <int STEP> __device__ __forceinline__ bool find_part(const AttendArgs &a, int u, Part &p, Sequence &seq)
@@ -549,33 +551,42 @@ template <int STEP> __device__ __forceinline__ bool find_part(const AttendArgs &
     if (busy == 0) return false;
     longest = __builtin_amdgcn_readfirstlane((int)row_max(max_of_row((float)longest)));
     // in units; joining takes time by the number of pieces, so that piece + a.joining_piece * longest / piece is to be small
-    int piece = __builtin_amdgcn_readfirstlane((int)__builtin_amdgcn_sqrtf(a.joining_piece * (float)longest)) + 1;
-    if (a.n == 1) {
-        const int even = (longest + a.parts - 1) / a.parts;
-        piece = even > piece ? even : piece;
-    } else {
-        sum = row_sum(sum_of_row(sum));
-        if (busy > a.parts) {
-            const int even = __builtin_amdgcn_readfirstlane((int)(2.0f * sum / (float)a.parts)) + 1;
-            piece = even > piece ? even : piece;
-        } else if (longest > piece) {
-            // between an even share and one that leaves room for a shorter last piece of every sequence, by bisection
-            const int even = __builtin_amdgcn_readfirstlane((int)(sum * 0.9999f / (float)a.parts));
-            piece = even > piece ? even : piece;
-            int most = longest;
-            if (busy < a.parts) {
-                const int roomy = __builtin_amdgcn_readfirstlane((int)(sum * 1.0001f / (float)(a.parts - busy))) + 1;
-                most = roomy < most ? roomy : most;
-            }
-            while (piece < most) {
-                const int middle = (piece + most) >> 1;
-                float made = 0.0f;           // (below 2^24: exact)
+    const int least = __builtin_amdgcn_readfirstlane((int)__builtin_amdgcn_sqrtf(a.joining_piece * (float)longest)) + 1;
+    if (a.n > 1) sum = row_sum(sum_of_row(sum));
+    // the shortest piece from there on with which there are no more than `parts`
+    auto shortest = [&](int parts) {
+        if (longest <= least) return least;
+        if (a.n == 1) {
+            const int even = (longest + parts - 1) / parts;
+            return even > least ? even : least;
+        }
+        // between an even share and one that leaves room for a shorter last piece of every sequence, by bisection
+        int piece = __builtin_amdgcn_readfirstlane((int)(sum * 0.9999f / (float)parts)), most = longest;
+        piece = piece > least ? piece : least;
+        if (busy < parts) {
+            const int roomy = __builtin_amdgcn_readfirstlane((int)(sum * 1.0001f / (float)(parts - busy))) + 1;
+            most = roomy < most ? roomy : most;
+        }
+        while (piece < most) {
+            const int middle = (piece + most) >> 1;
+            float made = 0.0f;               // (below 2^24: exact)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (64 * k < a.n) made += (float)(((unsigned)units[k] + (unsigned)middle - 1u) / (unsigned)middle);
-                if (row_sum(sum_of_row(made)) <= (float)a.parts) most = middle;
-                else piece = middle + 1;
-            }
+            for (int k = 0; k < 4; ++k)
+                if (64 * k < a.n) made += (float)(((unsigned)units[k] + (unsigned)middle - 1u) / (unsigned)middle);
+            if (row_sum(sum_of_row(made)) <= (float)parts) most = middle;
+            else piece = middle + 1;
+        }
+        return piece;
+    };
+    int piece;
+    if (busy > a.parts) {
+        piece = __builtin_amdgcn_readfirstlane((int)(2.0f * sum / (float)a.parts)) + 1;
+        piece = piece > least ? piece : least;
+    } else {
+        piece = shortest(a.parts);
+        if (a.alone > 0.0f && 2 * busy <= a.parts) {
+            const int longer = shortest(a.parts / 2);
+            if ((float)longer <= a.alone * (float)piece) piece = longer;
         }
     }
     if (piece + a.joining > longest) piece = longest;

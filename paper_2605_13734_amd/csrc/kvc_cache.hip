@@ -21,6 +21,7 @@ constexpr int kFewGroups = 256, kManyGroups = 512;
 // 0.5 / 2 for many: 64 drafts over 4k tokens 63 / 44.5 / 44.6 / 56 us.
 constexpr int kFewJoining = 3, kManyJoining = 4;
 constexpr float kFewJoiningPiece = 0.05f, kManyJoiningPiece = 0.3f;
+constexpr float kManyAlone = 1.5f;           // 64 drafts over 16k tokens: 18 pieces of 7 steps, 288 workgroups, 85 us, 16 of 8 steps 71
 constexpr int kLeastDivided = 256;           // tokens: calls of shorter sequences are not divided
 constexpr int kCounters = 2 * kManyGroups;   // at the start of the workspace
 constexpr size_t kPartBytes = (kDim + 2) * sizeof(float);
@@ -212,6 +213,7 @@ extern "C" int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_ba
     a.divide = s.divide;
     a.parts = (int)s.parts;
     a.joining_piece = s.tiles == kWideTiles ? kManyJoiningPiece : kFewJoiningPiece;
+    a.alone = s.tiles == kWideTiles ? kManyAlone : 0.0f;
     a.joining = s.tiles == kWideTiles ? kManyJoining : kFewJoining;
     a.dtype = f.dtype;
     a.rotate = f.transform == KVC_T_HADAMARD;

@@ -35,9 +35,10 @@ struct AttendArgs {
     long long q_row, q_head, o_row, o_head;        // strides in elements
     float scale;                   // of the scores, times log2(e)
     // the division of sequences (see find_part), in the tokens that a workgroup's waves take at a time: whether there is one, workgroups
-    // per head and block of rows that the chip holds at once, what cutting has to gain, and what joining takes per piece
+    // per head and block of rows that the chip holds at once, what cutting has to gain, what joining takes per piece, and how much
+    // longer a workgroup takes beside another one (0: there is none)
     int divide, parts, joining;
-    float joining_piece;
+    float joining_piece, alone;
     int per_kv;                    // query heads per KV head
     int row_blocks;                // of 16 * tiles query rows, in the longest sequence
     int n;
