@@ -17,9 +17,10 @@ namespace kvc {
 // for more (64 drafts over 8k tokens, 8 heads, divided among 512 / 768 / 1024: 305 us, and more with either of the others).
 constexpr int kFewGroups = 256, kManyGroups = 512;
 // What cutting sequences has to gain, in steps of a workgroup's waves, and what joining takes per piece (128 rows: 64 KB, read by one
-// workgroup).  One sequence, steps that cutting has to gain 0 / 3 / 5 for few rows: 1k tokens 12.1 / 11.3 / 11.4 us; per piece 0 / 0.2 /
-// 0.5 / 2 for many: 64 drafts over 4k tokens 63 / 44.5 / 44.6 / 56 us.
-constexpr int kFewJoining = 3, kManyJoining = 4;
+// workgroup; with few rows per 16 of them).  One sequence, one token, steps that cutting has to gain 1 / 2 / 3: 1k tokens 11.0 / 11.0 / 11.3 us;
+// 8 drafts over 4k, per piece and 16 rows 0.025 / 0.05: 18.4 / 16.5 us, one token over 16k 0.02 / 0.05 / 0.1: 16.7 / 16.7 / 17.6; 64 drafts, per
+// piece 0.1 / 0.3 / 0.5 / 1: over 4k 44.3 / 39.3 / 42.4 / 45.7, over 64k - / 161 / 162 / 189 us.
+constexpr int kFewJoining = 2, kManyJoining = 4;
 constexpr float kFewJoiningPiece = 0.05f, kManyJoiningPiece = 0.3f;
 constexpr float kManyAlone = 1.5f;           // 64 drafts over 16k tokens: 18 pieces of 7 steps, 288 workgroups, 85 us, 16 of 8 steps 71
 constexpr int kLeastDivided = 256;           // tokens: calls of shorter sequences are not divided
@@ -212,7 +213,7 @@ extern "C" int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_ba
     a.n = batch->n;
     a.divide = s.divide;
     a.parts = (int)s.parts;
-    a.joining_piece = s.tiles == kWideTiles ? kManyJoiningPiece : kFewJoiningPiece;
+    a.joining_piece = s.tiles == kWideTiles ? kManyJoiningPiece : kFewJoiningPiece * s.tiles;
     a.alone = s.tiles == kWideTiles ? kManyAlone : 0.0f;
     a.joining = s.tiles == kWideTiles ? kManyJoining : kFewJoining;
     a.dtype = f.dtype;

@@ -177,6 +177,18 @@ def test_attention_of_the_most_sequences_that_are_cut(n, new, per_kv):
     assert torch.equal(a, attend(w))
 
 
+@pytest.mark.parametrize("past,new,per_kv", [([16500], 64, 4), ([9000, 70], 64, 4), ([16500], 8, 4), ([9000, 70, 3], 16, 2)])
+def test_attention_of_drafts_over_long_contexts(past, new, per_kv):
+    """Many pieces to be joined, of 32 rows and of 128, with a short sequence beside them."""
+    w = World(past, [new] * len(past), seed=new + len(past), kv_heads=8, per_kv=per_kv, group=64, bf16=len(past) > 1)
+    masks, _ = tree_masks(w.g, w.new)
+    w.fill()
+    a = attend(w, masks)
+    out = torch.empty_like(a)
+    w.cache.attend(w.batch(w.mask_tensor(masks)), w.q.cuda(), out, SCALE, None, stream())
+    assert torch.equal(a, out)
+
+
 def test_rows_that_see_nothing():
     """Empty mask rows: zeros and -infinity where there is no context, the context alone where there is one; and rows that see later
     drafts, or not themselves."""
