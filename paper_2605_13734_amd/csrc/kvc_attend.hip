@@ -818,13 +818,15 @@ struct Results {
 // One block of 16 * TILES rows (16 up to 16 rows, 32 up to 64), whose queries are in the registers of every wave; the waves take 32 tokens
 // at a time in turn and their results meet in LDS at the end.  So a code is read once per block, straight into the registers of the one
 // wave that uses it: with few rows a token brings 160 to 300 bytes per head and 512 operations per row, and HBM is the bound.
-// One token over 128k (8 KV heads, 4 query heads each, 4 bits, groups of 32, fp16; 168 MB): 42.9 us, 3.9 TB/s; what more tokens cost,
-// 5.5 TB/s (a large copy: 4.8, a large fill: 6.8), and some 12 us do not depend on them: dividing (2), pages and queries (3), the waves' join (2),
-// the workgroups' join (4 to 6).  Vector instructions take 46 % of the time there, matrix instructions 18 %.  4 sequences of 16k to
-// 32k tokens, 8-bit K, groups of 128 (92 MB): 26.0 us.  One token over 1k: 11.2 us, latencies one after the other.
-// Two tiles per block, 16 queries of 4 heads over 1k tokens: 15 us.
+// One token over 128k (8 KV heads, 4 query heads each, 4 bits, groups of 32, fp16; 168 MB): 41.4 us, 4.1 TB/s; what more tokens cost,
+// 5.5 TB/s (a large copy: 4.8, a large fill: 6.8), and some 11 us do not depend on them: dividing (1.5), pages and queries (3), the waves' join
+// (2), the workgroups' join (4 to 5).  Vector instructions take 46 % of the time there, matrix instructions 18 %.  4 sequences of 16k to
+// 32k tokens, 8-bit K, groups of 128 (92 MB): 25.1 us.  One token over 1k: 10.9 us, latencies one after the other and one compute unit's
+// arithmetic per head.
+// Two tiles per block, 15 drafts over 1k tokens, 4 query heads: 14.5 us.
 // As many waves as the registers leave room for in a compute unit, three per SIMD or two: what is in flight is what hides the memory's
-// latency, one step's codes per wave.  (The same with four waves and three workgroups per unit was slower: more pieces to join.)
+// latency, one step's codes per wave.  (Four waves and three workgroups per unit: more pieces to join.  Eight waves with one / two / three steps
+// in flight: 19.1 / 18.7 / 19.0 us for 32 sequences of 0.5 to 2k tokens, twelve with one 17.5; sixteen spill.)
 constexpr int few_waves(int tiles, bool rotate) { return tiles == 1 && !rotate ? 12 : 8; }
 
 template <int BITS_K, int BITS_V, int GROUP, int TILES, bool ROTATE, int PARTS>
@@ -1056,9 +1058,9 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
 // 250 (fp16, groups of 32) of vector arithmetic: scales and zeros 48 or 80, 16 exponentials and their arguments, the sums, the
 // second parts, a quarter of the operands' making.  The two kinds hardly run side by side: for two waves per SIMD 16 products of
 // one kind and 64 multiply-adds take 235 and 188 ns alone and 432 together; only exponentials run beside products for nothing.
-// 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 692 us, 788 TFLOP/s (a large library product:
+// 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 688 us, 793 TFLOP/s (a large library product:
 // 1135), vector instructions 55 % of the time and matrix instructions 40 %; trees of 64 drafts over 8 x 8k (rotated 4 bits, groups of 32,
-// fp16; 137 GFLOP, 275 with the second parts): 297 us, 45 % and 49 %.
+// fp16; 137 GFLOP, 275 with the second parts): 288 us, 45 % and 50 %.
 // Two workgroups per compute unit, as 256 registers per lane allow (with rotated queries and groups of 32 some 64 to 152 bytes per lane do
 // not fit: addresses and numbers of the next load, once per 128 tokens, nothing between the products).  The scores of the next 32
 // tokens ahead of this one's weights gained nothing, nor did two steps of the loop at once.
