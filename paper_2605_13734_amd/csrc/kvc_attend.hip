@@ -1175,8 +1175,8 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
 #pragma unroll
                 for (int t = 0; t < 2; ++t) only_seen(score[t], c, seq, query[t].draft, token, past, end, have);
             }
-            // values are requested before the weights are made, as many as the registers hold (512 new tokens behind 32k: 718 -> 690 us;
-            // rotated, trees of 64 over 8k, none / 4 / 8: 307 / 299 / 312)
+            // values are requested before the weights are made, as many as the registers hold (512 new tokens behind 32k, one / 8: 700 / 687 us;
+            // rotated, trees of 64 over 8k, one / 4 / 8: 315 / 293 / 324)
             constexpr int early = ROTATE ? 4 : 8;
             half8 weight[2][PARTS], value[early];
 #pragma unroll
@@ -1184,7 +1184,8 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
             __builtin_amdgcn_s_setprio(0);
 #pragma unroll
             for (int t = 0; t < 2; ++t) state[t].weigh(score[t], query[t].factor, weight[t]);
-            // (a wave that has products to start goes before one with weights to make: 353 -> 340 us for trees of 64 over 8k)
+            // (a wave that has products to start goes before one with weights to make: 301 -> 293 us for trees of 64 over 8k, 718 -> 687 for 512
+            // new tokens behind 32k)
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int ch = 0; ch < 8; ++ch) {

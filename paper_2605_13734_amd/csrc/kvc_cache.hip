@@ -14,7 +14,7 @@ struct kvc_cache_plan_s {
 namespace kvc {
 
 // Workgroups that the chip holds, as the kernels' registers have it: one of 8 or 12 waves per compute unit for up to 64 rows, two of 4 waves
-// for more (64 drafts over 8k tokens, 8 heads, divided among 512 / 768 / 1024: 305 us, and more with either of the others).
+// for more (8 trees of 64 drafts over 8k tokens, 8 x 8 heads, divided among 512 / 768 / 1024: 293 / 344 / 321 us).
 constexpr int kFewGroups = 256, kManyGroups = 512;
 // What cutting sequences has to gain, in steps of a workgroup's waves, and what joining takes per piece (128 rows: 64 KB, read by one
 // workgroup; with few rows per 16 of them).  One sequence, one token, steps that cutting has to gain 1 / 2 / 3: 1k tokens 11.0 / 11.0 / 11.3 us;
