@@ -35,11 +35,33 @@ struct AttendShape {
     bool divide;
     int64_t parts, places, slots;            // parts per head and block of rows, workgroups, workgroups with results to be joined
 };
+// The largest tiles that a call with so many rows per sequence and KV head takes.
+static int most_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 64 ? 2 : kWideTiles; }
+
+// Small blocks of rows read a cache more often and share less of the codes' unpacking, large ones leave more of the chip without work and
+// have more to join.  What a call takes was measured for 1 to 16 sequences of 500 to 32k tokens, 8 KV heads, 32 to 512 rows (fp16, 4 bits,
+// groups of 32): a time for every 256 (128 rows: 512) blocks at once, and one per block and token.  Blocks of 16 / 32 / 128 rows, us:
+// 1 x 64 rows x 2k 13.0 / 15.7 / 26.0; 1 x 128 x 2k 14.2 / 16.1 / 31.4, x 16k 34.1 / 30.5 / 74.1; 1 x 512 x 2k 19.0 / 21.7 / 33.0; 4 x 256 x
+// 1k 25.7 / 18.8 / 28.6, x 8k 96.9 / 71.6 / 79.6, x 16k 178 / 134 / 130; 8 x 512 x 500 66.1 / 47.5 / 33.2, x 4k 209 / 154 / 128.
+// The formulas' choice is the best or within 12 % of it.  Up to 64 rows, blocks of 128 were never the best.
+static int tiles_of(int64_t rows, int64_t heads, int64_t tokens)
+{
+    const int most = most_tiles(rows);
+    auto blocks = [&](int size) { return (double)heads * (double)((rows + size - 1) / size); };
+    auto times = [](double blocks, double at_once) { return blocks > at_once ? blocks / at_once : 1.0; };
+    const double one = blocks(16), two = blocks(32), wide = blocks(kWideRows);
+    const double cost_one = 4.5 + 5.0 * times(one, kFewGroups) + 2.0e-5 * one * (double)tokens;
+    const double cost_two = 5.0 + 7.0 * times(two, kFewGroups) + 3.0e-5 * two * (double)tokens;
+    const double cost_wide = 18.0 + 6.0 * times(wide, kManyGroups) + 1.03e-4 * wide * (double)tokens;
+    if (most == 1 || (cost_one < cost_two && (most == 2 || cost_one < cost_wide))) return 1;
+    return most == 2 || cost_two <= cost_wide ? 2 : kWideTiles;
+}
+
 static AttendShape attend_shape(const kvc_cache_config &f, int n, int max_new, int64_t max_tokens)
 {
     AttendShape s;
     const int64_t rows = (int64_t)max_new * (f.q_heads / f.kv_heads);
-    s.tiles = rows <= 16 ? 1 : rows <= 64 ? 2 : kWideTiles;
+    s.tiles = tiles_of(rows, (int64_t)n * f.kv_heads, max_tokens);
     s.row_blocks = (int)((rows + 16 * s.tiles - 1) / (16 * s.tiles));
     const int64_t each = (int64_t)f.kv_heads * s.row_blocks;
     s.parts = (s.tiles != kWideTiles ? kFewGroups : kManyGroups) / each;
@@ -136,8 +158,8 @@ extern "C" int kvc_cache_plan(const kvc_cache_config *config, int64_t max_tokens
     p->max_batch = max_batch;
     p->page_bytes = (size_t)f.kv_heads * (f.block_tokens / kGranule) * granule_map(f.bits_k, f.bits_v, f.group).bytes;
     // the counters, and as many results as a call of up to max_new rows can have (attend_shape: each * (parts + 1) with each * parts of
-    // the groups at most and two parts or more)
-    const int tiles = attend_shape(f, 1, max_new, max_tokens).tiles;
+    // the groups at most and two parts or more, of the largest blocks that such a call may take)
+    const int tiles = most_tiles((int64_t)max_new * (f.q_heads / f.kv_heads));
     const size_t slots = (size_t)(tiles == kWideTiles ? kManyGroups : kFewGroups) * 3 / 2;
     p->workspace = max_tokens > kLeastDivided ? slots * 16 * tiles * kPartBytes + kCounters * sizeof(int) : 0;
     *out = p;

@@ -189,6 +189,44 @@ def test_attention_of_drafts_over_long_contexts(past, new, per_kv):
     assert torch.equal(a, out)
 
 
+def attend_with_loose_bounds(w, masks, tokens=1 << 22):
+    """As attend, but the call's bound of tokens is far beyond the sequences, as in a captured step of a server: blocks of 128 rows are
+    then chosen where they fit the rows."""
+    table = torch.full((len(w.new), tokens // w.page_tokens), -1, dtype=torch.int32, device="cuda")
+    table[:, : w.table.shape[1]] = w.table
+    batch = kvc.CacheBatch(w.new_start, w.tokens, table, w.most_new, tokens, w.num_pages, None if masks is None else w.mask_tensor(masks))
+    outs = []
+    for _ in range(2):
+        out = torch.full_like(w.q, float("nan"), device="cuda")
+        stat = torch.full(w.q.shape[:2], float("nan"), device="cuda")
+        w.cache.attend(batch, w.q.cuda(), out, SCALE, stat, stream())
+        outs.append(out)
+    assert not w.cache.status.any() and torch.equal(*outs)
+    w.check_attention(out, stat, SCALE, masks)
+
+
+@pytest.mark.parametrize("bits_k,bits_v,group", list(itertools.product((4, 8), (4, 8), (32, 64, 128))))
+@pytest.mark.parametrize("bf16,transform", [(False, 0), (True, 0), (False, 1), (True, 1)])
+def test_attention_of_every_kind_with_loose_bounds(bits_k, bits_v, group, bf16, transform):
+    w = World([0, 900, 45], [37, 37, 1], seed=group, kv_heads=1, per_kv=6, bf16=bf16, bits_k=bits_k, bits_v=bits_v, group=group,
+              transform=transform, block_tokens=32, limits={"tokens": 1 << 22})
+    w.page_tokens = 32
+    masks, _ = tree_masks(w.g, w.new)
+    w.fill()
+    attend_with_loose_bounds(w, masks)
+
+
+@pytest.mark.parametrize("past,new,per_kv,trees", [([16500], 64, 4, True), ([9000, 70], 64, 4, True), ([300, 0, 7000], 100, 5, False),
+                                                   ([4000], 16, 8, True), ([5000, 31], 1, 4, False), ([700], 8, 4, True)])
+def test_long_contexts_with_loose_bounds(past, new, per_kv, trees):
+    w = World(past, [new] * len(past), seed=new + len(past), kv_heads=4, per_kv=per_kv, group=64, bf16=len(past) > 1, block_tokens=64,
+              limits={"tokens": 1 << 22})
+    w.page_tokens = 64
+    masks = tree_masks(w.g, w.new)[0] if trees else None
+    w.fill()
+    attend_with_loose_bounds(w, masks)
+
+
 def test_rows_that_see_nothing():
     """Empty mask rows: zeros and -infinity where there is no context, the context alone where there is one; and rows that see later
     drafts, or not themselves."""
