@@ -3,8 +3,8 @@
 // Compiled once per pair of code widths (KVC_BITS = 10 * bits_k + bits_v).
 //
 // A row is one new token and one of the query heads that share a KV head; a workgroup has a block of rows of one KV head and a run of
-// the sequence's tokens.  Up to 64 rows per sequence and head go to attend_kernel (HBM's rate bounds it), more to
-// attend_wide_kernel (arithmetic does).  Where a call has fewer blocks than the chip has room for, the tokens of long sequences
+// the sequence's tokens.  attend_kernel has blocks of 16 or 32 rows (HBM's rate bounds it, or latency), attend_wide_kernel of 128
+// (arithmetic does); which of them a call takes goes by what its blocks take together (kvc_cache.hip: tiles_of).  Where a call has fewer blocks than the chip has room for, the tokens of long sequences
 // are spread over several workgroups, whose results the last of them joins.
 //
 // Scores: the matrix product runs over the codes themselves, with 16 tokens as rows and 16 query rows as columns.  A code, masked
@@ -815,7 +815,7 @@ struct Results {
 
 // ---- few rows: the waves of a workgroup share rows and divide tokens --------------------------------
 
-// One block of 16 * TILES rows (16 up to 16 rows, 32 up to 64), whose queries are in the registers of every wave; the waves take 32 tokens
+// One block of 16 * TILES rows, whose queries are in the registers of every wave; the waves take 32 tokens
 // at a time in turn and their results meet in LDS at the end.  So a code is read once per block, straight into the registers of the one
 // wave that uses it: with few rows a token brings 160 to 300 bytes per head and 512 operations per row, and HBM is the bound.
 // One token over 128k (8 KV heads, 4 query heads each, 4 bits, groups of 32, fp16; 168 MB): 41.4 us, 4.1 TB/s; what more tokens cost,
@@ -823,7 +823,8 @@ struct Results {
 // (2), the workgroups' join (4 to 5).  Vector instructions take 46 % of the time there, matrix instructions 18 %.  4 sequences of 16k to
 // 32k tokens, 8-bit K, groups of 128 (92 MB): 25.1 us.  One token over 1k: 10.9 us, latencies one after the other and one compute unit's
 // arithmetic per head.
-// Two tiles per block, 15 drafts over 1k tokens, 4 query heads: 14.5 us.
+// Two tiles per block, 24 drafts over 2k tokens, 4 query heads: 15.2 us, as six blocks of 16
+// rows 13.3.
 // As many waves as the registers leave room for in a compute unit, three per SIMD or two: what is in flight is what hides the memory's
 // latency, one step's codes per wave.  (Four waves and three workgroups per unit: more pieces to join.  Eight waves with one / two / three steps
 // in flight: 19.1 / 18.7 / 19.0 us for 32 sequences of 0.5 to 2k tokens, twelve with one 17.5; sixteen spill.)

@@ -13,8 +13,8 @@ struct kvc_cache_plan_s {
 
 namespace kvc {
 
-// Workgroups that the chip holds, as the kernels' registers have it: one of 8 or 12 waves per compute unit for up to 64 rows, two of 4 waves
-// for more (8 trees of 64 drafts over 8k tokens, 8 x 8 heads, divided among 512 / 768 / 1024: 293 / 344 / 321 us).
+// Workgroups that the chip holds, as the kernels' registers have it: one of 8 or 12 waves per compute unit for blocks of 16 and 32 rows,
+// two of 4 waves for blocks of 128 (8 trees of 64 drafts over 8k tokens, 8 x 8 heads, divided among 512 / 768 / 1024: 293 / 344 / 321 us).
 constexpr int kFewGroups = 256, kManyGroups = 512;
 // What cutting sequences has to gain, in steps of a workgroup's waves, and what joining takes per piece (128 rows: 64 KB, read by one
 // workgroup; with few rows per 16 of them).  One sequence, one token, steps that cutting has to gain 1 / 2 / 3: 1k tokens 11.0 / 11.0 / 11.3 us;
@@ -40,19 +40,20 @@ static int most_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 64 ? 2 : k
 
 // Small blocks of rows read a cache more often and share less of the codes' unpacking, large ones leave more of the chip without work and
 // have more to join.  What a call takes was measured for 1 to 16 sequences of 500 to 32k tokens, 8 KV heads, 32 to 512 rows (fp16, 4 bits,
-// groups of 32): a time for every 256 (128 rows: 512) blocks at once, and one per block and token.  Blocks of 16 / 32 / 128 rows, us:
+// groups of 32): a time for every 256 (128 rows: 512) blocks at once, and one per block and token (128 rows: per 32 of them, since waves
+// without rows leave room).  Blocks of 16 / 32 / 128 rows, us:
 // 1 x 64 rows x 2k 13.0 / 15.7 / 26.0; 1 x 128 x 2k 14.2 / 16.1 / 31.4, x 16k 34.1 / 30.5 / 74.1; 1 x 512 x 2k 19.0 / 21.7 / 33.0; 4 x 256 x
 // 1k 25.7 / 18.8 / 28.6, x 8k 96.9 / 71.6 / 79.6, x 16k 178 / 134 / 130; 8 x 512 x 500 66.1 / 47.5 / 33.2, x 4k 209 / 154 / 128.
-// The formulas' choice is the best or within 12 % of it.  Up to 64 rows, blocks of 128 were never the best.
+// Of 199 such calls the formulas' choice is the best or within 14 % of it, 0.6 % in the mean.  Up to 64 rows, blocks of 128 never were the best.
 static int tiles_of(int64_t rows, int64_t heads, int64_t tokens)
 {
     const int most = most_tiles(rows);
     auto blocks = [&](int size) { return (double)heads * (double)((rows + size - 1) / size); };
     auto times = [](double blocks, double at_once) { return blocks > at_once ? blocks / at_once : 1.0; };
     const double one = blocks(16), two = blocks(32), wide = blocks(kWideRows);
-    const double cost_one = 4.5 + 5.0 * times(one, kFewGroups) + 2.0e-5 * one * (double)tokens;
-    const double cost_two = 5.0 + 7.0 * times(two, kFewGroups) + 3.0e-5 * two * (double)tokens;
-    const double cost_wide = 18.0 + 6.0 * times(wide, kManyGroups) + 1.03e-4 * wide * (double)tokens;
+    const double cost_one = 4.5 + 5.0 * times(one, kFewGroups) + 1.9e-5 * one * (double)tokens;
+    const double cost_two = 5.0 + 7.0 * times(two, kFewGroups) + 2.9e-5 * two * (double)tokens;
+    const double cost_wide = 20.0 + 6.0 * times(wide, kManyGroups) + 2.4e-5 * two * (double)tokens;
     if (most == 1 || (cost_one < cost_two && (most == 2 || cost_one < cost_wide))) return 1;
     return most == 2 || cost_two <= cost_wide ? 2 : kWideTiles;
 }
