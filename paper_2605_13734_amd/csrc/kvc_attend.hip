@@ -1059,9 +1059,9 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
 // 250 (fp16, groups of 32) of vector arithmetic: scales and zeros 48 or 80, 16 exponentials and their arguments, the sums, the
 // second parts, a quarter of the operands' making.  The two kinds hardly run side by side: for two waves per SIMD 16 products of
 // one kind and 64 multiply-adds take 235 and 188 ns alone and 432 together; only exponentials run beside products for nothing.
-// 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 688 us, 793 TFLOP/s (a large library product:
+// 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 686 us, 795 TFLOP/s (a large library product:
 // 1135), vector instructions 55 % of the time and matrix instructions 40 %; trees of 64 drafts over 8 x 8k (rotated 4 bits, groups of 32,
-// fp16; 137 GFLOP, 275 with the second parts): 288 us, 45 % and 50 %.
+// fp16; 137 GFLOP, 275 with the second parts): 287 us, 45 % and 50 %.
 // Two workgroups per compute unit, as 256 registers per lane allow (with rotated queries and groups of 32 some 64 to 152 bytes per lane do
 // not fit: addresses and numbers of the next load, once per 128 tokens, nothing between the products).  The scores of the next 32
 // tokens ahead of this one's weights gained nothing, nor did two steps of the loop at once.
