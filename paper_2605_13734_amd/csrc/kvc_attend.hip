@@ -618,6 +618,17 @@ template <int STEP> __device__ __forceinline__ bool find_part(const AttendArgs &
     return false;
 }
 
+// Where a part that starts at token `begin` ends.  Granules whose page the table does not have are read from page 0 in their place, so a
+// pool without pages has no tokens to be read (reported).
+__device__ __forceinline__ int end_of(const CacheView &c, int s, const Part &part, int begin, int limit)
+{
+    if (c.num_pages == 0) {
+        if (threadIdx.x == 0) atomicOr(c.status + s, KVC_DEV_BAD_BLOCK);
+        return begin;
+    }
+    return begin + part.chunk < limit ? (int)(begin + part.chunk) : limit;
+}
+
 // ---- results of several workgroups --------------------------------------------------------------------
 
 // What workgroups leave for each other are pairs of numbers, stored as single words of agent scope: such a store goes through to memory,
@@ -852,8 +863,7 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
     const int limit = tokens_seen(c, seq, block, 16 * TILES, a.per_kv), past = seq.tokens - seq.fresh;
     const int count = (int)((limit + part.chunk - 1) / part.chunk);      // (of this block of rows)
     if (part.index >= count) return;
-    const int begin = (int)(part.index * part.chunk);
-    const int end = begin + part.chunk < limit ? (int)(begin + part.chunk) : limit;
+    const int begin = (int)(part.index * part.chunk), end = end_of(c, s, part, begin, limit);
 
     // overflow of half-precision arithmetic ends at 65504 instead of infinity (bit 23 of the mode register)
     __builtin_amdgcn_s_setreg((0 << 11) | (23 << 6) | 1, 1);
@@ -1090,8 +1100,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
     const int limit = tokens_seen(c, seq, block, kWideRows, a.per_kv), past = seq.tokens - seq.fresh;
     const int count = (int)((limit + part.chunk - 1) / part.chunk);
     if (part.index >= count) return;
-    const int begin = (int)(part.index * part.chunk);
-    const int end = begin + part.chunk < limit ? (int)(begin + part.chunk) : limit;
+    const int begin = (int)(part.index * part.chunk), end = end_of(c, s, part, begin, limit);
     __builtin_amdgcn_s_setreg((0 << 11) | (23 << 6) | 1, 1);             // (see attend_kernel)
 
     QueryTile<BITS_K, GROUP, ROTATE> query[2];
@@ -1123,7 +1132,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
             param[h] = *(const uint32_t *)(p + map.k_scales + (uint32_t)(lane % param_words) * 4u);
         }
     };
-    load(0);
+    if (rounds > 0) load(0);
     const bool busy = first + 32 * wave < rows;              // (a wave without rows still makes operands)
     for (int n = 0; n < rounds; ++n) {
         if (n) __syncthreads();              // everybody has read the round before

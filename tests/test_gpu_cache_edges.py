@@ -1,0 +1,45 @@
+"""GPU tests (run with -m gpu) of the quantised cache at the edges of what its calls accept."""
+import numpy as np
+import pytest
+import torch
+
+from cache_util import DIM
+from paper_2605_13734_amd import kvc
+
+pytestmark = pytest.mark.gpu
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def i32(*v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("new,per_kv,most", [(1, 4, 5000), (9, 4, 1 << 22), (70, 4, 1 << 22), (1, 4, 200)])
+@pytest.mark.parametrize("bf16,transform,tree", [(False, 0, False), (False, 1, True), (True, 0, True)])
+def test_a_pool_without_pages(new, per_kv, most, bf16, transform, tree):
+    """Every entry of the tables is out of range: nothing is read or written, attention gives zeros and -infinity."""
+    past = [4900 if most >= 5000 else 100, 0, 3]
+    dtype = torch.bfloat16 if bf16 else torch.float16
+    plan = kvc.CachePlan(kvc.BF16 if bf16 else kvc.F16, 2, 2 * per_kv, DIM, 4, 8, 64, 16, transform, max_batch=4, max_tokens=most, max_new=new)
+    cache = kvc.Cache(plan, 0)
+    cache.pages.fill_(0x5a)
+    table = torch.zeros(4, (most + 15) // 16, dtype=torch.int32, device="cuda")
+    mask = torch.full((3 * new, (new + 63) // 64), -1, dtype=torch.int64, device="cuda") if tree else None
+    batch = kvc.CacheBatch(i32(0, new, 2 * new, 3 * new, 3 * new), i32(*[p + new for p in past], 7), table, new, most, 0, mask)
+    want = [kvc.DEV_BAD_BLOCK] * 3 + [0]
+    q = torch.randn(3 * new, 2 * per_kv, DIM, device="cuda").to(dtype)
+    for _ in range(2):
+        out, lse = torch.full_like(q, 9.0), torch.full(q.shape[:2], 9.0, device="cuda")
+        cache.attend(batch, q, out, 0.1, lse, stream())
+        assert cache.status.tolist() == want and (out == 0).all() and (lse == -np.inf).all()
+        cache.status.zero_()
+    rows = torch.full((3 * new, 2, DIM), 3.0, dtype=dtype, device="cuda")
+    cache.store(batch, rows, rows, stream())
+    cache.load(batch, rows, rows.clone(), stream())
+    assert cache.status.tolist() == want and (rows == 3.0).all()
+    cache.status.zero_()
+    cache.keep(batch, i32(0, 1, 2, 3, 3), i32(new - 1, new - 1, new - 1), stream())
+    assert cache.status.tolist() == want and (cache.pages == 0x5a).all()
