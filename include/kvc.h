@@ -353,8 +353,9 @@ int kvc_policy_lookup(const kvc_policy_segment *table, int32_t count, double ban
  * overwritten): values are limited to +-65504 (NaN counts as 0); zero = fp16(min),
  * scale = fp16((max - min) / (2^b - 1)), code = clamp(rint((x - zero) * (1 / scale)), 0, 2^b - 1), as in
  * kvc_compress.  A code stands for code * scale + zero.  With transform = KVC_T_HADAMARD, for K whose
- * channels differ much in size, K rows are stored as H x / 8 (rounded to the type), and attention rotates the
- * queries: (H q / 16) . (H k / 8) = q . k.  V is not rotated.
+ * channels differ much in size, K rows are stored as H x / 8 (rounded to the type; a NaN in a row makes all of the
+ * row's channels NaN, so it counts as zeros), and attention rotates the queries: (H q / 16) . (H k / 8) = q . k.
+ * V is not rotated.
  *
  * Arrays of 32-bit words (lengths, tables, indices, status) have to be 4-byte aligned, masks 8-byte, all else 16-byte.
  *

@@ -127,7 +127,8 @@ __global__ __launch_bounds__(256) void cache_store_kernel(CacheView c, const uin
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         if (4 * p + 4 <= first || 4 * p >= end) continue;
-        if (ROTATE) rk[p] = hadamard_row<DT, true>(rk[p], false);
+        // (not limited by the rotation, which would make a number of NaN: rows with values to be limited are found here)
+        if (ROTATE) rk[p] = hadamard_row<DT, false>(rk[p], false);
         limit |= out_of_order<DT>(rk[p]) || out_of_order<DT>(rv[p]);
     }
     // A whole granule goes through LDS and out in pieces of 16 bytes per lane, past the caches as its rows came; part of one, and rows

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from cache_util import DIM
+from cache_util import DIM, World
 from paper_2605_13734_amd import kvc
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +43,41 @@ def test_a_pool_without_pages(new, per_kv, most, bf16, transform, tree):
     cache.status.zero_()
     cache.keep(batch, i32(0, 1, 2, 3, 3), i32(new - 1, new - 1, new - 1), stream())
     assert cache.status.tolist() == want and (cache.pages == 0x5a).all()
+
+
+def rows_without_numbers(rows, dtype):
+    """Rows with NaN, with one infinity, with both, and, for bf16, with numbers whose sums leave 32 bits; the others are normal."""
+    x = torch.randn(rows, 2, DIM, generator=torch.Generator().manual_seed(rows))
+    x[1, 0, 9] = float("nan")
+    x[2] = float("nan")
+    x[4, 1, 0], x[4, 0, 100] = float("inf"), float("-inf")
+    x[5, 1, 3], x[5, 1, 4] = float("inf"), float("-inf")
+    x[7, 0, 127], x[7, 0, 64], x[7, 1, 1] = float("-inf"), float("nan"), float("nan")
+    x[9] = 65504.0
+    if dtype == torch.bfloat16:
+        x[10] = 3.0e38
+        x[11, :, ::2], x[11, :, 1::2] = 3.0e38, -3.0e38
+        x[12, :, :64], x[12, :, 64:] = 3.0e38, -3.2e38
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("bits_k,group,transform", [(4, 32, 1), (8, 64, 1), (4, 128, 1), (8, 32, 0)])
+@pytest.mark.parametrize("past,new", [(0, 32), (3, 27)])
+def test_rows_that_hold_no_numbers(bf16, bits_k, group, transform, past, new):
+    """NaN counts as 0, also where the rotation makes it of two infinities, and what is beyond the range as its limit; whole granules and
+    parts of them.  Attention reads such a token as it is held."""
+    w = World([past], [new], seed=group, bf16=bf16, bits_k=bits_k, group=group, transform=transform, spread=False)
+    w.k[0][past: past + 16] = rows_without_numbers(16, w.dtype)
+    w.v[0][past: past + 16] = rows_without_numbers(16, w.dtype).flip(1)
+    w.fill()
+    k, v = (torch.empty(past + new, 2, DIM, dtype=w.dtype, device="cuda") for _ in range(2))
+    w.cache.load(w.all_batch(), k, v, stream())
+    held_k, held_v = w.held(0)
+    assert np.array_equal(k.double().cpu().numpy(), held_k.read_back(bf16)) and np.array_equal(v.double().cpu().numpy(), held_v.read_back(bf16))
+    assert (k[past + 2] == 0).all()
+    q, out = w.q.cuda() * 2.0 ** -12, torch.empty_like(w.q, device="cuda")
+    w.q = q.cpu()
+    w.cache.attend(w.batch(), q, out, 0.1, None, stream())
+    w.check_attention(out, None, 0.1)
+    assert not w.cache.status.any()
