@@ -407,7 +407,8 @@ class CacheBatch:
 
 class Cache:
     """One layer's pool of pages with its status words and the attention's workspace, allocated through torch (the workspace may be
-    shared between layers that run in stream order)."""
+    shared between layers that run in stream order).  The calls take tensors of the cache's device, a GPU (a cache in host memory
+    refuses them all)."""
 
     def __init__(self, plan, num_pages, device="cuda", workspace=None):
         import torch
@@ -421,6 +422,8 @@ class Cache:
         if self.workspace.numel() * self.workspace.element_size() < plan.workspace_size() or not self.workspace.is_contiguous() or \
                 self.workspace.get_device() != self._device:
             raise ValueError("the workspace has to be contiguous, on the cache's device and of kvc_cache_workspace_size bytes")
+        if not self.pages.is_cuda:           # no kernel follows its addresses: the calls find no tensor on its device
+            self._device = None
         self._pages, self._status, self._workspace = self.pages.data_ptr(), self.status.data_ptr(), self.workspace.data_ptr()
         f, lib = plan.config, load()
         self._kv_heads, self._q_heads, self._dim, self._plan = f.kv_heads, f.q_heads, f.head_dim, plan._h
