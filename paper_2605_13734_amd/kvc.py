@@ -5,6 +5,7 @@ the owner of device memory and streams.  There is no CPU fallback: `load()` rais
 library has not been built (python __graft_entry__.py, or build.py in this directory).
 """
 import ctypes as C
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -405,6 +406,13 @@ class CacheBatch:
         self._ref = C.byref(self.struct)
 
 
+def _on_device(device, call, *args):
+    """The call with its device as the current one, which is where a launch goes."""
+    import torch
+    with torch.cuda.device(device):
+        return call(*args)
+
+
 class Cache:
     """One layer's pool of pages with its status words and the attention's workspace, allocated through torch (the workspace may be
     shared between layers that run in stream order).  The calls take tensors of the cache's device, a GPU (a cache in host memory
@@ -427,7 +435,10 @@ class Cache:
         self._pages, self._status, self._workspace = self.pages.data_ptr(), self.status.data_ptr(), self.workspace.data_ptr()
         f, lib = plan.config, load()
         self._kv_heads, self._q_heads, self._dim, self._plan = f.kv_heads, f.q_heads, f.head_dim, plan._h
-        self._store, self._load, self._attend = lib.kvc_cache_store, lib.kvc_cache_load, lib.kvc_cache_attend
+        self._store, self._load, self._keep, self._attend = lib.kvc_cache_store, lib.kvc_cache_load, lib.kvc_cache_keep, lib.kvc_cache_attend
+        if torch.cuda.device_count() > 1:
+            self._store, self._load, self._keep, self._attend = (functools.partial(_on_device, self._device, call) for call in (
+                self._store, self._load, self._keep, self._attend))
 
     def _layout(self, x, heads):
         """(rows, strides) of a tensor of rows; the checks are the few that a call of microseconds can afford."""
@@ -469,8 +480,7 @@ class Cache:
             raise ValueError("keep_start [n + 1] and keep are contiguous int32 tensors on the cache's device")
         if batch.num_pages > self.num_pages or batch.device != self._device:
             raise ValueError("the batch names more pages than the pool has, or is on another device")
-        rc = _lib.kvc_cache_keep(self._plan, batch._ref, keep_start.data_ptr(), keep.data_ptr(), keep.numel(), self._pages, self._status,
-                                 stream)
+        rc = self._keep(self._plan, batch._ref, keep_start.data_ptr(), keep.data_ptr(), keep.numel(), self._pages, self._status, stream)
         if rc != OK:
             raise KvcError("kvc_cache_keep", rc)
 
