@@ -230,7 +230,7 @@ extern "C" int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_ba
     a.q_head = u.q_stride_head;
     a.o_row = u.out_stride_row;
     a.o_head = u.out_stride_head;
-    a.scale = u.scale * 1.44269504088896341f;
+    a.scale = u.scale;
     a.per_kv = f.q_heads / f.kv_heads;
     a.row_blocks = s.row_blocks;
     a.n = batch->n;

@@ -33,7 +33,7 @@ struct AttendArgs {
     int *counters;
     long long part_rows;           // rows that the results have room for (below 2^32 bytes)
     long long q_row, q_head, o_row, o_head;        // strides in elements
-    float scale;                   // of the scores, times log2(e)
+    float scale;                   // of the scores
     // the division of sequences (see find_part), in the tokens that a workgroup's waves take at a time: whether there is one, workgroups
     // per head and block of rows that the chip holds at once, what cutting has to gain, what joining takes per piece, and how much
     // longer a workgroup takes beside another one (0: there is none)

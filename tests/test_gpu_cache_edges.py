@@ -81,3 +81,17 @@ def test_rows_that_hold_no_numbers(bf16, bits_k, group, transform, past, new):
     w.cache.attend(w.batch(), q, out, 0.1, None, stream())
     w.check_attention(out, None, 0.1)
     assert not w.cache.status.any()
+
+
+@pytest.mark.parametrize("exponent,scale", [(-124, 2.9e38), (-124, -2.9e38), (-131, 2.9e38), (-124, 2.0e36), (-118, 3.0e34)])
+@pytest.mark.parametrize("new,transform,bits_k", [(2, 0, 4), (2, 1, 8), (40, 0, 8), (40, 1, 4)])
+def test_smallest_queries_and_largest_scales(exponent, scale, new, transform, bits_k):
+    """Queries near the smallest numbers of bf16, some below its normal ones, with scales that bring their scores to a few units; scales
+    whose product with log2(e) is beyond the largest number."""
+    w = World([200], [new], seed=7, bf16=True, bits_k=bits_k, transform=transform, spread=False)
+    w.q = (w.q.float() * 2.0 ** exponent).to(w.dtype)
+    w.fill()
+    out, lse = torch.empty_like(w.q, device="cuda"), torch.empty(w.q.shape[:2], device="cuda")
+    w.cache.attend(w.batch(), w.q.cuda(), out, scale, lse, stream())
+    assert w.q.abs().max() > 0 and not w.cache.status.any()
+    w.check_attention(out, lse, scale)
