@@ -266,7 +266,7 @@ template <int BITS_K, int GROUP, bool ROTATE> struct QueryTile {
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[g][e]));
         top = row_max(top);
         int power = (int)(__float_as_uint(top) >> 23) - 127;                 // 2^power <= top < 2^(power + 1)
-        power = top == 0.0f ? 7 : power < -119 ? -119 : power > 119 ? 119 : power;       // (both powers below are normal numbers)
+        power = top == 0.0f ? 7 : power < -119 ? -119 : power;               // (both powers below are normal numbers)
         float down = __uint_as_float((uint32_t)(127 + 7 - power) << 23);
         // (log2(e) last: the scale times it may be beyond the largest number)
         factor = fabsf(a.scale) * __uint_as_float((uint32_t)(127 + power - 7) << 23) * (ROTATE ? 0.0625f : 1.0f) * 1.44269504088896341f;

@@ -95,3 +95,16 @@ def test_smallest_queries_and_largest_scales(exponent, scale, new, transform, bi
     w.cache.attend(w.batch(), w.q.cuda(), out, scale, lse, stream())
     assert w.q.abs().max() > 0 and not w.cache.status.any()
     w.check_attention(out, lse, scale)
+
+
+@pytest.mark.parametrize("exponent", [118, 121, 124])
+@pytest.mark.parametrize("new,transform,bits_k,group", [(2, 0, 4, 32), (2, 1, 8, 128), (40, 0, 8, 128), (40, 1, 4, 64), (3, 0, 4, 128)])
+def test_largest_queries(exponent, new, transform, bits_k, group):
+    """Queries up to 2^127 whose channels have one sign for the most part, so that the sums of their groups are large, too."""
+    w = World([200], [new], seed=7, bf16=True, bits_k=bits_k, transform=transform, group=group, spread=False)
+    w.q = ((w.q.float() + 2.0).clamp(-1.0, 7.0) * 2.0 ** (exponent - (7 if transform else 0))).to(w.dtype)
+    w.fill()
+    out, lse, scale = torch.empty_like(w.q, device="cuda"), torch.empty(w.q.shape[:2], device="cuda"), 0.1 * 2.0 ** -exponent
+    w.cache.attend(w.batch(), w.q.cuda(), out, scale, lse, stream())
+    assert torch.isfinite(w.q).all() and not w.cache.status.any()
+    w.check_attention(out, lse, scale)
