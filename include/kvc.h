@@ -441,7 +441,8 @@ typedef struct {
  *                     Codes move as they are.  Indices that do not ascend or are out of range:
  *                     KVC_DEV_BAD_ROW, and the sequence stays as it is
  *   kvc_cache_attend  out = softmax(scale * q k^T) v over the tokens that a new token sees; a row that sees none
- *                     gives zeros and lse = -infinity (so does one whose scores are all below -7.9e17).  Scores, maxima and
+ *                     gives zeros and lse = -infinity (so does one whose scores are all below -7.9e17), one whose query holds NaN
+ *                     or an infinity, or whose scores leave 32 bits, NaN and lse = NaN.  Scores, maxima and
  *                     sums are held in 32 bits; weights and values enter the second product as fp16 numbers (values with
  *                     one rounding; weights with one where results are bf16, as two numbers where they are fp16).
  *                     workspace: DEVICE, kvc_cache_workspace_size bytes, all zero before the first call that

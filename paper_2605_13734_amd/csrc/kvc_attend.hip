@@ -38,6 +38,9 @@ constexpr float kBias = 6.0f;                // weights are kept as 2^(6 + score
 // are all below -2^60 counts as one that sees nothing.
 constexpr float kLeastFactor = 0x1p-60f, kNothing = -0x1p60f;
 constexpr float kLowest = -3.4028235e38f;
+// With overflow of half-precision arithmetic set to end at the largest number, matrix instructions take NaN as 0 and infinities as the largest
+// number.  A query that holds one has zeros in the products, is marked, and its row's sum becomes NaN at the end.
+constexpr int kLostRow = 1 << 30;            // (new tokens are below it)
 
 // maximum and sum over the four lanes that hold one row
 __device__ __forceinline__ float row_max(float x)
@@ -150,10 +153,10 @@ template <int BITS> __device__ __forceinline__ uint32_t value_pair(uint32_t pair
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, scale, zero));
 }
 
-// log of the sum of exp(scores), from the maximum in base 2 and the sum of weights
+// log of the sum of exp(scores), from the maximum in base 2 and the sum of weights (NaN: NaN)
 __device__ __forceinline__ float lse_of(float top, float total)
 {
-    return total > 0.0f ? (top - kBias + __builtin_log2f(total)) * 0.69314718055994531f : -__builtin_inff();
+    return total == 0.0f ? -__builtin_inff() : (top - kBias + __builtin_log2f(total)) * 0.69314718055994531f;
 }
 
 // The tokens that some row of a block of rows can see: [0, this).
@@ -184,7 +187,7 @@ template <int BITS_K, int GROUP, bool ROTATE> struct QueryTile {
     half8 part[4 * PARTS];
     half4 sums;                              // of the groups, high parts in lanes q = 0, remainders in lanes q = 1
     float factor;                            // scores in base 2 = products * factor (not negative)
-    int draft;                               // the row's new token
+    int draft;                               // the row's new token; kLostRow added: a query that holds NaN or an infinity
 
     __device__ __forceinline__ void fetch(const AttendArgs &a, const Sequence &seq, int head, int row, int rows)
     {
@@ -273,6 +276,7 @@ template <int BITS_K, int GROUP, bool ROTATE> struct QueryTile {
         factor = fmaxf(factor, kLeastFactor);
         if (a.scale < 0.0f) down = -down;
         float sum[4] = {0, 0, 0, 0};
+        bool good = true;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             float y[8];
@@ -293,10 +297,18 @@ template <int BITS_K, int GROUP, bool ROTATE> struct QueryTile {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const float total = row_sum(sum[g]);
+            good = good && fabsf(total) <= 65504.0f;         // (128 numbers below 2^8, or an infinity or NaN)
             const _Float16 high = (_Float16)total;
             // column i of a 16 x 16 x 16 product: lanes of q = 0 hold the sums, of q = 1 what their rounding left
             const float low = total - (float)high;
             sums[g] = g >= groups ? (_Float16)0.0f : q == 0 ? high : q == 1 ? (_Float16)low : (_Float16)0.0f;
+        }
+        if (!__all(good)) {
+#pragma unroll
+            for (int g = 0; g < 4 * PARTS; ++g) part[g] = good ? part[g] : half8{};
+            sums = good ? sums : half4{};
+            factor = good ? factor : kLeastFactor;
+            draft = good ? draft : draft | kLostRow;
         }
     }
 };
@@ -348,7 +360,12 @@ template <int PARTS> struct RowState {
 #pragma unroll
         for (int ch = 0; ch < 8; ++ch) out[ch] = f32x4{0, 0, 0, 0};
     }
-    __device__ __forceinline__ float total() const { return PARTS == 2 ? norm[0] : row_sum(norm[0]); }
+    // the row's sum of weights: NaN where its query or its scores are beyond 32 bits, 0 where it sees nothing
+    __device__ __forceinline__ float total(int draft) const
+    {
+        const float sum = PARTS == 2 ? norm[0] : row_sum(norm[0]);
+        return (draft >= kLostRow && sum != 0.0f) || top > 3.4028235e38f ? __builtin_nanf("") : sum;
+    }
     // Weights of 32 tokens.
     __device__ __forceinline__ void weigh(const float score[8], float factor, half8 weight[PARTS])
     {
@@ -816,7 +833,7 @@ struct Results {
     {
         int d, query_head;
         uint16_t *to = row(r, d, query_head);
-        const float share = total > 0.0f ? 1.0f / total : 0.0f;
+        const float share = total == 0.0f ? 0.0f : 1.0f / total;
         float y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = x[e] * share;
@@ -949,7 +966,7 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
         }
         if (!all) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) only_seen(score[t], c, seq, query[t].draft, token, past, end, f.there);
+            for (int t = 0; t < TILES; ++t) only_seen(score[t], c, seq, query[t].draft & (kLostRow - 1), token, past, end, f.there);
         }
 #pragma unroll
         for (int t = 0; t < TILES; ++t) state[t].weigh(score[t], query[t].factor, weight[t]);
@@ -989,7 +1006,7 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
     // ---- the waves' results: maxima and sums first, then the rows, a tile at a time
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
-        const float total = state[t].total();
+        const float total = state[t].total(query[t].draft);
         if (q == 0) {
             tops[wave][16 * t + i] = state[t].top;
             norms[wave][16 * t + i] = total;
@@ -1184,7 +1201,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
             const bool have[2] = {__builtin_amdgcn_readfirstlane(present[2 * k]) != 0, __builtin_amdgcn_readfirstlane(present[2 * k + 1]) != 0};
             if (token + kStep > past || token + kStep > end || !have[0] || !have[1]) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) only_seen(score[t], c, seq, query[t].draft, token, past, end, have);
+                for (int t = 0; t < 2; ++t) only_seen(score[t], c, seq, query[t].draft & (kLostRow - 1), token, past, end, have);
             }
             // values are requested before the weights are made, as many as the registers hold (512 new tokens behind 32k, one / 8: 700 / 687 us;
             // rotated, trees of 64 over 8k, one / 4 / 8: 315 / 293 / 324)
@@ -1215,7 +1232,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
     if (count == 1) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const float total = state[t].total();
+            const float total = state[t].total(query[t].draft);
             const int row = 32 * wave + 16 * t + i;
             if (row < here) {
 #pragma unroll
@@ -1236,7 +1253,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const float total = state[t].total();
+        const float total = state[t].total(query[t].draft);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll

@@ -108,3 +108,44 @@ def test_largest_queries(exponent, new, transform, bits_k, group):
     w.cache.attend(w.batch(), w.q.cuda(), out, scale, lse, stream())
     assert torch.isfinite(w.q).all() and not w.cache.status.any()
     w.check_attention(out, lse, scale)
+
+
+@pytest.mark.parametrize("bf16,new,transform,past", [(False, 1, 0, 40), (True, 9, 1, 40), (False, 40, 0, 40), (True, 40, 1, 40), (False, 1, 0, 3000),
+                                                     (True, 70, 0, 3000)])
+def test_queries_that_are_no_numbers(bf16, new, transform, past):
+    """A query with NaN or an infinity gives NaN, as a result and as its lse, and no other row; one that sees nothing gives zeros and
+    -infinity whatever it is."""
+    w = World([past], [new], seed=11, bf16=bf16, transform=transform)
+    w.fill()
+    q = w.q.cuda()
+    lost = torch.zeros(w.q.shape[:2], dtype=torch.bool)
+    for r, h, value in ((0, 1, "nan"), (0, 4, "inf"), (new - 1, 6, "-inf"), (new // 2, 7, "nan")):
+        q[r, h, (5 * r + h) % DIM] = float(value)
+        lost[r, h] = True
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    w.cache.attend(w.batch(), q, out, 0.1, lse, stream())
+    assert torch.isnan(out.cpu()[lost]).all() and torch.isnan(lse.cpu()[lost]).all()
+    good, good_lse = torch.empty_like(q), torch.empty_like(lse)
+    w.cache.attend(w.batch(), w.q.cuda(), good, 0.1, good_lse, stream())
+    out, lse = torch.where(lost.cuda()[:, :, None], good, out), torch.where(lost.cuda(), good_lse, lse)
+    w.check_attention(out, lse, 0.1)
+    if new > 1:
+        w = World([0], [new], seed=12, bf16=bf16, transform=transform)
+        w.fill()
+        masks = [[0] + [1 << i for i in range(1, new)]]
+        q = w.q.cuda()
+        q[0] = float("nan")
+        w.cache.attend(w.batch(w.mask_tensor(masks)), q, out, 0.1, lse, stream())
+        assert (out[0] == 0).all() and (lse[0] == -np.inf).all()
+        w.q[0] = 0.0
+        w.check_attention(out, lse, 0.1, masks)
+
+
+@pytest.mark.parametrize("new,bf16", [(1, False), (1, True), (40, False), (40, True)])
+def test_scores_beyond_32_bits(new, bf16):
+    """No sum of weights can be made of infinite scores: NaN, and not a row that sees nothing."""
+    w = World([200], [new], seed=13, bf16=bf16)
+    w.fill()
+    out, lse = torch.zeros_like(w.q, device="cuda"), torch.zeros(w.q.shape[:2], device="cuda")
+    w.cache.attend(w.batch(), w.q.cuda(), out, 3.0e38, lse, stream())
+    assert torch.isnan(out).all() and torch.isnan(lse).all() and not w.cache.status.any()
