@@ -389,8 +389,17 @@ size_t kvc_cache_page_bytes(const kvc_cache_plan_t *plan);
 size_t kvc_cache_workspace_size(const kvc_cache_plan_t *plan);
 
 /*
+ * Query rows (new tokens times query heads of one KV head) that a workgroup of kvc_cache_attend has in a call with these bounds: 16, 32 or
+ * 128, the size for which the time of such a call is estimated to be the least; 0 where there is nothing to do or the call is
+ * refused.  The lengths are on the device, so max_tokens stands for them: with a bound far above the lengths blocks are taken that are
+ * large for the call (128 rows of 8 KV heads over 2k tokens: 14 us with blocks of 16, which a bound of 2k gives, 31 with blocks of
+ * 128, which a bound of 128k gives).
+ */
+int32_t kvc_cache_block_rows(const kvc_cache_plan_t *plan, int32_t n, int32_t max_new, int64_t max_tokens);
+
+/*
  * The sequences of a call.  Their lengths are on the device, so that a captured graph can be replayed as they
- * grow; n, max_new and max_tokens are bounds that fix the launch and must hold for what the device arrays say.
+ * grow; n, max_new and max_tokens are bounds that fix the launch (kvc_cache_block_rows) and must hold for what the device arrays say.
  * Sequence s has tokens[s] tokens, the last new_start[s+1] - new_start[s] of which are its new ones:
  * rows new_start[s] ... of the tensors that a call names.  Token t of it lives in page
  * block_table[s * table_stride + t / block_tokens].

@@ -173,6 +173,13 @@ extern "C" size_t kvc_cache_page_bytes(const kvc_cache_plan_t *plan) { return pl
 
 extern "C" size_t kvc_cache_workspace_size(const kvc_cache_plan_t *plan) { return plan ? plan->workspace : 0; }
 
+extern "C" int32_t kvc_cache_block_rows(const kvc_cache_plan_t *plan, int32_t n, int32_t max_new, int64_t max_tokens)
+{
+    using namespace kvc;
+    if (!plan || n < 1 || max_new < 1 || max_tokens < 1 || n > plan->max_batch || max_new > plan->max_new || max_tokens > plan->max_tokens) return 0;
+    return 16 * attend_shape(plan->config, n, max_new < max_tokens ? max_new : (int)max_tokens, max_tokens).tiles;
+}
+
 extern "C" int kvc_cache_store(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_rows *rows, void *pages,
                                int32_t *dev_status, void *hip_stream)
 {

@@ -20,7 +20,7 @@ DEV_BAD_BLOCK, DEV_BAD_HEADER, DEV_BAD_CHUNK, DEV_BAD_TABLE, DEV_SCAN_TIMEOUT, D
 SYMBOLS = ["kvc_plan", "kvc_plan_free", "kvc_payload_size", "kvc_workspace_size", "kvc_compress",
            "kvc_decompress", "kvc_payload_inspect", "kvc_check_block_table", "kvc_status_string",
            "kvc_trace", "kvc_selftest", "kvc_table_bytes", "kvc_workspace_init", "kvc_compress_static", "kvc_stream_probe", "kvc_profile_throughput", "kvc_benefit_threshold", "kvc_policy_build",
-           "kvc_policy_lookup", "kvc_cache_plan", "kvc_cache_plan_free", "kvc_cache_page_bytes", "kvc_cache_workspace_size",
+           "kvc_policy_lookup", "kvc_cache_plan", "kvc_cache_plan_free", "kvc_cache_page_bytes", "kvc_cache_workspace_size", "kvc_cache_block_rows",
            "kvc_cache_store", "kvc_cache_load", "kvc_cache_keep", "kvc_cache_attend"]
 
 
@@ -130,6 +130,7 @@ def load():
         L.kvc_cache_page_bytes.restype = C.c_size_t
         L.kvc_cache_workspace_size.argtypes = [C.c_void_p]
         L.kvc_cache_workspace_size.restype = C.c_size_t
+        L.kvc_cache_block_rows.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int64]
         for f in (L.kvc_cache_store, L.kvc_cache_load):
             f.argtypes = [C.c_void_p, C.POINTER(CacheSequences), C.POINTER(CacheRows), C.c_void_p, C.c_void_p, C.c_void_p]
         L.kvc_cache_keep.argtypes = [C.c_void_p, C.POINTER(CacheSequences), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
@@ -377,6 +378,10 @@ class CachePlan:
 
     def workspace_size(self):
         return load().kvc_cache_workspace_size(self._h)
+
+    def block_rows(self, n, max_new, max_tokens):
+        """kvc_cache_block_rows: query rows of a workgroup of an attention with these bounds."""
+        return load().kvc_cache_block_rows(self._h, n, max_new, max_tokens)
 
 
 class CacheBatch:

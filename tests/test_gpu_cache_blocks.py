@@ -1,0 +1,119 @@
+"""GPU tests (run with -m gpu) of the attention over the quantised cache in blocks of 16, 32 and 128 query rows, whichever of them a call
+of these sizes would take by itself: the call's bounds are such that it takes the size that a test names, and the test checks that it does."""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+from cache_util import DIM, World, tree_masks
+from paper_2605_13734_amd import kvc
+
+pytestmark = pytest.mark.gpu
+SCALE = 1 / np.sqrt(DIM)
+SIZES = (16, 32, 128)
+MOST = 1 << 22                               # the bound of tokens far beyond the lengths
+NEW = {16: 7, 32: 15, 128: 37}               # new tokens, four query heads per KV head: 28, 60 and 148 rows
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+class Blocks(World):
+    """A world whose attention takes blocks of `size` rows."""
+
+    def __init__(self, size, past, new, **kw):
+        super().__init__(past, new, limits={"tokens": MOST}, **kw)
+        self.page_tokens, self.bound = kw.get("block_tokens", 16), self.most if size == 16 else MOST
+        assert self.plan.block_rows(len(new), self.most_new, self.bound) == size
+
+    def wide_batch(self, masks=None, words=None):
+        table = torch.full((len(self.new), max(self.bound // self.page_tokens, self.table.shape[1])), -1, dtype=torch.int32, device=self.device)
+        table[:, : self.table.shape[1]] = self.table
+        return kvc.CacheBatch(self.new_start, self.tokens, table, self.most_new, self.bound, self.num_pages,
+                              None if masks is None else self.mask_tensor(masks, words))
+
+    def attend(self, masks=None, words=None, status=None):
+        """Twice the same bits; (results, lse)."""
+        batch, outs = self.wide_batch(masks, words), []
+        for _ in range(2):
+            out, lse = torch.full_like(self.q, float("nan"), device="cuda"), torch.full(self.q.shape[:2], float("nan"), device="cuda")
+            self.cache.attend(batch, self.q.cuda(), out, SCALE, lse, stream())
+            outs.append((out, lse))
+        assert self.cache.status.tolist() == (status or [0] * len(self.new))
+        assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+        return outs[0]
+
+
+@pytest.mark.parametrize("bits_k,bits_v,group", list(itertools.product((4, 8), (4, 8), (32, 64, 128))))
+@pytest.mark.parametrize("bf16,transform", [(False, 0), (True, 0), (False, 1), (True, 1)])
+@pytest.mark.parametrize("size", SIZES)
+def test_every_kind(size, bf16, transform, bits_k, bits_v, group):
+    """Each pair of widths, group, type and transform: consecutive tokens and trees, behind nothing and behind contexts."""
+    new = NEW[size]
+    w = Blocks(size, [0, 900, 45], [new, new, 1], seed=size + group, kv_heads=1, per_kv=4, bf16=bf16, bits_k=bits_k, bits_v=bits_v, group=group,
+               transform=transform, block_tokens=32)
+    masks, _ = tree_masks(w.g, w.new)
+    w.fill()
+    for m in (None, masks):
+        w.check_attention(*w.attend(m), SCALE, m)
+
+
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("bf16,transform,group,per_kv", [(False, 0, 64, 4), (True, 1, 32, 4), (True, 0, 128, 4)])
+def test_long_contexts_in_pieces(size, bf16, transform, group, per_kv):
+    """Contexts that are cut into many pieces, each sequence into another number of them, at lengths around a step's and a page's end."""
+    new = NEW[size]
+    w = Blocks(size, [6007, 130, 2048 - new, 3000], [new, new - 1, new, 2], seed=size, kv_heads=2, per_kv=per_kv, bf16=bf16, transform=transform, group=group,
+               block_tokens=64)
+    masks, _ = tree_masks(w.g, w.new)
+    w.fill()
+    for m in (None, masks):
+        w.check_attention(*w.attend(m), SCALE, m)
+
+
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("bf16,transform", [(False, 0), (True, 1)])
+def test_rows_that_see_nothing(size, bf16, transform):
+    """Empty mask rows: zeros and -infinity without a context, the context alone with one; rows that see others but not themselves."""
+    new = NEW[size]
+    w = Blocks(size, [0, 9, 700], [new, new, new], seed=4, kv_heads=1, bf16=bf16, transform=transform)
+    masks = [[0 if i % 3 == 0 else 1 << ((i * 5) % new) for i in range(new)] for _ in range(2)] + [[0] * new]
+    w.fill()
+    out, lse = w.attend(masks)
+    w.check_attention(out, lse, SCALE, masks)
+    assert (out[0] == 0).all() and (lse[0] == -np.inf).all() and (out[3] == 0).all() and not (out[new] == 0).all()
+
+
+@pytest.mark.parametrize("size,new,per_kv", [(16, 70, 1), (32, 64, 1), (32, 50, 1), (128, 150, 2), (128, 200, 1)])
+@pytest.mark.parametrize("words", [None, 5])
+def test_masks_of_several_words(size, new, per_kv, words):
+    """More than 64 new tokens, contexts of odd lengths, masks with more words than are needed."""
+    w = Blocks(size, [0, 77, 413], [new, new - 3, min(new, 65)], seed=new, kv_heads=1, per_kv=per_kv)
+    masks, _ = tree_masks(w.g, w.new)
+    w.fill()
+    w.check_attention(*w.attend(masks, words), SCALE, masks)
+
+
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("bf16,transform,trees", [(False, 0, False), (True, 1, True)])
+def test_pages_outside_the_pool(size, bf16, transform, trees):
+    """Entries out of range, one, two and all of a step's: reported, and attention goes on with the other tokens; a sequence without
+    a page that is there gives zeros."""
+    new = NEW[size]
+    w = Blocks(size, [700, 60, 12], [new, new, new], seed=14, kv_heads=1, bf16=bf16, transform=transform)
+    masks = tree_masks(w.g, w.new)[0] if trees else None
+    w.fill()
+    lost = [1, 2, 5, 9, 30, 31, 40]
+    w.table[0, lost] = torch.tensor([w.num_pages, -5, -1, 1 << 30, w.num_pages + 7, -(1 << 31), w.num_pages], dtype=torch.int32, device="cuda")
+    w.table[2] = -1
+    before = w.cache.pages.clone()
+    out, lse = w.attend(masks, status=[kvc.DEV_BAD_BLOCK, 0, kvc.DEV_BAD_BLOCK])
+    assert torch.equal(before, w.cache.pages)
+    assert (out[2 * new:] == 0).all() and (lse[2 * new:] == -np.inf).all()
+    # the same as a sequence without those tokens
+    keep = [t for t in range(700 + new) if t // 16 not in lost]
+    w.k[0], w.v[0], w.past, w.total = w.k[0][keep], w.v[0][keep], [700 - 16 * len(lost), 60], [len(keep), 60 + new]
+    w.new = w.new[:2]
+    w.check_attention(out[: 2 * new], lse[: 2 * new], SCALE, None if masks is None else masks[:2])
