@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from cache_util import DIM, World, tree_masks
+from oracle import cache_ref
 from paper_2605_13734_amd import kvc
 
 pytestmark = pytest.mark.gpu
@@ -117,3 +118,32 @@ def test_pages_outside_the_pool(size, bf16, transform, trees):
     w.k[0], w.v[0], w.past, w.total = w.k[0][keep], w.v[0][keep], [700 - 16 * len(lost), 60], [len(keep), 60 + new]
     w.new = w.new[:2]
     w.check_attention(out[: 2 * new], lse[: 2 * new], SCALE, None if masks is None else masks[:2])
+
+
+@pytest.mark.parametrize("size,new", [(16, 5), (32, 6), (128, 20)])
+@pytest.mark.parametrize("transform,bits_k", [(0, 4), (0, 8), (1, 8)])
+@pytest.mark.parametrize("places", [(0, 1), (3, 37)])
+def test_weights_of_half_precision_results(size, new, transform, bits_k, places):
+    """Two tokens with values of 1 and -1, held exactly, and scores that differ by 2^-9 to 2^-6; all others weigh less than e^-15.
+    The result, below 2^-6, is the difference of two weights near one half, so an error of 2^-12 of one of them (a single half-precision
+    number) would be 2^-14 at least in most of 100 rows and more.  What is allowed: half a unit of the result (2^-11 of it, at most 2^-17) and 2^-18
+    for the scores (32 bits, below 8: 2^-21 each), the exponentials and the rest of the weights (2^-22)."""
+    w = Blocks(size, [40, 38], [new, new], seed=21, kv_heads=2, per_kv=4, bits_k=bits_k, bits_v=8, transform=transform, spread=False)
+    for s in range(2):
+        w.k[s][:] = -16.0
+        w.k[s][places[0]], w.k[s][places[1]] = 1.0, 1.0 - 2.0 ** -8
+        w.v[s][:] = 1.0
+        w.v[s][places[1]] = -1.0
+    w.q[:] = torch.rand(2 * new, 8, 1, generator=w.g).half() + 1.0
+    w.fill()
+    batch, out = w.wide_batch(), torch.empty_like(w.q, device="cuda")
+    w.cache.attend(batch, w.q.cuda(), out, 1.0 / DIM, None, stream())
+    for s in range(2):
+        k, v = w.held(s)
+        q = w.q[s * new: (s + 1) * new].double().numpy()
+        want, _, _, _ = cache_ref.attention(q, k, v, w.seen(s), 1.0 / DIM, 4)
+        assert 0 < np.abs(want).min() and np.abs(want).max() < 2.0 ** -6
+        got = out[s * new: (s + 1) * new].double().cpu().numpy()
+        off = np.abs(got - want)
+        assert np.all(off <= np.abs(want) * 2.0 ** -11 + 2.0 ** -18), off.max()
+    assert not w.cache.status.any()
