@@ -39,8 +39,8 @@ constexpr float kBias = 6.0f;                // weights are kept as 2^(6 + score
 constexpr float kLeastFactor = 0x1p-60f, kNothing = -0x1p60f;
 constexpr float kLowest = -3.4028235e38f;
 // With overflow of half-precision arithmetic set to end at the largest number, matrix instructions take NaN as 0 and infinities as the largest
-// number.  A query that holds one has zeros in the products, is marked, and its row's sum becomes NaN at the end.
-constexpr int kLostRow = 1 << 30;            // (new tokens are below it)
+// number.  A query that holds one has zeros in the products, is marked in LDS (a register would be held through all of the tokens), and
+// its row's sum becomes NaN at the end.
 
 // maximum and sum over the four lanes that hold one row
 __device__ __forceinline__ float row_max(float x)
@@ -187,7 +187,7 @@ template <int BITS_K, int GROUP, bool ROTATE> struct QueryTile {
     half8 part[4 * PARTS];
     half4 sums;                              // of the groups, high parts in lanes q = 0, remainders in lanes q = 1
     float factor;                            // scores in base 2 = products * factor (not negative)
-    int draft;                               // the row's new token; kLostRow added: a query that holds NaN or an infinity
+    int draft;                               // the row's new token
 
     __device__ __forceinline__ void fetch(const AttendArgs &a, const Sequence &seq, int head, int row, int rows)
     {
@@ -218,7 +218,8 @@ template <int BITS_K, int GROUP, bool ROTATE> struct QueryTile {
         factor = __uint_as_float(w[2]);
         draft = (int)w[3];
     }
-    __device__ __forceinline__ void prepare(const AttendArgs &a)
+    // whether the query is made of numbers
+    __device__ __forceinline__ bool prepare(const AttendArgs &a)
     {
         constexpr int groups = kDim / GROUP;
         const int lane = lane_id(), q = lane >> 4;
@@ -308,8 +309,8 @@ template <int BITS_K, int GROUP, bool ROTATE> struct QueryTile {
             for (int g = 0; g < 4 * PARTS; ++g) part[g] = good ? part[g] : half8{};
             sums = good ? sums : half4{};
             factor = good ? factor : kLeastFactor;
-            draft = good ? draft : draft | kLostRow;
         }
+        return good;
     }
 };
 
@@ -361,10 +362,10 @@ template <int PARTS> struct RowState {
         for (int ch = 0; ch < 8; ++ch) out[ch] = f32x4{0, 0, 0, 0};
     }
     // the row's sum of weights: NaN where its query or its scores are beyond 32 bits, 0 where it sees nothing
-    __device__ __forceinline__ float total(int draft) const
+    __device__ __forceinline__ float total(bool lost) const
     {
         const float sum = PARTS == 2 ? norm[0] : row_sum(norm[0]);
-        return (draft >= kLostRow && sum != 0.0f) || top > 3.4028235e38f ? __builtin_nanf("") : sum;
+        return (lost && sum != 0.0f) || top > 3.4028235e38f ? __builtin_nanf("") : sum;
     }
     // Weights of 32 tokens.
     __device__ __forceinline__ void weigh(const float score[8], float factor, half8 weight[PARTS])
@@ -867,6 +868,7 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
     typedef RawGranule<BITS_K, BITS_V, GROUP> Raw;
     __shared__ __attribute__((aligned(16))) float sums[waves][16][kDim + 4];
     __shared__ float tops[waves][16 * TILES], norms[waves][16 * TILES];
+    __shared__ int lost[16 * TILES];         // rows whose queries are no numbers
 
     const CacheView &c = a.c;
     const int lane = lane_id(), wave = wave_id(), q = lane >> 4, i = lane & 15;
@@ -937,7 +939,7 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
         if (wave == t) {                     // one wave per tile prepares it for all of them
-            query[t].prepare(a);
+            lost[16 * t + i] = !query[t].prepare(a);
             query[t].put(shared_queries + t * Query::kPlaces);
         }
     __syncthreads();
@@ -966,7 +968,7 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
         }
         if (!all) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) only_seen(score[t], c, seq, query[t].draft & (kLostRow - 1), token, past, end, f.there);
+            for (int t = 0; t < TILES; ++t) only_seen(score[t], c, seq, query[t].draft, token, past, end, f.there);
         }
 #pragma unroll
         for (int t = 0; t < TILES; ++t) state[t].weigh(score[t], query[t].factor, weight[t]);
@@ -1006,7 +1008,7 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
     // ---- the waves' results: maxima and sums first, then the rows, a tile at a time
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
-        const float total = state[t].total(query[t].draft);
+        const float total = state[t].total(lost[16 * t + i] != 0);
         if (q == 0) {
             tops[wave][16 * t + i] = state[t].top;
             norms[wave][16 * t + i] = total;
@@ -1104,6 +1106,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
     u32x4(*values)[8][64] = (u32x4(*)[8][64])(lds + 2 * kManyWaves * 4 * 64);      // of 4 steps
     __shared__ __attribute__((aligned(16))) uint32_t params[2 * kManyWaves][param_words];
     __shared__ int present[2 * kManyWaves];
+    __shared__ int lost[kWideRows];          // rows whose queries are no numbers
 
     const CacheView &c = a.c;
     const int lane = lane_id(), wave = wave_id(), q = lane >> 4, i = lane & 15;
@@ -1128,7 +1131,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         query[t].fetch(a, seq, head, first + 32 * wave + 16 * t + i, rows);
-        query[t].prepare(a);
+        lost[32 * wave + 16 * t + i] = !query[t].prepare(a);
         state[t].clear();
         __builtin_amdgcn_sched_barrier(0);   // (one tile's numbers in 32 bits at a time)
     }
@@ -1201,7 +1204,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
             const bool have[2] = {__builtin_amdgcn_readfirstlane(present[2 * k]) != 0, __builtin_amdgcn_readfirstlane(present[2 * k + 1]) != 0};
             if (token + kStep > past || token + kStep > end || !have[0] || !have[1]) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) only_seen(score[t], c, seq, query[t].draft & (kLostRow - 1), token, past, end, have);
+                for (int t = 0; t < 2; ++t) only_seen(score[t], c, seq, query[t].draft, token, past, end, have);
             }
             // values are requested before the weights are made, as many as the registers hold (512 new tokens behind 32k, one / 8: 700 / 687 us;
             // rotated, trees of 64 over 8k, one / 4 / 8: 315 / 293 / 324)
@@ -1232,7 +1235,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
     if (count == 1) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const float total = state[t].total(query[t].draft);
+            const float total = state[t].total(lost[32 * wave + 16 * t + i] != 0);
             const int row = 32 * wave + 16 * t + i;
             if (row < here) {
 #pragma unroll
@@ -1253,7 +1256,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const float total = state[t].total(query[t].draft);
+        const float total = state[t].total(lost[32 * wave + 16 * t + i] != 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
