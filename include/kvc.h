@@ -410,6 +410,9 @@ int32_t kvc_cache_block_rows(const kvc_cache_plan_t *plan, int32_t n, int32_t ma
  * A sequence whose numbers do not fit (more than max_new new rows, tokens < new rows or > max_tokens,
  * rows outside the tensors) is left out and gets KVC_DEV_BAD_ROW; a page outside [0, num_pages) is
  * neither written nor read (attention skips its tokens) and sets KVC_DEV_BAD_BLOCK.
+ * An attention is divided among workgroups by max_new and by the number of sequences, so sequences with many and with few new tokens
+ * belong in calls of their own: 512 new tokens over 32k and one token over 128k (8 KV heads, 64 query heads) take 0.87 and 0.04 ms
+ * in two calls, 5.1 in one.
  */
 typedef struct {
     int32_t n, max_new;
@@ -452,8 +455,10 @@ typedef struct {
  *   kvc_cache_attend  out = softmax(scale * q k^T) v over the tokens that a new token sees; a row that sees none
  *                     gives zeros and lse = -infinity (so does one whose scores are all below -7.9e17), one whose query holds NaN
  *                     or an infinity, or whose scores leave 32 bits, NaN and lse = NaN.  Scores, maxima and
- *                     sums are held in 32 bits; weights and values enter the second product as fp16 numbers (values with
- *                     one rounding; weights with one where results are bf16, as two numbers where they are fp16).
+ *                     sums are held in 32 bits; queries enter the first product as fp16 numbers times a power of two (as two
+ *                     numbers where they are rotated; elements 2^-17 and more below a query's largest lose bits), weights and values the
+ *                     second as fp16 numbers (values with one rounding; weights with one where results are bf16, as two
+ *                     numbers where they are fp16).
  *                     workspace: DEVICE, kvc_cache_workspace_size bytes, all zero before the first call that
  *                     uses it (calls leave what has to be zero as they find it), may be NULL when that is 0;
  *                     several plans may share one of the largest size; calls on one workspace must be in

@@ -11,8 +11,9 @@
 // out of its word together with a second one, is a half-precision subnormal, code * 2^-24 (or 2^-20), which the matrix
 // instructions take as it is; the group's scale multiplies the product in 32 bits and the zero enters through one more product, of
 // the zeros with the sums of the query's groups: sum_d q_d (code_d scale + zero) = scale sum_d q_d code_d + zero sum_d q_d.
-// So a key costs a mask per two codes and no rounding.  Queries are scaled by a power of two to a maximum in [2^7, 2^8) (exact, and
-// the sums stay in the half type's range); a rotated query is the sum of two half-precision parts.
+// So a key costs a mask per two codes and no rounding.  Queries are scaled by a power of two to a maximum in [2^7, 2^8), so that the sums
+// stay in the half type's range, and are half-precision numbers there: exact, but for elements 2^-17 and more below the largest, which lose
+// bits (2^-28 of the largest at most); a rotated query is the sum of two half-precision parts.
 // Softmax: running maximum and sum per row in 32 bits, base 2; sums are rescaled only when a maximum has grown by more than
 // 2^kSlack.  A lane holds the weights of tokens 4 q ... 4 q + 3 of two granules for one row, which is the operand that the second
 // product takes: nothing moves between lanes.
@@ -848,16 +849,18 @@ struct Results {
 // One block of 16 * TILES rows, whose queries are in the registers of every wave; the waves take 32 tokens
 // at a time in turn and their results meet in LDS at the end.  So a code is read once per block, straight into the registers of the one
 // wave that uses it: with few rows a token brings 160 to 300 bytes per head and 512 operations per row, and HBM is the bound.
-// One token over 128k (8 KV heads, 4 query heads each, 4 bits, groups of 32, fp16; 168 MB): 41.4 us, 4.1 TB/s; what more tokens cost,
-// 5.5 TB/s (a large copy: 4.8, a large fill: 6.8), and some 11 us do not depend on them: dividing (1.5), pages and queries (3), the waves' join
-// (2), the workgroups' join (4 to 5).  Vector instructions take 46 % of the time there, matrix instructions 18 %.  4 sequences of 16k to
-// 32k tokens, 8-bit K, groups of 128 (92 MB): 25.1 us.  One token over 1k: 10.9 us, latencies one after the other and one compute unit's
+// One token over 128k (8 KV heads, 4 query heads each, 4 bits, groups of 32, fp16; 168 MB): 41.5 us, 4.1 TB/s; what more tokens cost,
+// 5.5 TB/s (pure reads past the caches reach 7.0, and why these do not is not known), and some 11 us do not depend on them: dividing (1.5), pages and queries (3), the waves' join
+// (2), the workgroups' join (4 to 5).  Vector instructions take 45 % of the time there, matrix instructions 17 %.  4 sequences of 16k to
+// 32k tokens, 8-bit K, groups of 128 (92 MB): 25.2 us.  One token over 1k: 10.9 us, latencies one after the other and one compute unit's
 // arithmetic per head.
-// Two tiles per block, 24 drafts over 2k tokens, 4 query heads: 15.2 us, as six blocks of 16
-// rows 13.3.
+// Two tiles per block, 64 drafts over 16k tokens, 4 query heads: 45 us, in blocks of 16 rows 54, of 128 71; 24 drafts over 2k 15.7, in blocks
+// of 16 13.9.
 // As many waves as the registers leave room for in a compute unit, three per SIMD or two: what is in flight is what hides the memory's
 // latency, one step's codes per wave.  (Four waves and three workgroups per unit: more pieces to join.  Eight waves with one / two / three steps
-// in flight: 19.1 / 18.7 / 19.0 us for 32 sequences of 0.5 to 2k tokens, twelve with one 17.5; sixteen spill.)
+// in flight: 19.1 / 18.7 / 19.0 us for 32 sequences of 0.5 to 2k tokens, twelve with one 17.5; sixteen spill.)  Two
+// tiles of rotated queries do not fit in full: 36 to 108 bytes per lane are held in memory with groups of 32, up to 32 with larger ones, and up to
+// twelve registers per 32 tokens come from there.
 constexpr int few_waves(int tiles, bool rotate) { return tiles == 1 && !rotate ? 12 : 8; }
 
 template <int BITS_K, int BITS_V, int GROUP, int TILES, bool ROTATE, int PARTS>
@@ -1087,13 +1090,16 @@ __global__ __launch_bounds__(64 * few_waves(TILES, ROTATE), few_waves(TILES, ROT
 // Arithmetic bounds it: per wave and 32 tokens 36 matrix instructions (16 of 16 x 16 x 32 for the scores, 4 smaller ones for the zeros, 16
 // for the values; a second part of rotated queries adds 16, of the weights for fp16 results 20) and some 180 (bf16, groups of 64) to
 // 250 (fp16, groups of 32) of vector arithmetic: scales and zeros 48 or 80, 16 exponentials and their arguments, the sums, the
-// second parts, a quarter of the operands' making.  The two kinds hardly run side by side: for two waves per SIMD 16 products of
-// one kind and 64 multiply-adds take 235 and 188 ns alone and 432 together; only exponentials run beside products for nothing.
-// 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 686 us, 795 TFLOP/s (a large library product:
-// 1135), vector instructions 55 % of the time and matrix instructions 40 %; trees of 64 drafts over 8 x 8k (rotated 4 bits, groups of 32,
-// fp16; 137 GFLOP, 275 with the second parts): 287 us, 45 % and 50 %.
-// Two workgroups per compute unit, as 256 registers per lane allow (with rotated queries and groups of 32 some 64 to 152 bytes per lane do
-// not fit: addresses and numbers of the next load, once per 128 tokens, nothing between the products).  The scores of the next 32
+// second parts, a quarter of the operands' making.  Two waves of a SIMD get little from each other: 16 products
+// and 64 multiply-adds of each take 226 and 159 ns alone, 399 one kind after the other in both waves, 392 with four multiply-adds behind
+// every product, and 470 (twice 235) where one wave has all the products and the other all the multiply-adds; only exponentials run
+// beside products for nothing.
+// 512 new tokens behind 32k (8 x 8 heads, 8 bits, groups of 64, bf16; 545 GFLOP): 690 us, 790 TFLOP/s (a large library product:
+// 1135; fp16, with weights in two parts, 857), vector instructions 56 % of the time and matrix instructions 40 %; trees of 64 drafts over
+// 8 x 8k (rotated 4 bits, groups of 32, fp16; 137 GFLOP, 275 with the second parts): 285 us, 46 % and 51 %.
+// Two workgroups per compute unit, as 256 registers per lane allow.  Not all fits: with rotated queries 84 to 156 bytes per lane are held
+// in memory (groups of 64 24 to 116, of 128 up to 60), without up to 20, nearly all of them numbers of the beginning, the next load and
+// the end; among the products of 32 tokens up to four registers come from there.  The scores of the next 32
 // tokens ahead of this one's weights gained nothing, nor did two steps of the loop at once.
 template <int BITS_K, int BITS_V, int GROUP, bool ROTATE, int PARTS>
 __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendArgs a)
@@ -1206,8 +1212,8 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void attend_wide_kernel(AttendA
 #pragma unroll
                 for (int t = 0; t < 2; ++t) only_seen(score[t], c, seq, query[t].draft, token, past, end, have);
             }
-            // values are requested before the weights are made, as many as the registers hold (512 new tokens behind 32k, one / 8: 700 / 687 us;
-            // rotated, trees of 64 over 8k, one / 4 / 8: 315 / 293 / 324)
+            // values are requested before the weights are made, as many as the registers hold (when measured: 512 new tokens behind 32k, one / 8:
+            // 700 / 687 us; rotated, trees of 64 over 8k, one / 4 / 8: 315 / 293 / 324)
             constexpr int early = ROTATE ? 4 : 8;
             half8 weight[2][PARTS], value[early];
 #pragma unroll
