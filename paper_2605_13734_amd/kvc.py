@@ -421,7 +421,7 @@ def _on_device(device, call, *args):
 class Cache:
     """One layer's pool of pages with its status words and the attention's workspace, allocated through torch (the workspace may be
     shared between layers that run in stream order).  The calls take tensors of the cache's device, a GPU (a cache in host memory
-    refuses them all)."""
+    refuses them all), and go to `stream`, a raw handle (torch.cuda.current_stream().cuda_stream; None is the null stream)."""
 
     def __init__(self, plan, num_pages, device="cuda", workspace=None):
         import torch
