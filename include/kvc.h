@@ -50,7 +50,8 @@ enum {
     KVC_DEV_BAD_TABLE = 8,     /* code-length table is not a complete prefix code             */
     KVC_DEV_SCAN_TIMEOUT = 16, /* internal: chunk-offset scan gave up waiting; the payload's
                                   directory, header sizes and size word are not written       */
-    KVC_DEV_BAD_ROW = 32       /* kvc_cache_*: rows, tokens or indices of a sequence do not fit */
+    KVC_DEV_BAD_ROW = 32,      /* kvc_cache_*, kvc_prompt_*: rows, tokens or indices of a sequence do not fit */
+    KVC_DEV_NO_PAGE = 64       /* kvc_cache_advance: no free pages for a sequence             */
 };
 
 enum { KVC_F16 = 1, KVC_BF16 = 2 };
@@ -473,6 +474,134 @@ int kvc_cache_keep(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, c
                    int64_t keep_rows, void *pages, int32_t *dev_status, void *hip_stream);
 int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch, const kvc_cache_queries *queries,
                      const void *pages, int32_t *dev_status, void *workspace, void *hip_stream);
+
+/*
+ * The sequences of a step, on the GPU: kvc_cache_advance makes the arrays that the other calls read, from what every sequence holds, keeps
+ * and gets, and moves pages between the block tables and the free ones.
+ *
+ * Sequence s has held[s] tokens in the cache.  The first kept[s] of them remain (all of them where kept is NULL; fewer after drafts
+ * were refused, none when it ends) and fresh[s] new ones follow (none where fresh is NULL).  It needs ceil(t / block_tokens) pages for t
+ * tokens, in the first places of its row of the block table.
+ *   held         in and out: kept + fresh afterwards
+ *   free_pages   in and out: word 0 the number of free pages, words 1 to 3 zero, then that many page numbers, and room for num_pages in
+ *                all.  Pages are taken from the last one downwards, in the order of the sequences; what sequences give back in the same
+ *                call is taken first, in the order in which it was held, and the rest of it goes onto the stack, the first given last: two
+ *                calls that take and give back the same leave the stack as it was
+ *   block_table  in and out: places of pages that are taken are written, all others left
+ *   new_start    out, n + 1: first new row of every sequence (a sequence whose fresh[s] is not in 0 ... max_new has none)
+ *   tokens       out, n: kept + fresh, or -1 where the sequence is left out (which the other calls refuse: KVC_DEV_BAD_ROW)
+ *   positions    out, `rows` words or NULL: the token number of every new row
+ *   slots        out, `rows` 64-bit words or NULL: page * block_tokens + place inside the page of every new row
+ * Rows behind the last sequence's, and those of sequences that are left out, get -1.  A sequence is left out, and keeps what it holds, where
+ * its numbers do not fit (0 <= kept <= held <= max_tokens, 0 <= fresh <= max_new, kept + fresh <= max_tokens, rows up to `rows`):
+ * KVC_DEV_BAD_ROW; or where it needs more pages and those left by the sequences before it (left out or not) are too few:
+ * KVC_DEV_NO_PAGE.  A page outside [0, num_pages) in the stack or among the given ones is passed on as -1: KVC_DEV_BAD_BLOCK.
+ * Up to KVC_MOST_ADVANCING sequences.  Arrays do not overlap; slots is 8-byte aligned.  Like the other calls it is enqueued on hip_stream
+ * and may be captured.
+ */
+#define KVC_MOST_ADVANCING 4096
+typedef struct {
+    int32_t n, max_new;
+    int64_t max_tokens, rows;
+    int32_t *held;                       /* DEVICE, n */
+    const int32_t *kept, *fresh;         /* DEVICE, n, or NULL */
+    int32_t *free_pages;                 /* DEVICE, 4 + num_pages */
+    int32_t *block_table;                /* DEVICE, n x table_stride, table_stride >= ceil(max_tokens / block_tokens) */
+    int64_t table_stride;
+    int32_t *new_start, *tokens;         /* DEVICE, n + 1 and n */
+    int32_t *positions;                  /* DEVICE or NULL, rows */
+    int64_t *slots;                      /* DEVICE or NULL, rows */
+    int32_t num_pages;
+} kvc_cache_step;
+
+int kvc_cache_advance(const kvc_cache_plan_t *plan, const kvc_cache_step *step, int32_t *dev_status, void *hip_stream);
+
+/*
+ * ---- Prompts, before their K and V are cached or sent ---------------------------------------
+ *
+ * What a prefill worker (section 4: Prefill -> Compression) does with the heads of a layer in 16 bits: queries and keys are normed per
+ * head and rotated by their positions (kvc_prompt_rotate, also for the new tokens of a decode step), and the prompt is attended
+ * (kvc_prompt_attend); kvc_compress and kvc_cache_store take its K and V.
+ *
+ *   dtype        KVC_F16 or KVC_BF16: type of queries, keys, values, weights and results
+ *   layout       pairs of channels that are rotated together: KVC_ROTARY_HALVES (i, i + rotary_dim / 2) or KVC_ROTARY_PAIRS (2 i, 2 i + 1)
+ *   norm         1: heads are divided by sqrt(mean of squares + eps) and multiplied by a weight per channel before the rotation
+ *   rotary_dim   channels that are rotated, the first ones: a multiple of 16 up to head_dim, or 0; the others pass
+ *   frequencies  HOST, rotary_dim / 2 values, copied by the plan: radians per position of every pair (kvc_rotary_frequencies)
+ *   amplitude    factor of cosines and sines (1, or what a scaling for long contexts asks for)
+ *   kv_heads, q_heads, head_dim   as for the cache
+ */
+enum { KVC_ROTARY_HALVES = 0, KVC_ROTARY_PAIRS = 1 };
+typedef struct {
+    uint8_t dtype, layout, norm;
+    int32_t kv_heads, q_heads, head_dim, rotary_dim;
+    float eps, amplitude;
+    const double *frequencies;
+} kvc_prompt_config;
+
+typedef struct kvc_prompt_plan_s kvc_prompt_plan_t;    /* opaque, host memory */
+
+/*
+ * Host function: base^(-2 i / rotary_dim) for i = 0 ... rotary_dim / 2 - 1, and scaled for contexts longer than the original ones:
+ *   KVC_SCALE_LINEAR  all divided by factor
+ *   KVC_SCALE_BASE    base * factor^(rotary_dim / (rotary_dim - 2)) as the base
+ *   KVC_SCALE_BANDS   divided by factor where a pair makes fewer than `low` turns in original_tokens, unchanged where it makes more than
+ *                     `high`, in between the mixture that is linear in the turns
+ *   KVC_SCALE_RAMP    the same with a mixture that is linear in the pair's number, between (rounded outwards) those that make `high` and
+ *                     `low` turns
+ * KVC_ERR_ARG for values outside: base > 1, rotary_dim even, factor >= 1, 0 < low < high, original_tokens >= 1.
+ */
+enum { KVC_SCALE_NONE = 0, KVC_SCALE_LINEAR = 1, KVC_SCALE_BASE = 2, KVC_SCALE_BANDS = 3, KVC_SCALE_RAMP = 4 };
+int kvc_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double low, double high,
+                           int64_t original_tokens, double *frequencies);
+
+/* Validates a configuration; max_batch sequences in one kvc_prompt_attend.  Touches no device; read-only afterwards, so several threads may
+ * use one plan.  Errors as for kvc_cache_plan. */
+int kvc_prompt_plan(const kvc_prompt_config *config, int32_t max_batch, kvc_prompt_plan_t **out);
+void kvc_prompt_plan_free(kvc_prompt_plan_t *plan);
+
+/* Queries and keys of `rows` rows.  Element d of head h of row r at q + r * q_stride_row + h * q_stride_head + d; strides are multiples of
+ * 8.  q or k may be NULL (the other alone), and q_out = q, k_out = k with the same strides. */
+typedef struct {
+    const void *q, *k;                   /* DEVICE */
+    void *q_out, *k_out;                 /* DEVICE */
+    const void *q_weight, *k_weight;     /* DEVICE, head_dim values; not looked at where the plan does not norm */
+    const int32_t *positions;            /* DEVICE, rows; rows with a position below zero are left as they are */
+    int64_t rows, q_stride_row, q_stride_head, k_stride_row, k_stride_head, q_out_stride_row, q_out_stride_head, k_out_stride_row,
+        k_out_stride_head;
+} kvc_prompt_rows;
+
+/* The prompts of a call: sequence s has rows start[s] ... start[s + 1] - 1.  max_rows bounds their rows and fixes the launch; a sequence
+ * whose numbers do not fit (start below zero or descending, more than max_rows rows, rows outside the tensors) is left out: KVC_DEV_BAD_ROW
+ * (behind descending starts two sequences may have the same rows, which then get the result of one of them). */
+typedef struct {
+    int32_t n, max_rows;
+    const int32_t *start;                /* DEVICE, n + 1 */
+} kvc_prompt_batch;
+
+/* Queries, keys, values and results of `rows` rows; strides are multiples of 8.  lse: optional, [rows][q_heads].  out may be q itself, with
+ * the same strides. */
+typedef struct {
+    const void *q, *k, *v;               /* DEVICE */
+    void *out;                           /* DEVICE */
+    float *lse;                          /* DEVICE or NULL: log(sum of exp(scores)), for joining with other attention */
+    int64_t rows, q_stride_row, q_stride_head, k_stride_row, k_stride_head, v_stride_row, v_stride_head, out_stride_row, out_stride_head;
+    float scale;                         /* of the scores, usually 1 / sqrt(head_dim); -1e38 to 1e38 */
+} kvc_prompt_heads;
+
+/*
+ * Everything is enqueued on hip_stream; nothing is allocated, copied or waited for, and the calls may be captured into a graph.
+ *   kvc_prompt_rotate   in 32 bits, rounded once; angles are exact to 2^-31 of a turn at every position.  NaN and infinities stay in
+ *                       their head, and in their pair where heads are not normed
+ *   kvc_prompt_attend   out = softmax(scale * q k^T) v, where a row sees the rows of its sequence up to itself.  Scores, maxima and sums
+ *                       are held in 32 bits, weights enter the second product in the type (one rounding).  Rows of no sequence are left
+ *                       as they are.  What a row does not see has no influence, whatever it holds; a row that sees a NaN, or an infinity
+ *                       that its result depends on, has no finite result there (NaN or an infinity).  dev_status: n words, bits are OR-ed in.  Equal
+ *                       inputs give equal bits
+ */
+int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt_rows *rows, void *hip_stream);
+int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt_batch *batch, const kvc_prompt_heads *heads, int32_t *dev_status,
+                      void *hip_stream);
 
 const char *kvc_status_string(int status);
 

@@ -1,5 +1,6 @@
 // Host side of the quantised cache: plans, checks of the arguments, how the attention's work is divided.
 #include "kvc_cache_internal.h"
+#include "kvc_prompt_internal.h"
 #include "../../include/kvc.h"
 
 #include <new>
@@ -204,6 +205,42 @@ extern "C" int kvc_cache_keep(const kvc_cache_plan_t *plan, const kvc_cache_batc
     if (rc != KVC_OK || nothing(batch)) return rc;
     if (!keep_start || (keep_rows && !keep) || keep_rows < 0 || keep_rows > 0x7fffffffll || !aligned(keep_start, 4) || !aligned(keep, 4)) return KVC_ERR_ARG;
     launch_cache_keep(types_of(plan->config), c, keep_start, keep, (int)keep_rows, batch->n, (hipStream_t)hip_stream);
+    return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
+}
+
+extern "C" int kvc_cache_advance(const kvc_cache_plan_t *plan, const kvc_cache_step *step, int32_t *dev_status, void *hip_stream)
+{
+    using namespace kvc;
+    if (!plan || !step) return KVC_ERR_ARG;
+    const kvc_cache_config &f = plan->config;
+    const kvc_cache_step &t = *step;
+    if (t.n < 0 || t.max_new < 0 || t.max_tokens < 0 || t.num_pages < 0 || t.table_stride < 0 || t.rows < 0) return KVC_ERR_ARG;
+    if (t.n > plan->max_batch || t.n > KVC_MOST_ADVANCING || t.max_tokens > plan->max_tokens || t.rows > 0x7fffffffll) return KVC_ERR_CAPACITY;
+    if (t.n == 0) return KVC_OK;
+    if (!t.held || !t.free_pages || !t.new_start || !t.tokens || !dev_status || (t.max_tokens && !t.block_table)) return KVC_ERR_ARG;
+    for (const void *p : {(const void *)t.held, (const void *)t.kept, (const void *)t.fresh, (const void *)t.free_pages, (const void *)t.block_table,
+                          (const void *)t.new_start, (const void *)t.tokens, (const void *)t.positions, (const void *)dev_status})
+        if (!aligned(p, 4)) return KVC_ERR_ARG;
+    if (!aligned(t.slots, 8) || t.table_stride < (t.max_tokens + f.block_tokens - 1) / f.block_tokens) return KVC_ERR_ARG;
+    AdvanceArgs a = {};
+    a.held = t.held;
+    a.kept = t.kept;
+    a.fresh = t.fresh;
+    a.free_pages = t.free_pages;
+    a.block_table = t.block_table;
+    a.new_start = t.new_start;
+    a.tokens = t.tokens;
+    a.positions = t.positions;
+    a.slots = (long long *)t.slots;
+    a.status = dev_status;
+    a.table_stride = t.table_stride;
+    a.rows = t.rows;
+    a.n = t.n;
+    a.max_new = t.max_new;
+    a.max_tokens = (int)t.max_tokens;
+    a.num_pages = t.num_pages;
+    a.page_shift = __builtin_ctz((unsigned)f.block_tokens);
+    launch_advance(a, (hipStream_t)hip_stream);
     return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
 }
 

@@ -1,0 +1,228 @@
+// A step of the cache's sequences: their lengths, the starts, positions and slots of their new rows, and the pages that they take from the
+// free ones or give back, from the tokens that they hold, keep and get.
+//
+// Everything is a few integers per sequence and a few words per page and row, so a call is bound by latency: one launch, in which every
+// workgroup makes the running sums over all sequences for itself (in LDS) and then does its share of the rows and pages.  The
+// numbers of the caller that change (held tokens, the free pages' count) are written by the workgroup that is done last, when no other
+// reads them any more.
+//
+// Pages given back and pages taken meet in one list: the free stack and above it the given ones, the last given lowest.  The i-th page
+// taken is the i-th from its top: given page i, and with no given ones left the stack's own downwards.  So a call either reads the
+// stack or pushes onto it, and two calls that take and give back the same restore it.
+#include "kvc_prompt_internal.h"
+#include "../../include/kvc.h"
+
+namespace kvc {
+
+constexpr int kThreads = 1024, kEach = KVC_MOST_ADVANCING / kThreads;       // sequences per thread at most
+constexpr uint32_t kTop = 0x7fffffffu;       // the running sums stop here
+
+__device__ __forceinline__ uint32_t add_up(uint32_t a, uint32_t b) { return a + b < kTop ? a + b : kTop; }
+
+// Sum of x over the workgroup's threads before this one; total: over all.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t &total)
+{
+    __shared__ uint32_t waves[kThreads / 64];
+    uint32_t sum = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t up = __shfl_up(sum, d, 64);
+        if (lane_id() >= d) sum = add_up(sum, up);
+    }
+    __syncthreads();                         // (the words may still be read for another sum)
+    if (lane_id() == 63) waves[wave_id()] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) {
+        if (w == wave_id()) before = total;
+        total = add_up(total, waves[w]);
+    }
+    const uint32_t up = __shfl_up(sum, 1, 64);
+    return lane_id() ? add_up(before, up) : before;
+}
+
+// The last place whose running sum is not above x (sums[0] = 0, x < sums[n]).
+__device__ __forceinline__ int place_of(const uint32_t *sums, int n, uint32_t x)
+{
+    int low = 0, high = n;
+    while (high - low > 1) {
+        const int mid = (low + high) >> 1;
+        if (sums[mid] <= x) low = mid;
+        else high = mid;
+    }
+    return low;
+}
+
+struct Step {
+    int held, kept, fresh;
+    bool fits;                               // (but for the rows' room and the pages)
+};
+__device__ __forceinline__ Step step_of(const AdvanceArgs &a, int s)
+{
+    Step t;
+    t.held = a.held[s];
+    t.kept = a.kept ? a.kept[s] : t.held;
+    t.fresh = a.fresh ? a.fresh[s] : 0;
+    t.fits = t.kept >= 0 && t.kept <= t.held && t.held <= a.max_tokens && t.fresh >= 0 && t.fresh <= a.max_new &&
+             (long long)t.kept + t.fresh <= a.max_tokens;
+    return t;
+}
+
+__global__ __launch_bounds__(kThreads) void advance_kernel(AdvanceArgs a)
+{
+    __shared__ uint32_t start[KVC_MOST_ADVANCING + 1], takes[KVC_MOST_ADVANCING + 1], gives[KVC_MOST_ADVANCING + 1];
+    __shared__ uint32_t taken;
+    __shared__ int last;
+    const int tid = threadIdx.x, each = (a.n + kThreads - 1) / kThreads;
+    const bool first = blockIdx.x == 0;
+    int count = a.free_pages[0];
+    count = count < 0 ? 0 : count > a.num_pages ? a.num_pages : count;
+    auto pages = [&](int tokens) { return (int)(((long long)tokens + (1 << a.page_shift) - 1) >> a.page_shift); };
+
+    Step mine[kEach];
+    uint32_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int s = tid * each + i;
+        mine[i] = Step{0, 0, 0, false};
+        if (i < each && s < a.n) {
+            mine[i] = step_of(a, s);
+            sum = add_up(sum, (unsigned)mine[i].fresh <= (unsigned)a.max_new ? mine[i].fresh : 0);
+        }
+    }
+    uint32_t total_rows, total_takes, total_gives;
+    uint32_t row = sum_before(sum, total_rows);
+    uint32_t take = 0, give = 0;
+    if (tid == 0) taken = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int s = tid * each + i;
+        if (i < each && s < a.n) {
+            start[s] = row;
+            row = add_up(row, (unsigned)mine[i].fresh <= (unsigned)a.max_new ? mine[i].fresh : 0);
+            mine[i].fits = mine[i].fits && (long long)row <= a.rows;
+            if (mine[i].fits) {
+                const int now = pages(mine[i].kept + mine[i].fresh), before = pages(mine[i].held);
+                take = add_up(take, now > before ? now - before : 0);
+                give = add_up(give, before > now ? before - now : 0);
+            }
+        }
+    }
+    if (tid == 0) {
+        start[a.n] = total_rows;
+        if (first) a.new_start[a.n] = (int)total_rows;
+    }
+    uint32_t my_take = sum_before(take, total_takes), my_give = sum_before(give, total_gives);
+    if (tid == 0) {
+        takes[a.n] = total_takes;
+        gives[a.n] = total_gives;
+    }
+    const uint32_t room = add_up((uint32_t)count, total_gives);
+    int after[kEach];                        // tokens that are held afterwards
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int s = tid * each + i;
+        if (i < each && s < a.n) {
+            takes[s] = my_take;
+            gives[s] = my_give;
+            int report = 0;
+            bool done = mine[i].fits;
+            if (done) {
+                const int now = pages(mine[i].kept + mine[i].fresh), before = pages(mine[i].held);
+                my_take = add_up(my_take, now > before ? now - before : 0);
+                my_give = add_up(my_give, before > now ? before - now : 0);
+                if (now > before) {
+                    done = my_take <= room && my_take < kTop;
+                    if (done) atomicMax(&taken, my_take);
+                    else report = KVC_DEV_NO_PAGE;
+                }
+            } else report = KVC_DEV_BAD_ROW;
+            after[i] = done ? mine[i].kept + mine[i].fresh : mine[i].held;
+            if (first) {
+                a.new_start[s] = (int)start[s];
+                a.tokens[s] = done ? mine[i].kept + mine[i].fresh : -1;
+                if (report) atomicOr(a.status + s, report);
+            }
+        }
+    }
+    __syncthreads();
+    total_takes = taken;
+
+    // page i of those taken; who: the sequence that it is reported for
+    auto page_taken = [&](uint32_t i, int who) {
+        int page;
+        if (i < total_gives) {
+            const int s = place_of(gives, a.n, i);
+            const Step t = step_of(a, s);
+            page = a.block_table[s * a.table_stride + pages(t.kept + t.fresh) + (i - gives[s])];
+        } else page = i - total_gives < (uint32_t)count ? a.free_pages[4 + count - 1 - (int)(i - total_gives)] : -1;
+        if ((unsigned)page < (unsigned)a.num_pages) return page;
+        atomicOr(a.status + who, KVC_DEV_BAD_BLOCK);
+        return -1;
+    };
+    const long long at = (long long)blockIdx.x * kThreads + tid, stride = (long long)gridDim.x * kThreads;
+    for (long long i = at; i < total_takes; i += stride) {
+        const int s = place_of(takes, a.n, (uint32_t)i);
+        a.block_table[s * a.table_stride + pages(a.held[s]) + (i - takes[s])] = page_taken((uint32_t)i, s);
+    }
+    // what is left of the given ones (more than the pool has: the first are dropped)
+    const long long dropped = (long long)count + total_gives - a.num_pages;
+    for (long long i = (dropped > (long long)total_takes ? dropped : (long long)total_takes) + at; i < total_gives; i += stride)
+        a.free_pages[4 + count + ((long long)total_gives - 1 - i)] = page_taken((uint32_t)i, place_of(gives, a.n, (uint32_t)i));
+    if (a.positions || a.slots) {
+        for (long long r = at; r < a.rows; r += stride) {
+            int position = -1;
+            long long slot = -1;
+            if (r < total_rows) {
+                const int s = place_of(start, a.n, (uint32_t)r);
+                const Step t = step_of(a, s);
+                const int before = pages(t.held);
+                const bool needs = pages(t.kept + t.fresh) > before;
+                if (t.fits && start[s + 1] <= a.rows && (!needs || takes[s + 1] <= total_takes)) {
+                    position = t.kept + (int)(r - start[s]);
+                    if (a.slots) {
+                        const int place = position >> a.page_shift;
+                        int page = place < before ? a.block_table[s * a.table_stride + place] : page_taken(takes[s] + (place - before), s);
+                        if ((unsigned)page < (unsigned)a.num_pages)
+                            slot = ((long long)page << a.page_shift) + (position & ((1 << a.page_shift) - 1));
+                        else atomicOr(a.status + s, KVC_DEV_BAD_BLOCK);
+                    }
+                }
+            }
+            if (a.positions) a.positions[r] = position;
+            if (a.slots) a.slots[r] = slot;
+        }
+    }
+
+    // the workgroup that is done last: all others have read what changes now
+    __syncthreads();
+    if (tid == 0) {
+        last = 1;
+        if (gridDim.x > 1) {
+            __threadfence();
+            last = atomicAdd(a.free_pages + 1, 1) == (int)gridDim.x - 1;
+        }
+    }
+    __syncthreads();
+    if (!last) return;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int s = tid * each + i;
+        if (i < each && s < a.n) a.held[s] = after[i];
+    }
+    if (tid == 0) {
+        const long long now = (long long)count + total_gives - total_takes;
+        a.free_pages[0] = (int)(now < a.num_pages ? now : a.num_pages);
+        a.free_pages[1] = 0;
+    }
+}
+
+void launch_advance(const AdvanceArgs &a, hipStream_t stream)
+{
+    const long long groups = a.positions || a.slots ? (a.rows + kThreads - 1) / kThreads : 1;
+    advance_kernel<<<(int)(groups < 1 ? 1 : groups > 256 ? 256 : groups), kThreads, 0, stream>>>(a);
+}
+
+}  // namespace kvc

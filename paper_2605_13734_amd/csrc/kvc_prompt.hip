@@ -1,0 +1,157 @@
+// Host side of the calls on prompts: plans, frequencies of the rotation, checks of the arguments.
+#include "kvc_prompt_internal.h"
+#include "../../include/kvc.h"
+
+#include <math.h>
+#include <new>
+
+struct kvc_prompt_plan_s {
+    kvc_prompt_config config;
+    int32_t max_batch;
+    uint64_t turns[kvc::kMostPairs];
+};
+
+namespace kvc {
+
+constexpr long double kTwoPi = 6.283185307179586476925286766559L;
+
+static bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+static bool strides_ok(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
+
+// The part of a turn that a position adds, in 2^-64 of a turn.
+static uint64_t turns_of(double radians)
+{
+    long double t = (long double)radians / kTwoPi;
+    t -= floorl(t);
+    // (t may be rounded up to 1: no turn)
+    return t >= 1.0L ? 0 : (uint64_t)(t * 18446744073709551616.0L);
+}
+
+}  // namespace kvc
+
+extern "C" int kvc_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double low, double high,
+                                      int64_t original_tokens, double *frequencies)
+{
+    if (!frequencies || rotary_dim < 2 || rotary_dim % 2 || !(base > 1.0) || !(base <= 1e300)) return KVC_ERR_ARG;
+    if (scaling < KVC_SCALE_NONE || scaling > KVC_SCALE_RAMP) return KVC_ERR_ARG;
+    if (scaling != KVC_SCALE_NONE && !(factor >= 1.0 && factor <= 1e9)) return KVC_ERR_ARG;
+    const bool windows = scaling == KVC_SCALE_BANDS || scaling == KVC_SCALE_RAMP;
+    if (windows && (!(low > 0.0) || !(high > low) || !(high <= 1e9) || original_tokens < 1)) return KVC_ERR_ARG;
+    if (scaling == KVC_SCALE_BASE && rotary_dim == 2) return KVC_ERR_ARG;
+    const double R = rotary_dim, two_pi = (double)kvc::kTwoPi, original = (double)original_tokens;
+    if (scaling == KVC_SCALE_BASE) base *= pow(factor, R / (R - 2.0));
+    double first = 0.0, last = 0.0;
+    if (scaling == KVC_SCALE_RAMP) {
+        first = floor(R * log(original / (high * two_pi)) / (2.0 * log(base)));
+        last = ceil(R * log(original / (low * two_pi)) / (2.0 * log(base)));
+        first = first > 0.0 ? first : 0.0;
+        last = last < R - 1.0 ? last : R - 1.0;
+    }
+    for (int32_t i = 0; i < rotary_dim / 2; ++i) {
+        const double f = pow(base, -2.0 * i / R);
+        double t = 1.0;                                  // the share of the unscaled frequency
+        if (scaling == KVC_SCALE_LINEAR) t = 0.0;
+        else if (scaling == KVC_SCALE_BANDS) t = (original * f / two_pi - low) / (high - low);
+        else if (scaling == KVC_SCALE_RAMP) t = 1.0 - (i - first) / (last - first > 0.001 ? last - first : 0.001);
+        t = t < 0.0 ? 0.0 : t > 1.0 ? 1.0 : t;
+        frequencies[i] = scaling == KVC_SCALE_NONE || scaling == KVC_SCALE_BASE ? f : t * f + (1.0 - t) * f / factor;
+    }
+    return KVC_OK;
+}
+
+extern "C" int kvc_prompt_plan(const kvc_prompt_config *config, int32_t max_batch, kvc_prompt_plan_t **out)
+{
+    using namespace kvc;
+    if (!out) return KVC_ERR_ARG;
+    *out = nullptr;
+    if (!config || max_batch < 1) return KVC_ERR_ARG;
+    const kvc_prompt_config &f = *config;
+    if (f.dtype != KVC_F16 && f.dtype != KVC_BF16) return KVC_ERR_ARG;
+    if (f.norm > 1 || (f.layout != KVC_ROTARY_HALVES && f.layout != KVC_ROTARY_PAIRS)) return KVC_ERR_ARG;
+    if (f.kv_heads < 1 || f.q_heads < 1 || f.q_heads % f.kv_heads || f.head_dim < 1) return KVC_ERR_ARG;
+    if (f.rotary_dim < 0 || f.rotary_dim > f.head_dim || f.rotary_dim % 2 || (f.rotary_dim && !f.frequencies)) return KVC_ERR_ARG;
+    if (f.norm && !(f.eps >= 0.0f && f.eps <= 1e30f)) return KVC_ERR_ARG;
+    if (f.rotary_dim && !(f.amplitude > 0.0f && f.amplitude <= 1e30f)) return KVC_ERR_ARG;
+    for (int i = 0; i < f.rotary_dim / 2; ++i)
+        if (!(f.frequencies[i] >= -1e9 && f.frequencies[i] <= 1e9)) return KVC_ERR_ARG;
+    if (f.head_dim != kDim || f.rotary_dim % 16 || f.q_heads > 65536 || max_batch > 65535) return KVC_ERR_UNSUPPORTED;
+    kvc_prompt_plan_t *p = new (std::nothrow) kvc_prompt_plan_t();
+    if (!p) return KVC_ERR_CAPACITY;
+    p->config = f;
+    p->config.frequencies = nullptr;
+    p->max_batch = max_batch;
+    for (int i = 0; i < f.rotary_dim / 2; ++i) p->turns[i] = turns_of(f.frequencies[i]);
+    *out = p;
+    return KVC_OK;
+}
+
+extern "C" void kvc_prompt_plan_free(kvc_prompt_plan_t *plan) { delete plan; }
+
+extern "C" int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt_rows *r, void *hip_stream)
+{
+    using namespace kvc;
+    if (!plan || !r || r->rows < 0) return KVC_ERR_ARG;
+    const kvc_prompt_config &f = plan->config;
+    if (r->rows == 0 || (!r->q && !r->k)) return KVC_OK;
+    if ((r->q && !r->q_out) || (r->k && !r->k_out) || (f.norm && ((r->q && !r->q_weight) || (r->k && !r->k_weight)))) return KVC_ERR_ARG;
+    if (f.rotary_dim && !r->positions) return KVC_ERR_ARG;
+    if (!aligned(r->q, 16) || !aligned(r->k, 16) || !aligned(r->q_out, 16) || !aligned(r->k_out, 16) || !aligned(r->q_weight, 16) ||
+        !aligned(r->k_weight, 16) || !aligned(r->positions, 4)) return KVC_ERR_ARG;
+    if (!strides_ok(r->q_stride_row, r->q_stride_head) || !strides_ok(r->k_stride_row, r->k_stride_head) ||
+        !strides_ok(r->q_out_stride_row, r->q_out_stride_head) || !strides_ok(r->k_out_stride_row, r->k_out_stride_head)) return KVC_ERR_ARG;
+    if (r->rows > 0x7fffffffll) return KVC_ERR_CAPACITY;
+    RotateArgs a = {};
+    a.q = RotateTensor{(const uint16_t *)r->q, f.norm ? (const uint16_t *)r->q_weight : nullptr, (uint16_t *)r->q_out, r->q_stride_row,
+                       r->q_stride_head, r->q_out_stride_row, r->q_out_stride_head, r->q ? f.q_heads : 0, 0};
+    a.k = RotateTensor{(const uint16_t *)r->k, f.norm ? (const uint16_t *)r->k_weight : nullptr, (uint16_t *)r->k_out, r->k_stride_row,
+                       r->k_stride_head, r->k_out_stride_row, r->k_out_stride_head, r->k ? f.kv_heads : 0, 0};
+    a.positions = r->positions;
+    a.rows = r->rows;
+    a.eps = f.eps;
+    a.amplitude = f.rotary_dim ? f.amplitude : 1.0f;
+    a.pairs = f.rotary_dim / 2;
+    for (int i = 0; i < a.pairs; ++i) a.turns[i] = plan->turns[i];
+    launch_rotate(f.dtype, f.layout == KVC_ROTARY_PAIRS, f.norm != 0, a, (hipStream_t)hip_stream);
+    return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
+}
+
+extern "C" int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt_batch *batch, const kvc_prompt_heads *heads,
+                                 int32_t *dev_status, void *hip_stream)
+{
+    using namespace kvc;
+    if (!plan || !batch || !heads) return KVC_ERR_ARG;
+    const kvc_prompt_config &f = plan->config;
+    const kvc_prompt_heads &h = *heads;
+    if (batch->n < 0 || batch->max_rows < 0 || h.rows < 0) return KVC_ERR_ARG;
+    if (batch->n > plan->max_batch || h.rows > 0x7fffffffll) return KVC_ERR_CAPACITY;
+    if (batch->n == 0 || batch->max_rows == 0) return KVC_OK;
+    if (!batch->start || !dev_status || (h.rows && (!h.q || !h.k || !h.v || !h.out))) return KVC_ERR_ARG;
+    if (!aligned(batch->start, 4) || !aligned(dev_status, 4) || !aligned(h.q, 16) || !aligned(h.k, 16) || !aligned(h.v, 16) || !aligned(h.out, 16) ||
+        !aligned(h.lse, 4)) return KVC_ERR_ARG;
+    if (!strides_ok(h.q_stride_row, h.q_stride_head) || !strides_ok(h.k_stride_row, h.k_stride_head) ||
+        !strides_ok(h.v_stride_row, h.v_stride_head) || !strides_ok(h.out_stride_row, h.out_stride_head)) return KVC_ERR_ARG;
+    if (!(h.scale >= -1e38f && h.scale <= 1e38f)) return KVC_ERR_ARG;
+    PromptArgs a = {};
+    a.q = (const uint16_t *)h.q;
+    a.k = (const uint16_t *)h.k;
+    a.v = (const uint16_t *)h.v;
+    a.out = (uint16_t *)h.out;
+    a.lse = h.lse;
+    a.start = batch->start;
+    a.status = dev_status;
+    a.rows = h.rows;
+    a.q_row = h.q_stride_row, a.q_head = h.q_stride_head;
+    a.k_row = h.k_stride_row, a.k_head = h.k_stride_head;
+    a.v_row = h.v_stride_row, a.v_head = h.v_stride_head;
+    a.o_row = h.out_stride_row, a.o_head = h.out_stride_head;
+    // (a factor of zero would turn the -infinity of scores that are not seen into NaN)
+    a.factor = h.scale == 0.0f ? 1.0f : fabsf(h.scale) * 1.44269504f;
+    a.query_and = h.scale == 0.0f ? 0u : 0xffffffffu;
+    a.query_xor = h.scale < 0.0f ? 0x80008000u : 0u;
+    a.n = batch->n;
+    a.max_rows = batch->max_rows;
+    a.kv_heads = f.kv_heads;
+    a.per_kv = f.q_heads / f.kv_heads;
+    launch_prompt(f.dtype, a, prompt_shape(a), (hipStream_t)hip_stream);
+    return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
+}

@@ -1,0 +1,194 @@
+// Queries and keys of new rows: every head normed and rotated by the row's position, in one pass.
+//
+//   y = x / sqrt(mean(x^2) + eps) * w          (where the plan norms heads)
+//   (a, b) <- A (a cos t - b sin t, a sin t + b cos t),   t = position * frequency of the pair
+//
+// All in 32 bits, rounded once as it is stored.  Bound by HBM where there are many rows (every element is read and written once) and by
+// latency where there are few.  A wave has one row and a run of its heads, four heads at a time, 16 lanes per head and 8 channels
+// per lane: cosines and sines are made once per row and wave, the mean of a head inside a row of lanes.
+//
+// Angles are fixed-point numbers of 2^-64 of a turn: a position times a frequency's part of a turn, modulo a turn, is one integer product
+// whose upper word is the angle, exact to 2^-32 of a turn wherever the position is (in 32-bit floating point a position of 10^6 would be
+// off by 0.03 radians).  Sine and cosine are the Taylor polynomials of degree 9 and 8 on an eighth of a turn to either side of a
+// quarter's multiple (the first terms left out: 2e-9 and 3e-8).
+#include "kvc_prompt_internal.h"
+
+namespace kvc {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+template <int DT> __device__ __forceinline__ uint32_t round_pair(float a, float b)
+{
+    const f32x2 x = {a, b};
+    if constexpr (DT == DT_F16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+
+// cos and sin of t * 2^-32 turns
+__device__ __forceinline__ void turn(uint32_t t, float &c, float &s)
+{
+    const uint32_t quarter = (t + 0x20000000u) >> 30;
+    const float x = (float)(int)(t - (quarter << 30)) * 1.46291807926715968e-9f;       // 2 pi / 2^32
+    const float y = x * x;
+    float sine = __builtin_fmaf(y, 2.75573192e-6f, -1.98412698e-4f);
+    sine = __builtin_fmaf(y, sine, 8.33333333e-3f);
+    sine = __builtin_fmaf(y, sine, -1.66666667e-1f);
+    sine = __builtin_fmaf(x * y, sine, x);
+    float cosine = __builtin_fmaf(y, 2.48015873e-5f, -1.38888889e-3f);
+    cosine = __builtin_fmaf(y, cosine, 4.16666667e-2f);
+    cosine = __builtin_fmaf(y, cosine, -0.5f);
+    cosine = __builtin_fmaf(y, cosine, 1.0f);
+    const bool odd = quarter & 1;
+    c = odd ? sine : cosine;
+    s = odd ? cosine : sine;
+    c = (quarter + 1) & 2 ? -c : c;
+    s = quarter & 2 ? -s : s;
+}
+
+template <int N> __device__ __forceinline__ float turned_lane(float x)       // the value N lanes further in the row of 16
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x120 + N, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum_of_row(float x)
+{
+    x += turned_lane<8>(x);
+    x += turned_lane<4>(x);
+    x += turned_lane<2>(x);
+    return x + turned_lane<1>(x);
+}
+
+// The octet of channels of the lane that holds the other half of the lane's pairs.
+__device__ __forceinline__ u32x4 other_octet(const u32x4 &x, int other, bool opposite)
+{
+    u32x4 r;
+    if (opposite) {                          // all 128 channels in halves: the lane 8 further
+#pragma unroll
+        for (int w = 0; w < 4; ++w) r[w] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x[w], 0x128, 0xf, 0xf, true);
+    } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) r[w] = (uint32_t)__builtin_amdgcn_ds_bpermute(other * 4, (int)x[w]);
+    }
+    return r;
+}
+
+template <int DT, bool NEIGHBOURS, bool NORM> __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a)
+{
+    const long long unit = (long long)blockIdx.x * 4 + wave_id();
+    const long long row = unit / a.chunks;
+    if (row >= a.rows) return;
+    const int position = a.pairs ? __builtin_amdgcn_readfirstlane(a.positions[row]) : 0;
+    if (position < 0) return;
+    const int q_chunks = (a.q.heads + a.chunk - 1) / a.chunk;
+    const int part = (int)(unit - row * a.chunks);
+    const bool is_k = part >= q_chunks;
+    const RotateTensor &x = is_k ? a.k : a.q;
+    const int first = (is_k ? part - q_chunks : part) * a.chunk;
+    const int end = first + a.chunk < x.heads ? first + a.chunk : x.heads;
+    const int lane = lane_id(), col = lane & 15, sub = lane >> 4;
+
+    // factors of the lane's channels and of their partners'
+    float own[8], other[8];
+    const int half = a.pairs / 8;            // octets of one half
+    const bool turns = col < 2 * half, front = col < half;
+    const int partner = NEIGHBOURS || !turns ? lane : front ? lane + half : lane - half;
+    if (turns) {
+        const uint64_t *f = a.turns + (NEIGHBOURS ? 4 * col : 8 * (front ? col : col - half));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (NEIGHBOURS && (e & 1)) {
+                own[e] = own[e - 1];
+                other[e] = -other[e - 1];
+                continue;
+            }
+            const uint64_t each = f[NEIGHBOURS ? e / 2 : e];
+            float c, s;
+            turn(__umulhi((uint32_t)position, (uint32_t)each) + (uint32_t)position * (uint32_t)(each >> 32), c, s);
+            own[e] = c * a.amplitude;
+            other[e] = (NEIGHBOURS || front ? -s : s) * a.amplitude;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            own[e] = 1.0f;
+            other[e] = 0.0f;
+        }
+    }
+    if (NORM) {
+        const u32x4 w = *(const u32x4 *)(x.weight + 8 * col);
+        const u32x4 p = NEIGHBOURS ? w : other_octet(w, partner, false);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            own[e] *= elem_f32<DT>(w, e);
+            other[e] *= elem_f32<DT>(p, NEIGHBOURS ? e ^ 1 : e);
+        }
+    }
+    const uint16_t *in = x.in + row * x.in_row + 8 * col;
+    uint16_t *out = x.out + row * x.out_row + 8 * col;
+    for (int h = first; h < end; h += 4) {
+        const int head = h + sub < end ? h + sub : end - 1;
+        const u32x4 r = *(const u32x4 *)(in + head * x.in_head);
+        const u32x4 p = NEIGHBOURS ? r : other_octet(r, partner, half == 8);
+        float mine[8], theirs[8], y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            mine[e] = elem_f32<DT>(r, e);
+            theirs[e] = elem_f32<DT>(p, NEIGHBOURS ? e ^ 1 : e);
+        }
+        float by = 1.0f;
+        if (NORM) {
+            float sum = 0.0f, eps = a.eps;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(mine[e], mine[e], sum);
+            sum = sum_of_row(sum);
+            // bf16 values whose squares leave 32 bits: all of the head times a power of two
+            const bool large = sum > 1e38f, small = sum < 1e-30f && eps < 1e-30f;
+            if (DT == DT_BF16 && __any(large || small)) {
+                const float f = large ? 0x1p-70f : small ? 0x1p80f : 1.0f;
+                sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    mine[e] *= f;
+                    theirs[e] *= f;
+                    sum = __builtin_fmaf(mine[e], mine[e], sum);
+                }
+                sum = sum_of_row(sum);
+                eps = eps * f * f;               // (the square alone may leave 32 bits)
+            }
+            by = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, 1.0f / kDim, eps));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            y[e] = mine[e] * own[e];
+            if (turns) y[e] = __builtin_fmaf(theirs[e], other[e], y[e]);
+            if (NORM) y[e] *= by;
+        }
+        if (h + sub < end) {
+            const u32x4 z = {round_pair<DT>(y[0], y[1]), round_pair<DT>(y[2], y[3]), round_pair<DT>(y[4], y[5]), round_pair<DT>(y[6], y[7])};
+            *(u32x4 *)(out + head * x.out_head) = z;
+        }
+    }
+}
+
+template <int DT, bool NEIGHBOURS> static void launch_layout(bool norm, const RotateArgs &a, dim3 grid, hipStream_t stream)
+{
+    if (norm) rotate_kernel<DT, NEIGHBOURS, true><<<grid, 256, 0, stream>>>(a);
+    else rotate_kernel<DT, NEIGHBOURS, false><<<grid, 256, 0, stream>>>(a);
+}
+
+// Heads of a row that a wave takes: all of a tensor's where the rows alone fill the chip, four where they do not.
+constexpr long long kManyRows = 8192;
+
+void launch_rotate(int dtype, bool neighbours, bool norm, const RotateArgs &args, hipStream_t stream)
+{
+    RotateArgs a = args;
+    const int most = a.q.heads > a.k.heads ? a.q.heads : a.k.heads;
+    a.chunk = a.rows >= kManyRows ? (most + 3) / 4 * 4 : 4;
+    a.chunks = (a.q.heads + a.chunk - 1) / a.chunk + (a.k.heads + a.chunk - 1) / a.chunk;
+    const dim3 grid((unsigned)((a.rows * a.chunks + 3) / 4));
+    if (dtype == DT_F16) neighbours ? launch_layout<DT_F16, true>(norm, a, grid, stream) : launch_layout<DT_F16, false>(norm, a, grid, stream);
+    else neighbours ? launch_layout<DT_BF16, true>(norm, a, grid, stream) : launch_layout<DT_BF16, false>(norm, a, grid, stream);
+}
+
+}  // namespace kvc

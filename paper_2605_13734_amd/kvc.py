@@ -15,13 +15,16 @@ F16, BF16 = 1, 2
 CODEC_NONE, CODEC_HUFF8 = 0, 1
 T_NONE, T_HADAMARD, T_DELTA = 0, 1, 2
 OK = 0
-DEV_BAD_BLOCK, DEV_BAD_HEADER, DEV_BAD_CHUNK, DEV_BAD_TABLE, DEV_SCAN_TIMEOUT, DEV_BAD_ROW = 1, 2, 4, 8, 16, 32
+DEV_BAD_BLOCK, DEV_BAD_HEADER, DEV_BAD_CHUNK, DEV_BAD_TABLE, DEV_SCAN_TIMEOUT, DEV_BAD_ROW, DEV_NO_PAGE = 1, 2, 4, 8, 16, 32, 64
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+SCALE_NONE, SCALE_LINEAR, SCALE_BASE, SCALE_BANDS, SCALE_RAMP = 0, 1, 2, 3, 4
 
 SYMBOLS = ["kvc_plan", "kvc_plan_free", "kvc_payload_size", "kvc_workspace_size", "kvc_compress",
            "kvc_decompress", "kvc_payload_inspect", "kvc_check_block_table", "kvc_status_string",
            "kvc_trace", "kvc_selftest", "kvc_table_bytes", "kvc_workspace_init", "kvc_compress_static", "kvc_stream_probe", "kvc_profile_throughput", "kvc_benefit_threshold", "kvc_policy_build",
            "kvc_policy_lookup", "kvc_cache_plan", "kvc_cache_plan_free", "kvc_cache_page_bytes", "kvc_cache_workspace_size", "kvc_cache_block_rows",
-           "kvc_cache_store", "kvc_cache_load", "kvc_cache_keep", "kvc_cache_attend"]
+           "kvc_cache_store", "kvc_cache_load", "kvc_cache_keep", "kvc_cache_attend", "kvc_cache_advance", "kvc_rotary_frequencies",
+           "kvc_prompt_plan", "kvc_prompt_plan_free", "kvc_prompt_rotate", "kvc_prompt_attend"]
 
 
 class Strategy(C.Structure):
@@ -70,6 +73,33 @@ class CacheRows(C.Structure):
 class CacheQueries(C.Structure):
     _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("rows", C.c_int64), ("q_stride_row", C.c_int64),
                 ("q_stride_head", C.c_int64), ("out_stride_row", C.c_int64), ("out_stride_head", C.c_int64), ("scale", C.c_float)]
+
+
+class CacheStep(C.Structure):
+    _fields_ = [("n", C.c_int32), ("max_new", C.c_int32), ("max_tokens", C.c_int64), ("rows", C.c_int64)] + \
+               [(name, C.c_void_p) for name in ("held", "kept", "fresh", "free_pages", "block_table")] + [("table_stride", C.c_int64)] + \
+               [(name, C.c_void_p) for name in ("new_start", "tokens", "positions", "slots")] + [("num_pages", C.c_int32)]
+
+
+class PromptConfig(C.Structure):
+    _fields_ = [("dtype", C.c_uint8), ("layout", C.c_uint8), ("norm", C.c_uint8), ("kv_heads", C.c_int32), ("q_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("eps", C.c_float), ("amplitude", C.c_float), ("frequencies", C.c_void_p)]
+
+
+class PromptRows(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("q", "k", "q_out", "k_out", "q_weight", "k_weight", "positions")] + \
+               [(name, C.c_int64) for name in ("rows", "q_stride_row", "q_stride_head", "k_stride_row", "k_stride_head", "q_out_stride_row",
+                                               "q_out_stride_head", "k_out_stride_row", "k_out_stride_head")]
+
+
+class PromptSequences(C.Structure):
+    _fields_ = [("n", C.c_int32), ("max_rows", C.c_int32), ("start", C.c_void_p)]
+
+
+class PromptHeads(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("q", "k", "v", "out", "lse")] + \
+               [(name, C.c_int64) for name in ("rows", "q_stride_row", "q_stride_head", "k_stride_row", "k_stride_head", "v_stride_row",
+                                               "v_stride_head", "out_stride_row", "out_stride_head")] + [("scale", C.c_float)]
 
 
 class KvcError(RuntimeError):
@@ -137,6 +167,13 @@ def load():
                                      C.c_void_p]
         L.kvc_cache_attend.argtypes = [C.c_void_p, C.POINTER(CacheSequences), C.POINTER(CacheQueries), C.c_void_p, C.c_void_p, C.c_void_p,
                                        C.c_void_p]
+        L.kvc_cache_advance.argtypes = [C.c_void_p, C.POINTER(CacheStep), C.c_void_p, C.c_void_p]
+        L.kvc_rotary_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_int64, C.c_void_p]
+        L.kvc_prompt_plan.argtypes = [C.POINTER(PromptConfig), C.c_int32, C.POINTER(C.c_void_p)]
+        L.kvc_prompt_plan_free.argtypes = [C.c_void_p]
+        L.kvc_prompt_plan_free.restype = None
+        L.kvc_prompt_rotate.argtypes = [C.c_void_p, C.POINTER(PromptRows), C.c_void_p]
+        L.kvc_prompt_attend.argtypes = [C.c_void_p, C.POINTER(PromptSequences), C.POINTER(PromptHeads), C.c_void_p, C.c_void_p]
         L.kvc_status_string.argtypes = [C.c_int]
         L.kvc_status_string.restype = C.c_char_p
         _lib = L
@@ -506,3 +543,183 @@ class Cache:
         rc = self._attend(self._plan, batch._ref, u, self._pages, self._status, self._workspace, stream)
         if rc != OK:
             raise KvcError("kvc_cache_attend", rc)
+
+
+class CachePages:
+    """Lengths, block tables and free pages of a cache's sequences (kvc_cache_advance), on the GPU.  held [n]: tokens of every sequence;
+    table [n, pages per sequence]; all pages are free at first.  The layers of a model share one: their pools have the same pages."""
+
+    def __init__(self, plan, num_pages, n, device="cuda"):
+        import torch
+        self.plan, self.num_pages = plan, num_pages
+        i32 = dict(dtype=torch.int32, device=device)
+        places = (plan.max_tokens + plan.config.block_tokens - 1) // plan.config.block_tokens
+        self.held = torch.zeros(n, **i32)
+        self.table = torch.full((n, max(places, 1)), -1, **i32)
+        self.status = torch.zeros(n, **i32)
+        self.free = torch.zeros(4 + num_pages, **i32)
+        self.set_free(torch.arange(num_pages - 1, -1, -1, dtype=torch.int32))
+        self._device = self.held.get_device() if self.held.is_cuda else None
+        self._plan, self._advance = plan._h, load().kvc_cache_advance
+        if torch.cuda.device_count() > 1:
+            self._advance = functools.partial(_on_device, self._device, self._advance)
+
+    @property
+    def free_count(self):
+        """The number of free pages, a tensor of one word."""
+        return self.free[:1]
+
+    @property
+    def free_pages(self):
+        """The stack of free pages, the next one to be taken last of the first free_count."""
+        return self.free[4:]
+
+    def set_free(self, pages):
+        """The free pages, an int32 tensor: the last is taken first."""
+        if pages.numel() > self.num_pages:
+            raise ValueError("more free pages than the pool has")
+        self.free[:4] = 0
+        self.free[0] = pages.numel()
+        self.free[4: 4 + pages.numel()] = pages.to(self.free.device)
+
+    def advance(self, new_start, tokens, kept=None, fresh=None, max_new=0, max_tokens=None, positions=None, slots=None, rows=None,
+                stream=None):
+        """kvc_cache_advance.  new_start [n + 1], tokens [n]: int32, written; kept, fresh [n]: int32 or None; positions [rows] int32,
+        slots [rows] int64: written, or None (then rows is the room that the new rows have, if it is bounded)."""
+        import torch
+        n = self.held.shape[0]
+        for x, size in ((new_start, n + 1), (tokens, n), (kept, n), (fresh, n)):
+            if x is not None and (x.dtype is not torch.int32 or x.shape != (size,) or not x.is_contiguous() or x.get_device() != self._device):
+                raise ValueError("new_start [n + 1], tokens, kept and fresh [n] are contiguous int32 tensors on the tables' device")
+        for x, dtype in ((positions, torch.int32), (slots, torch.int64)):
+            if x is not None:
+                if x.dtype is not dtype or x.dim() != 1 or not x.is_contiguous() or x.get_device() != self._device or \
+                        (rows is not None and rows != x.shape[0]):
+                    raise ValueError("positions (int32) and slots (int64) are contiguous tensors of one length on the tables' device")
+                rows = x.shape[0]
+        step = CacheStep(n, max_new, self.plan.max_tokens if max_tokens is None else max_tokens, 0x7fffffff if rows is None else rows,
+                         self.held.data_ptr(), kept.data_ptr() if kept is not None else None, fresh.data_ptr() if fresh is not None else None,
+                         self.free.data_ptr(), self.table.data_ptr(), self.table.shape[1], new_start.data_ptr(), tokens.data_ptr(),
+                         positions.data_ptr() if positions is not None else None, slots.data_ptr() if slots is not None else None,
+                         self.num_pages)
+        rc = self._advance(self._plan, step, self.status.data_ptr(), stream)
+        if rc != OK:
+            raise KvcError("kvc_cache_advance", rc)
+
+
+# ---- prompts --------------------------------------------------------------------------------------
+
+def rotary_frequencies(rotary_dim, base=10000.0, scaling=SCALE_NONE, factor=1.0, low=1.0, high=4.0, original_tokens=8192):
+    """kvc_rotary_frequencies: radians per position of every pair of channels, a list."""
+    out = (C.c_double * max(rotary_dim // 2, 1))()
+    rc = load().kvc_rotary_frequencies(rotary_dim, base, scaling, factor, low, high, original_tokens, out)
+    if rc != OK:
+        raise KvcError("kvc_rotary_frequencies", rc)
+    return list(out)
+
+
+class PromptPlan:
+    """kvc_prompt_plan / kvc_prompt_plan_free.  eps: heads are normed (None: they are not); frequencies: rotary_dim / 2 numbers, as
+    rotary_frequencies gives them (None: those of base 10000)."""
+
+    def __init__(self, dtype, kv_heads, q_heads, head_dim=128, rotary_dim=128, layout=ROTARY_HALVES, frequencies=None, amplitude=1.0,
+                 eps=None, max_batch=1):
+        if frequencies is None:
+            frequencies = rotary_frequencies(rotary_dim) if rotary_dim else []
+        if len(frequencies) != rotary_dim // 2:
+            raise ValueError("a frequency for each of rotary_dim / 2 pairs")
+        values = (C.c_double * max(len(frequencies), 1))(*frequencies)
+        self.config = PromptConfig(dtype, layout, eps is not None, kv_heads, q_heads, head_dim, rotary_dim, eps or 0.0, amplitude,
+                                   C.cast(values, C.c_void_p))
+        self.max_batch = max_batch
+        self._h = C.c_void_p()
+        rc = load().kvc_prompt_plan(C.byref(self.config), max_batch, C.byref(self._h))
+        self.config.frequencies = None       # (the plan has its own)
+        if rc != OK:
+            raise KvcError("kvc_prompt_plan", rc)
+
+    def __del__(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.kvc_prompt_plan_free(self._h)
+            self._h = None
+
+
+class PromptBatch:
+    """The prompts of a call (kvc_prompt_batch).  start [n + 1]: int32 device tensor; max_rows: host bound of a prompt's rows."""
+
+    def __init__(self, start, max_rows):
+        import torch
+        if start.dtype is not torch.int32 or start.dim() != 1 or start.shape[0] < 1 or not start.is_contiguous():
+            raise ValueError("start is a contiguous int32 tensor [n + 1]")
+        self.keep_alive, self.device = start, start.get_device()
+        self.struct = PromptSequences(start.shape[0] - 1, max_rows, start.data_ptr())
+        self._ref = C.byref(self.struct)
+
+
+class Prompt:
+    """The calls on the heads of a prompt's (kvc_prompt_rotate: any) rows, with their status words.  They take tensors of `device`, a
+    GPU, and go to `stream`, a raw handle (None is the null stream)."""
+
+    def __init__(self, plan, device="cuda"):
+        import torch
+        self.plan = plan
+        self.dtype = torch.float16 if plan.config.dtype == F16 else torch.bfloat16
+        self.status = torch.zeros(plan.max_batch, dtype=torch.int32, device=device)
+        self._device = self.status.get_device() if self.status.is_cuda else None
+        f, lib = plan.config, load()
+        self._kv_heads, self._q_heads, self._dim, self._plan, self._norm = f.kv_heads, f.q_heads, f.head_dim, plan._h, bool(f.norm)
+        self._rotate, self._attend = lib.kvc_prompt_rotate, lib.kvc_prompt_attend
+        if torch.cuda.device_count() > 1:
+            self._rotate, self._attend = (functools.partial(_on_device, self._device, call) for call in (self._rotate, self._attend))
+
+    _layout = Cache._layout
+
+    def rotate(self, q, k, positions, q_out=None, k_out=None, q_weight=None, k_weight=None, stream=None):
+        """kvc_prompt_rotate: q [rows, q_heads, 128], k [rows, kv_heads, 128], either may be None; positions [rows] int32; without q_out
+        or k_out in place."""
+        import torch
+        u, seen = PromptRows(), None
+        for name, x, out, weight, heads in (("q", q, q_out, q_weight, self._q_heads), ("k", k, k_out, k_weight, self._kv_heads)):
+            if x is None:
+                continue
+            out = x if out is None else out
+            rows, strides = self._layout(x, heads)
+            out_rows, out_strides = self._layout(out, heads)
+            if out_rows != rows or seen not in (None, rows):
+                raise ValueError("q, k and their results have the same rows")
+            if self._norm and (weight is None or weight.dtype is not self.dtype or weight.shape != (self._dim,) or not weight.is_contiguous() or
+                               weight.get_device() != self._device):
+                raise ValueError("weights are contiguous tensors [%d] of the plan's type on its device" % self._dim)
+            u.rows = seen = rows
+            setattr(u, name, x.data_ptr())
+            setattr(u, name + "_out", out.data_ptr())
+            setattr(u, name + "_weight", weight.data_ptr() if self._norm else None)
+            for prefix, pair in ((name, strides), (name + "_out", out_strides)):
+                setattr(u, prefix + "_stride_row", pair[0])
+                setattr(u, prefix + "_stride_head", pair[1])
+        if positions is not None:
+            if positions.dtype is not torch.int32 or positions.shape != (u.rows,) or not positions.is_contiguous() or \
+                    positions.get_device() != self._device:
+                raise ValueError("positions are a contiguous int32 tensor [rows]")
+            u.positions = positions.data_ptr()
+        rc = self._rotate(self._plan, u, stream)
+        if rc != OK:
+            raise KvcError("kvc_prompt_rotate", rc)
+
+    def attend(self, batch, q, k, v, out, scale, lse=None, stream=None):
+        """kvc_prompt_attend: q, out [rows, q_heads, 128], k, v [rows, kv_heads, 128]; lse: optional contiguous float32 [rows, q_heads]."""
+        rows, q_strides = self._layout(q, self._q_heads)
+        out_rows, out_strides = self._layout(out, self._q_heads)
+        k_rows, k_strides = self._layout(k, self._kv_heads)
+        v_rows, v_strides = self._layout(v, self._kv_heads)
+        if not rows == out_rows == k_rows == v_rows or batch.device != self._device:
+            raise ValueError("q, k, v and out have the same rows, and the batch is on their device")
+        if lse is not None:
+            import torch
+            if lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.get_device() != self._device:
+                raise ValueError("lse is a contiguous float32 tensor [rows, q_heads]")
+        u = PromptHeads(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, rows,
+                        q_strides[0], q_strides[1], k_strides[0], k_strides[1], v_strides[0], v_strides[1], out_strides[0], out_strides[1], scale)
+        rc = self._attend(self._plan, batch._ref, u, self.status.data_ptr(), stream)
+        if rc != OK:
+            raise KvcError("kvc_prompt_attend", rc)
