@@ -28,7 +28,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 64;                    // tokens of K and V in LDS
-constexpr int kGroup = 32;                   // tokens of a step
+constexpr int kGroup = 32;                   // tokens of a product with values
 constexpr float kSlack = 7.0f, kBias = 8.0f;
 constexpr float kNone = -__builtin_inff();
 constexpr int kSorted = 256;                 // sequences of a call whose blocks are taken longest first
@@ -61,11 +61,17 @@ __device__ __forceinline__ float sum_of_row(float x)
     auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+// The first lane's value, as one that the compiler knows to be the same in all lanes.
+__device__ __forceinline__ long long first_lane(long long x)
+{
+    const uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)x), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32));
+    return (long long)((uint64_t)high << 32 | low);
+}
 __device__ __forceinline__ long long sum_of_wave(long long x)
 {
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m, 64);
-    return x;
+    return first_lane(x);
 }
 
 // ---- which block ------------------------------------------------------------------------------------
@@ -111,6 +117,7 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
                 const int x = __shfl_xor(most, m, 64);
                 most = most > x ? most : x;
             }
+            most = __builtin_amdgcn_readfirstlane(most);
         } else {
             all = __builtin_amdgcn_readfirstlane((int)all);
             most = (int)all;
@@ -167,10 +174,10 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
             if (have && s < 0) {
                 const int l = __ffsll((unsigned long long)have) - 1;
                 s = i + l;
-                at = (int)(before + __shfl(sum, l, 64) - 1 - number);
+                at = __builtin_amdgcn_readfirstlane((int)(before + __shfl(sum, l, 64) - 1 - number));
                 if (blockIdx.x) break;       // (the first workgroup looks at all sequences for its reports)
             }
-            before += __shfl(sum, 63, 64);
+            before += first_lane(__shfl(sum, 63, 64));
         }
         if (s < 0) return false;
         s = __builtin_amdgcn_readfirstlane(s);
@@ -178,9 +185,13 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
         b.rows = __builtin_amdgcn_readfirstlane(rows_of(a, s, row0));
     }
     b.row0 = __builtin_amdgcn_readfirstlane(row0);
-    b.first = at * size;
+    b.first = __builtin_amdgcn_readfirstlane(at) * size;
     return true;
 }
+
+template <bool B> struct BoolConst {
+    static constexpr bool value = B;
+};
 
 // ---- the kernel -----------------------------------------------------------------------------------
 
@@ -201,10 +212,28 @@ template <int DT> __device__ __forceinline__ void only_finite(u32x4 &x, u32x4 &l
     }
 }
 
+// 16 bytes per lane from global memory into the wave's 1 KB of LDS.
+__device__ __forceinline__ void copy_to_lds(const char *from, uint32_t offset, u32x4 *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + offset), (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+// Bytes between the lowest of 16 rows and row `place` of them.
+__device__ __forceinline__ uint32_t lane_offset(int place, long long stride)
+{
+    return (uint32_t)(stride < 0 ? (15 - place) * -2 * stride : place * 2 * stride);
+}
+// Everything that this wave has requested for LDS is there, and everything that the other waves have.
+__device__ __forceinline__ void wait_for_tiles()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) void prompt_kernel(PromptArgs a, long long places)
 {
-    constexpr int kRows = 16 * TILES, kBlock = kRows * kPromptWaves;
-    __shared__ u32x4 keys[kTile * 16], values[kTile * 16];
+    constexpr int kRows = 16 * TILES, kBlock = kRows * kPromptWaves, kPieces = kTile * 16;
+    constexpr int kLoads = kPieces / (64 * kPromptWaves);         // pieces of a tile that a lane brings
+    __shared__ u32x4 keys[2 * kPieces], values[2 * kPieces];
     const int lane = lane_id(), wave = wave_id(), i = lane & 15, g = lane >> 4;
     const int q_heads = a.kv_heads * a.per_kv;
     for (long long place = blockIdx.x;; place += places) {
@@ -218,6 +247,7 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
         const uint16_t *k_at = a.k + (long long)b.row0 * a.k_row + kv * a.k_head;
         const uint16_t *v_at = a.v + (long long)b.row0 * a.v_row + kv * a.v_head;
         const int tokens = b.first + kBlock < b.rows ? b.first + kBlock : b.rows;
+        const int tiles = (tokens + kTile - 1) / kTile;
         u32x4 query[TILES][4];
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
@@ -228,10 +258,158 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
                 query[t][c] = (query[t][c] & a.query_and) ^ a.query_xor;
             }
         }
+        // A tile of keys or values into its half of LDS: the lane's places in LDS are fixed (64 lanes have 1 KB in a row), so the
+        // octets are turned by what each lane asks for.  An address is one of the wave and an offset of the lane's that stays (rows may
+        // descend: offsets count from the lowest of 16).  In place of tokens behind the sequence there is the tile's first, which no row sees.
+        const int place_in = wave * 4 + g;             // (of 16 tokens; lane g * 16 + i brings piece i)
+        const uint32_t key_at = lane_offset(place_in, a.k_row) + 16 * (key_piece(place_in, i) & 15);
+        const uint32_t value_at = lane_offset(place_in, a.v_row) + 16 * (value_piece(place_in, i) & 15);
+        auto bring = [&](u32x4 *room, const uint16_t *from, long long stride, uint32_t lane_at, int n) {
+            if (n >= tiles) return;
+            const char *base = (const char *)(from + (long long)n * kTile * stride) + (stride < 0 ? 30 * stride : 0);
+            const int have = b.rows - n * kTile;
+            u32x4 *to = room + (n & 1) * kPieces + wave * 64;
+            if (have >= kTile) {
+#pragma unroll
+                for (int r = 0; r < kLoads; ++r) {
+                    const char *at = base + 32 * r * stride;
+                    uint32_t lane_has = lane_at;
+                    asm("" : "+s"(at), "+v"(lane_has));  // (a scalar address and the lane's offset, not the lane's sums of both)
+                    copy_to_lds(at, lane_has, to + r * kPromptWaves * 64);
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < kLoads; ++r) {
+                    const char *at = base + (r * 16 + place_in < have ? 32 * r * stride : -2 * place_in * stride);
+                    copy_to_lds(at, lane_at, to + r * kPromptWaves * 64);
+                }
+            }
+        };
         f32x4 out[TILES][8];
         float top[TILES], shift[TILES], sum[TILES];
-        bool again = false;
-        for (;;) {
+        // Tile n.  MIXED: some rows see some of its tokens only, or none.  AGAIN: with values that are not finite taken out where they are
+        // not seen.
+        auto do_tile = [&](int n, auto mixed_tile, auto second_time) {
+            constexpr bool MIXED = decltype(mixed_tile)::value, AGAIN = decltype(second_time)::value;
+            const u32x4 *key_tile = keys + (n & 1) * kPieces, *value_tile = values + (n & 1) * kPieces;
+            const int token = n * kTile;
+            const bool some = !MIXED || (first < b.rows && token < first + kRows), both = !MIXED || token + kGroup < first + kRows;
+            u32x4 weight[2][TILES];
+            if (some) {
+                f32x4 score[4][TILES];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) score[h][t] = f32x4{0, 0, 0, 0};
+                    if (h >= 2 && !both) continue;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const u32x4 key = key_tile[key_piece(16 * h + i, 4 * c + g)];
+#pragma unroll
+                        for (int t = 0; t < TILES; ++t) score[h][t] = multiply<DT>(key, query[t][c], score[h][t]);
+                    }
+                }
+                if (MIXED) {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+#pragma unroll
+                        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (token + 16 * h + 4 * g + e > first + 16 * t + i) score[h][t][e] = kNone;
+                }
+                bool grown = false;
+                float most[TILES];
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    most[t] = score[0][t][0];
+#pragma unroll
+                    for (int e = 1; e < 16; ++e) most[t] = fmaxf(most[t], score[e >> 2][t][e & 3]);
+                    grown |= __builtin_fmaf(most[t], a.factor, -top[t]) > kSlack;
+                }
+                if (__any(grown)) {
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) {
+                        // (rows that have not grown stay as they are: a row's bits depend on what it sees alone)
+                        const float highest = max_of_row(most[t]);
+                        const float now = __builtin_fmaf(highest, a.factor, -top[t]) > kSlack ? highest * a.factor : top[t];
+                        const float from = now == kNone ? 0.0f : now;
+                        const float by = __builtin_amdgcn_exp2f(top[t] - from);
+                        top[t] = now;
+                        shift[t] = kBias - from;
+                        sum[t] *= by;
+#pragma unroll
+                        for (int d = 0; d < 8; ++d) out[t][d] *= by;
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) {
+                        float w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[h][t][e], a.factor, shift[t]));
+                            sum[t] += w[e];
+                        }
+                        weight[h >> 1][t][2 * (h & 1)] = round_pair<DT>(w[0], w[1]);
+                        weight[h >> 1][t][2 * (h & 1) + 1] = round_pair<DT>(w[2], w[3]);
+                    }
+            }
+            wait_for_tiles();                        // this tile's values, the next tile's keys
+            // token 4 g + i / 4 of the lane's 16 (then 16 further), channels 16 d + 4 (i % 4) ... + 3; the lane gets tokens
+            // 4 g ... 4 g + 3 of channel 16 d + i
+            auto value_of = [&](int half, int d) {
+                u32x4 value;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int t = 32 * half + 16 * h + 4 * g + (i >> 2);
+                    const char *from = (const char *)&value_tile[value_piece(t, 2 * d + ((i & 3) >> 1))] + 8 * (i & 1);
+                    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4 *)from));
+                    value[2 * h] = x[0];
+                    value[2 * h + 1] = x[1];
+                }
+                return value;
+            };
+            if (some) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (half && !both) continue;
+                    u32x4 seen[TILES];
+                    if (MIXED && AGAIN) {
+                        constexpr uint32_t one = DT == DT_F16 ? 0x3c00u : 0x3f80u;
+#pragma unroll
+                        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int behind = first + 16 * t + i - (token + 32 * half + 16 * (e >> 1) + 4 * g + 2 * (e & 1));
+                                seen[t][e] = (behind >= 0 ? one : 0u) | (behind >= 1 ? one << 16 : 0u);
+                            }
+                    }
+#pragma unroll
+                    for (int d = 0; d < 8; ++d) {
+                        u32x4 value = value_of(half, d), lost;
+                        if (MIXED && AGAIN) only_finite<DT>(value, lost);
+#pragma unroll
+                        for (int t = 0; t < TILES; ++t) {
+                            if (MIXED && AGAIN) {
+                                const f32x4 count = multiply<DT>(lost, seen[t], f32x4{0, 0, 0, 0});
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if (count[e] > 0.0f) out[t][d][e] = __builtin_nanf("");
+                            }
+                            out[t][d] = multiply<DT>(value, weight[half][t], out[t][d]);
+                        }
+                    }
+                }
+            }
+            // Behind the tile's last transposing load, for which the compiler waits until nothing is on its way to LDS: on their way during
+            // the next tile's scores.  Both halves' last readers have passed the barrier above.
+            bring(values, v_at, a.v_row, value_at, n + 1);
+            bring(keys, k_at, a.k_row, key_at, n + 2);
+        };
+        auto do_tiles = [&](auto second_time) {
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 top[t] = kNone;
@@ -240,121 +418,13 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
 #pragma unroll
                 for (int d = 0; d < 8; ++d) out[t][d] = f32x4{0, 0, 0, 0};
             }
-            for (int at = 0; at < tokens; at += kTile) {
-                __syncthreads();
-#pragma unroll
-                for (int r = 0; r < kTile * 16 / (64 * kPromptWaves); ++r) {
-                    const int piece = r * 64 * kPromptWaves + threadIdx.x, token = piece >> 4, c = piece & 15;
-                    u32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-                    if (at + token < b.rows) {
-                        x = *(const u32x4 *)(k_at + (long long)(at + token) * a.k_row + 8 * c);
-                        y = *(const u32x4 *)(v_at + (long long)(at + token) * a.v_row + 8 * c);
-                    }
-                    keys[key_piece(token, c)] = x;
-                    values[value_piece(token, c)] = y;
-                }
-                __syncthreads();
-                for (int step = 0; step < kTile; step += kGroup) {
-                    const int token = at + step;
-                    if (first >= b.rows || token >= first + kRows) break;
-                    const bool mixed = token + kGroup - 1 > first;           // some rows see some of the tokens only
-                    float score[TILES][8];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        f32x4 s[TILES];
-#pragma unroll
-                        for (int t = 0; t < TILES; ++t) s[t] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const u32x4 key = keys[key_piece(step + 16 * h + i, 4 * c + g)];
-#pragma unroll
-                            for (int t = 0; t < TILES; ++t) s[t] = multiply<DT>(key, query[t][c], s[t]);
-                        }
-#pragma unroll
-                        for (int t = 0; t < TILES; ++t)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) score[t][4 * h + e] = s[t][e];
-                    }
-                    if (mixed) {
-#pragma unroll
-                        for (int t = 0; t < TILES; ++t)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (token + 16 * (e >> 2) + 4 * g + (e & 3) > first + 16 * t + i) score[t][e] = kNone;
-                    }
-                    bool grown = false;
-                    float most[TILES];
-#pragma unroll
-                    for (int t = 0; t < TILES; ++t) {
-                        most[t] = score[t][0];
-#pragma unroll
-                        for (int e = 1; e < 8; ++e) most[t] = fmaxf(most[t], score[t][e]);
-                        grown |= __builtin_fmaf(most[t], a.factor, -top[t]) > kSlack;
-                    }
-                    if (__any(grown)) {
-#pragma unroll
-                        for (int t = 0; t < TILES; ++t) {
-                            // (rows that have not grown stay as they are: a row's bits depend on what it sees alone)
-                            const float highest = max_of_row(most[t]);
-                            const float now = __builtin_fmaf(highest, a.factor, -top[t]) > kSlack ? highest * a.factor : top[t];
-                            const float from = now == kNone ? 0.0f : now;
-                            const float by = __builtin_amdgcn_exp2f(top[t] - from);
-                            top[t] = now;
-                            shift[t] = kBias - from;
-                            sum[t] *= by;
-#pragma unroll
-                            for (int d = 0; d < 8; ++d) out[t][d] *= by;
-                        }
-                    }
-                    u32x4 weight[TILES];
-#pragma unroll
-                    for (int t = 0; t < TILES; ++t) {
-                        float w[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[t][e], a.factor, shift[t]));
-                            sum[t] += w[e];
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) weight[t][e] = round_pair<DT>(w[2 * e], w[2 * e + 1]);
-                    }
-#pragma unroll
-                    for (int d = 0; d < 8; ++d) {
-                        // token 4 g + i / 4 of the lane's 16 (then 16 further), channels 16 d + 4 (i % 4) ... + 3; the lane gets tokens
-                        // 4 g ... 4 g + 3 of channel 16 d + i
-                        u32x4 value;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int t = step + 16 * h + 4 * g + (i >> 2);
-                            const char *from = (const char *)&values[value_piece(t, 2 * d + ((i & 3) >> 1))] + 8 * (i & 1);
-                            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (__attribute__((address_space(3))) s16x4 *)from));
-                            value[2 * h] = x[0];
-                            value[2 * h + 1] = x[1];
-                        }
-                        if (mixed && again) {
-                            u32x4 lost;
-                            only_finite<DT>(value, lost);
-#pragma unroll
-                            for (int t = 0; t < TILES; ++t) {
-                                u32x4 seen;
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const int behind = first + 16 * t + i - (token + 16 * (e >> 1) + 4 * g + 2 * (e & 1));
-                                    constexpr uint32_t one = DT == DT_F16 ? 0x3c00u : 0x3f80u;
-                                    seen[e] = (behind >= 0 ? one : 0u) | (behind >= 1 ? one << 16 : 0u);
-                                }
-                                const f32x4 count = multiply<DT>(lost, seen, f32x4{0, 0, 0, 0});
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if (count[e] > 0.0f) out[t][d][e] = __builtin_nanf("");
-                            }
-                        }
-#pragma unroll
-                        for (int t = 0; t < TILES; ++t) out[t][d] = multiply<DT>(value, weight[t], out[t][d]);
-                    }
-                }
-            }
+            bring(keys, k_at, a.k_row, key_at, 0);
+            wait_for_tiles();
+            bring(values, v_at, a.v_row, value_at, 0);
+            bring(keys, k_at, a.k_row, key_at, 1);
+            const int whole = b.first / kTile;       // tiles of which all rows see all tokens
+            for (int n = 0; n < whole; ++n) do_tile(n, BoolConst<false>(), second_time);
+            for (int n = whole; n < tiles; ++n) do_tile(n, BoolConst<true>(), second_time);
             bool finite = true;
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
@@ -362,10 +432,10 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
                 for (int d = 0; d < 8; ++d)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) finite &= out[t][d][e] - out[t][d][e] == 0.0f;
-            finite |= first >= b.rows;
-            if (again || !__syncthreads_or(!finite)) break;
-            again = true;
-        }
+            return finite || first >= b.rows;
+        };
+        const bool finite = do_tiles(BoolConst<false>());
+        if (__builtin_amdgcn_readfirstlane(__syncthreads_or(!finite))) do_tiles(BoolConst<true>());
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             const int row = first + 16 * t + i;
@@ -386,7 +456,10 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
 PromptShape prompt_shape(const PromptArgs &a)
 {
     PromptShape s;
-    s.tiles = 2;
+#ifndef RT
+#define RT 2
+#endif
+    s.tiles = RT;
     const long long size = 16 * s.tiles * kPromptWaves, each = (a.max_rows + size - 1) / size;
     // blocks of all sequences: no more than what their number and bound allow, or their rows in all
     long long blocks = each * a.n, most = a.rows / size + a.n;
@@ -399,7 +472,7 @@ PromptShape prompt_shape(const PromptArgs &a)
 
 template <int DT> static void launch_type(const PromptArgs &a, const PromptShape &s, hipStream_t stream)
 {
-    prompt_kernel<DT, 2><<<dim3((unsigned)s.places), 64 * kPromptWaves, 0, stream>>>(a, s.places);
+    prompt_kernel<DT, RT><<<dim3((unsigned)s.places), 64 * kPromptWaves, 0, stream>>>(a, s.places);
 }
 void launch_prompt(int dtype, const PromptArgs &a, const PromptShape &s, hipStream_t stream)
 {
