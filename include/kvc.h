@@ -579,7 +579,7 @@ typedef struct {
     const int32_t *start;                /* DEVICE, n + 1 */
 } kvc_prompt_batch;
 
-/* Queries, keys, values and results of `rows` rows; strides are multiples of 8.  lse: optional, [rows][q_heads].  out may be q itself, with
+/* Queries, keys, values and results of `rows` rows, up to 2^28; strides are multiples of 8, those between rows of k and v 0 to 2^24.  lse: optional, [rows][q_heads].  out may be q itself, with
  * the same strides. */
 typedef struct {
     const void *q, *k, *v;               /* DEVICE */

@@ -15,6 +15,9 @@ namespace kvc {
 
 constexpr long double kTwoPi = 6.283185307179586476925286766559L;
 
+constexpr int64_t kMostStride = 1 << 24;      // of rows of K and V, in elements
+constexpr int64_t kMostRows = 1 << 28;        // of an attention
+
 static bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 static bool strides_ok(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
 
@@ -123,7 +126,7 @@ extern "C" int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt
     const kvc_prompt_config &f = plan->config;
     const kvc_prompt_heads &h = *heads;
     if (batch->n < 0 || batch->max_rows < 0 || h.rows < 0) return KVC_ERR_ARG;
-    if (batch->n > plan->max_batch || h.rows > 0x7fffffffll) return KVC_ERR_CAPACITY;
+    if (batch->n > plan->max_batch || h.rows > kMostRows) return KVC_ERR_CAPACITY;
     if (batch->n == 0 || batch->max_rows == 0) return KVC_OK;
     if (!batch->start || !dev_status || (h.rows && (!h.q || !h.k || !h.v || !h.out))) return KVC_ERR_ARG;
     if (!aligned(batch->start, 4) || !aligned(dev_status, 4) || !aligned(h.q, 16) || !aligned(h.k, 16) || !aligned(h.v, 16) || !aligned(h.out, 16) ||
@@ -131,6 +134,8 @@ extern "C" int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt
     if (!strides_ok(h.q_stride_row, h.q_stride_head) || !strides_ok(h.k_stride_row, h.k_stride_head) ||
         !strides_ok(h.v_stride_row, h.v_stride_head) || !strides_ok(h.out_stride_row, h.out_stride_head)) return KVC_ERR_ARG;
     if (!(h.scale >= -1e38f && h.scale <= 1e38f)) return KVC_ERR_ARG;
+    // (offsets of the 64 rows of a tile are 32-bit numbers above zero)
+    if (h.k_stride_row < 0 || h.v_stride_row < 0 || h.k_stride_row > kMostStride || h.v_stride_row > kMostStride) return KVC_ERR_UNSUPPORTED;
     PromptArgs a = {};
     a.q = (const uint16_t *)h.q;
     a.k = (const uint16_t *)h.k;

@@ -67,11 +67,17 @@ __device__ __forceinline__ long long first_lane(long long x)
     const uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)x), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32));
     return (long long)((uint64_t)high << 32 | low);
 }
-__device__ __forceinline__ long long sum_of_wave(long long x)
+template <int N> __device__ __forceinline__ int turned_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, 0x120 + N, 0xf, 0xf, true); }
+__device__ __forceinline__ int sum_of_wave(int x)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m, 64);
-    return first_lane(x);
+    x += turned_lane<8>(x);
+    x += turned_lane<4>(x);
+    x += turned_lane<2>(x);
+    x += turned_lane<1>(x);
+    auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = (int)(a[0] + a[1]);
+    auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return __builtin_amdgcn_readfirstlane((int)(b[0] + b[1]));
 }
 
 // ---- which block ------------------------------------------------------------------------------------
@@ -98,94 +104,80 @@ __device__ __forceinline__ int rows_of(const PromptArgs &a, int s, int &row0)
 __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number, int size, Block &b)
 {
     const int lane = lane_id();
-    int at, row0;
+    if (a.n == 1) {
+        b.rows = __builtin_amdgcn_readfirstlane(rows_of(a, 0, b.row0));
+        b.row0 = __builtin_amdgcn_readfirstlane(b.row0);
+        b.all = (unsigned)(b.rows + size - 1) / (unsigned)size;
+        b.first = (int)(b.all - 1 - number) * size;
+        return number < b.all;
+    }
     if (a.n <= kSorted) {
-        int blocks[kSorted / 64];
-        long long all = 0;
-        int most = 0;
+        constexpr int kEach = kSorted / 64;
+        int blocks[kEach], rows[kEach], row0[kEach], all = 0;
 #pragma unroll
-        for (int i = 0; i < kSorted / 64; ++i) {
+        for (int i = 0; i < kEach; ++i) {
             const int s = 64 * i + lane;
-            blocks[i] = s < a.n ? (int)(((unsigned)rows_of(a, s, row0) + size - 1) / size) : 0;
+            rows[i] = row0[i] = 0;
+            if (s < a.n) rows[i] = rows_of(a, s, row0[i]);
+            blocks[i] = (int)((unsigned)(rows[i] + size - 1) / (unsigned)size);
             all += blocks[i];
-            most = most > blocks[i] ? most : blocks[i];
         }
-        if (a.n > 1) {
-            all = sum_of_wave(all);
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const int x = __shfl_xor(most, m, 64);
-                most = most > x ? most : x;
-            }
-            most = __builtin_amdgcn_readfirstlane(most);
-        } else {
-            all = __builtin_amdgcn_readfirstlane((int)all);
-            most = (int)all;
-        }
+        all = sum_of_wave(all);
         b.all = all;
         if (number >= all) return false;
         // the highest level (blocks before it in its sequence) at and above which there are more than `number` blocks
-        int low = 0, high = most;            // (low: more than `number`; high: no more)
-        long long above = 0;                 // blocks at and above `high`
-        if (a.n == 1) {
-            low = most - 1 - (int)number;
-            above = number;
-        }
-        while (a.n > 1 && high - low > 1) {
-            const int mid = (low + high) >> 1;
-            long long sum = 0;
+        int low = 0, above = 0;              // (low: more than `number`; the next that was tried: `above`, which is no more)
+        for (int step = 1 << (31 - __builtin_clz(((unsigned)a.max_rows + size - 1) / size | 1u)); step; step >>= 1) {
+            const int level = low + step;
+            int sum = 0;
 #pragma unroll
-            for (int i = 0; i < kSorted / 64; ++i) sum += blocks[i] > mid ? blocks[i] - mid : 0;
+            for (int i = 0; i < kEach; ++i) sum += blocks[i] > level ? blocks[i] - level : 0;
             sum = sum_of_wave(sum);
-            if (sum > number) low = mid;
-            else {
-                high = mid;
-                above = sum;
-            }
+            if (sum > number) low = level;
+            else above = sum;
         }
-        // the (number - above)-th sequence that has a block at this level
-        int left = (int)(number - above), s = 0;
+        // Of the last level tried above `low` no more than `number` blocks are there; the sequences that have one at `low`, in their order:
+        int left = (int)number - above;
+        b.first = low * size;
+        b.row0 = b.rows = 0;
 #pragma unroll
-        for (int i = 0; i < kSorted / 64; ++i) {
+        for (int i = 0; i < kEach; ++i) {
             unsigned long long have = __ballot(blocks[i] > low);
             const int many = __popcll(have);
             if (left >= 0 && left < many) {
                 for (int k = 0; k < left; ++k) have &= have - 1;
-                s = 64 * i + __ffsll((unsigned long long)have) - 1;
+                const int l = __ffsll(have) - 1;
+                b.row0 = __builtin_amdgcn_readlane(row0[i], l);
+                b.rows = __builtin_amdgcn_readlane(rows[i], l);
             }
             left -= many;
         }
-        s = __builtin_amdgcn_readfirstlane(s);
-        b.rows = __builtin_amdgcn_readfirstlane(rows_of(a, s, row0));
-        at = low;
-    } else {
-        b.all = INT64_MAX / 65536;
-        int s = -1, mine = 0;
-        long long before = 0;
-        for (int i = 0; i < a.n; i += 64) {
-            mine = i + lane < a.n ? (int)(((unsigned)rows_of(a, i + lane, row0) + size - 1) / size) : 0;
-            long long sum = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const long long up = __shfl_up(sum, d, 64);
-                if (lane >= d) sum += up;
-            }
-            const unsigned long long have = __ballot(before + sum > number);
-            if (have && s < 0) {
-                const int l = __ffsll((unsigned long long)have) - 1;
-                s = i + l;
-                at = __builtin_amdgcn_readfirstlane((int)(before + __shfl(sum, l, 64) - 1 - number));
-                if (blockIdx.x) break;       // (the first workgroup looks at all sequences for its reports)
-            }
-            before += first_lane(__shfl(sum, 63, 64));
-        }
-        if (s < 0) return false;
-        s = __builtin_amdgcn_readfirstlane(s);
-        at = __builtin_amdgcn_readfirstlane(at);
-        b.rows = __builtin_amdgcn_readfirstlane(rows_of(a, s, row0));
+        return true;
     }
+    b.all = INT64_MAX / 65536;
+    int s = -1, at = 0, row0;
+    long long before = 0;
+    for (int i = 0; i < a.n; i += 64) {
+        const int mine = i + lane < a.n ? (int)((unsigned)(rows_of(a, i + lane, row0) + size - 1) / (unsigned)size) : 0;
+        long long sum = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const long long up = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += up;
+        }
+        const unsigned long long have = __ballot(before + sum > number);
+        if (have && s < 0) {
+            const int l = __ffsll(have) - 1;
+            s = i + l;
+            at = __builtin_amdgcn_readfirstlane((int)(before + __shfl(sum, l, 64) - 1 - number));
+            if (blockIdx.x) break;           // (the first workgroup looks at all sequences for its reports)
+        }
+        before += first_lane(__shfl(sum, 63, 64));
+    }
+    if (s < 0) return false;
+    b.rows = __builtin_amdgcn_readfirstlane(rows_of(a, s, row0));
     b.row0 = __builtin_amdgcn_readfirstlane(row0);
-    b.first = __builtin_amdgcn_readfirstlane(at) * size;
+    b.first = at * size;
     return true;
 }
 
@@ -212,15 +204,19 @@ template <int DT> __device__ __forceinline__ void only_finite(u32x4 &x, u32x4 &l
     }
 }
 
-// 16 bytes per lane from global memory into the wave's 1 KB of LDS.
-__device__ __forceinline__ void copy_to_lds(const char *from, uint32_t offset, u32x4 *to)
+// A value that nothing computed from it is moved away from: what a loop needs is made in front of that loop and not held through another.
+__device__ __forceinline__ int here_only(int x)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + offset), (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+    asm volatile("" : "+v"(x));
+    return x;
 }
-// Bytes between the lowest of 16 rows and row `place` of them.
-__device__ __forceinline__ uint32_t lane_offset(int place, long long stride)
+#define in_lds __attribute__((address_space(3)))
+__device__ __forceinline__ uint32_t lds_address(const u32x4 *x) { return (uint32_t)(uintptr_t)(const in_lds u32x4 *)x; }
+// 16 bytes per lane from global memory into the wave's 1 KB of LDS.  (Written out: for the builtin the compiler waits until nothing is on its way
+// to LDS before every transposing load.  There is no register that the load would write; wait_for_tiles waits.)
+__device__ __forceinline__ void copy_to_lds(const char *from, uint32_t offset, uint32_t to)
 {
-    return (uint32_t)(stride < 0 ? (15 - place) * -2 * stride : place * 2 * stride);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(from) : "memory");
 }
 // Everything that this wave has requested for LDS is there, and everything that the other waves have.
 __device__ __forceinline__ void wait_for_tiles()
@@ -233,15 +229,25 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
 {
     constexpr int kRows = 16 * TILES, kBlock = kRows * kPromptWaves, kPieces = kTile * 16;
     constexpr int kLoads = kPieces / (64 * kPromptWaves);         // pieces of a tile that a lane brings
-    __shared__ u32x4 keys[2 * kPieces], values[2 * kPieces];
+    __shared__ __attribute__((aligned(256))) u32x4 keys[2 * kPieces], values[2 * kPieces];
     const int lane = lane_id(), wave = wave_id(), i = lane & 15, g = lane >> 4;
     const int q_heads = a.kv_heads * a.per_kv;
     for (long long place = blockIdx.x;; place += places) {
         // neighbouring workgroups, which run on different XCDs, have different KV heads; those of one KV head meet in an L2
-        const int kv = (int)(place % a.kv_heads);
-        const int head = kv * a.per_kv + (int)(place / a.kv_heads % a.per_kv);
+        int kv, head;
+        long long number;
+        if (place >> 32) {
+            kv = (int)(place % a.kv_heads);
+            head = kv * a.per_kv + (int)(place / a.kv_heads % a.per_kv);
+            number = place / q_heads;
+        } else {                             // (a division of 64-bit numbers takes ten times as long)
+            const unsigned low = (unsigned)place, rest = low / (unsigned)a.kv_heads;
+            number = rest / (unsigned)a.per_kv;
+            kv = (int)(low - rest * (unsigned)a.kv_heads);
+            head = kv * a.per_kv + (int)(rest - (unsigned)number * (unsigned)a.per_kv);
+        }
         Block b;
-        if (!find_block(a, place / q_heads, kBlock, b)) return;
+        if (!find_block(a, number, kBlock, b)) return;
         const int first = b.first + wave * kRows;                  // of the wave
         const uint16_t *q_at = a.q + (long long)b.row0 * a.q_row + head * a.q_head;
         const uint16_t *k_at = a.k + (long long)b.row0 * a.k_row + kv * a.k_head;
@@ -259,29 +265,25 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
             }
         }
         // A tile of keys or values into its half of LDS: the lane's places in LDS are fixed (64 lanes have 1 KB in a row), so the
-        // octets are turned by what each lane asks for.  An address is one of the wave and an offset of the lane's that stays (rows may
-        // descend: offsets count from the lowest of 16).  In place of tokens behind the sequence there is the tile's first, which no row sees.
+        // octets are turned by what each lane asks for.  An address is one of the wave and an offset of the lane's that stays.  In place of
+        // tokens behind the sequence there is the tile's first, which no row sees.
         const int place_in = wave * 4 + g;             // (of 16 tokens; lane g * 16 + i brings piece i)
-        const uint32_t key_at = lane_offset(place_in, a.k_row) + 16 * (key_piece(place_in, i) & 15);
-        const uint32_t value_at = lane_offset(place_in, a.v_row) + 16 * (value_piece(place_in, i) & 15);
+        const uint32_t key_at = place_in * 2 * (uint32_t)a.k_row + 16 * (key_piece(place_in, i) & 15);
+        const uint32_t value_at = place_in * 2 * (uint32_t)a.v_row + 16 * (value_piece(place_in, i) & 15);
         auto bring = [&](u32x4 *room, const uint16_t *from, long long stride, uint32_t lane_at, int n) {
             if (n >= tiles) return;
-            const char *base = (const char *)(from + (long long)n * kTile * stride) + (stride < 0 ? 30 * stride : 0);
+            const char *base = (const char *)(from + (long long)n * kTile * stride);
             const int have = b.rows - n * kTile;
-            u32x4 *to = room + (n & 1) * kPieces + wave * 64;
+            const uint32_t to = lds_address(room + (n & 1) * kPieces + wave * 64);
             if (have >= kTile) {
 #pragma unroll
-                for (int r = 0; r < kLoads; ++r) {
-                    const char *at = base + 32 * r * stride;
-                    uint32_t lane_has = lane_at;
-                    asm("" : "+s"(at), "+v"(lane_has));  // (a scalar address and the lane's offset, not the lane's sums of both)
-                    copy_to_lds(at, lane_has, to + r * kPromptWaves * 64);
-                }
+                for (int r = 0; r < kLoads; ++r) copy_to_lds(base + 32 * r * stride, lane_at, to + r * kPromptWaves * 1024);
             } else {
+                const uint32_t own = here_only(place_in), step = 32 * (uint32_t)stride;
 #pragma unroll
                 for (int r = 0; r < kLoads; ++r) {
-                    const char *at = base + (r * 16 + place_in < have ? 32 * r * stride : -2 * place_in * stride);
-                    copy_to_lds(at, lane_at, to + r * kPromptWaves * 64);
+                    const bool there = (int)own < have - r * 16;
+                    copy_to_lds(base, there ? lane_at + r * step : lane_at - own * 2 * (uint32_t)stride, to + r * kPromptWaves * 1024);
                 }
             }
         };
@@ -289,9 +291,13 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
         float top[TILES], shift[TILES], sum[TILES];
         // Tile n.  MIXED: some rows see some of its tokens only, or none.  AGAIN: with values that are not finite taken out where they are
         // not seen.
-        auto do_tile = [&](int n, auto mixed_tile, auto second_time) {
+        auto do_tile = [&](int n, int lane, auto mixed_tile, auto second_time) {
+            const int i = lane & 15, g = lane >> 4;
             constexpr bool MIXED = decltype(mixed_tile)::value, AGAIN = decltype(second_time)::value;
-            const u32x4 *key_tile = keys + (n & 1) * kPieces, *value_tile = values + (n & 1) * kPieces;
+            // (turning an octet by a token's number is an exclusive or, and the tiles lie at multiples of their rows: all octets' addresses
+            // are the first one's and an exclusive or with a constant)
+            const uint32_t key_lane = lds_address(keys + (n & 1) * kPieces) + 16 * key_piece(i, g);
+            const uint32_t value_lane = lds_address(values + (n & 1) * kPieces) + 16 * value_piece(4 * g + (i >> 2), (i & 3) >> 1) + 8 * (i & 1);
             const int token = n * kTile;
             const bool some = !MIXED || (first < b.rows && token < first + kRows), both = !MIXED || token + kGroup < first + kRows;
             u32x4 weight[2][TILES];
@@ -304,7 +310,7 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
                     if (h >= 2 && !both) continue;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const u32x4 key = key_tile[key_piece(16 * h + i, 4 * c + g)];
+                        const u32x4 key = *(const in_lds u32x4 *)(uintptr_t)((key_lane ^ 64 * c) + 4096 * h);       // token 16 h + i, octet 4 c + g
 #pragma unroll
                         for (int t = 0; t < TILES; ++t) score[h][t] = multiply<DT>(key, query[t][c], score[h][t]);
                     }
@@ -356,17 +362,20 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
                         weight[h >> 1][t][2 * (h & 1) + 1] = round_pair<DT>(w[2], w[3]);
                     }
             }
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) asm volatile("" : "+v"(sum[t]));   // (added up here, not held apart until the products are done)
             wait_for_tiles();                        // this tile's values, the next tile's keys
+            // (what the next ones overwrite has no readers behind the barrier: this tile's keys, the last tile's values)
+            bring(values, v_at, a.v_row, value_at, n + 1);
+            bring(keys, k_at, a.k_row, key_at, n + 2);
             // token 4 g + i / 4 of the lane's 16 (then 16 further), channels 16 d + 4 (i % 4) ... + 3; the lane gets tokens
             // 4 g ... 4 g + 3 of channel 16 d + i
             auto value_of = [&](int half, int d) {
                 u32x4 value;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int t = 32 * half + 16 * h + 4 * g + (i >> 2);
-                    const char *from = (const char *)&value_tile[value_piece(t, 2 * d + ((i & 3) >> 1))] + 8 * (i & 1);
                     const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4 *)from));
+                        (in_lds s16x4 *)(uintptr_t)((value_lane ^ 32 * d) + 8192 * half + 4096 * h)));
                     value[2 * h] = x[0];
                     value[2 * h + 1] = x[1];
                 }
@@ -404,10 +413,6 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
                     }
                 }
             }
-            // Behind the tile's last transposing load, for which the compiler waits until nothing is on its way to LDS: on their way during
-            // the next tile's scores.  Both halves' last readers have passed the barrier above.
-            bring(values, v_at, a.v_row, value_at, n + 1);
-            bring(keys, k_at, a.k_row, key_at, n + 2);
         };
         auto do_tiles = [&](auto second_time) {
 #pragma unroll
@@ -423,8 +428,10 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
             bring(values, v_at, a.v_row, value_at, 0);
             bring(keys, k_at, a.k_row, key_at, 1);
             const int whole = b.first / kTile;       // tiles of which all rows see all tokens
-            for (int n = 0; n < whole; ++n) do_tile(n, BoolConst<false>(), second_time);
-            for (int n = whole; n < tiles; ++n) do_tile(n, BoolConst<true>(), second_time);
+            const int for_whole = here_only(lane);
+            for (int n = 0; n < whole; ++n) do_tile(n, for_whole, BoolConst<false>(), second_time);
+            const int for_mixed = here_only(lane);
+            for (int n = whole; n < tiles; ++n) do_tile(n, for_mixed, BoolConst<true>(), second_time);
             bool finite = true;
 #pragma unroll
             for (int t = 0; t < TILES; ++t)

@@ -133,10 +133,12 @@ def test_attention_refused(lib):
                dict(q_stride_row=1), dict(k_stride_head=12), dict(v_stride_row=2), dict(out_stride_head=4), dict(scale=math.nan),
                dict(scale=math.inf), dict(scale=-2e38)]:
         assert call(**kw) == -1, kw
-    assert call(n=4) == -3 and call(rows=1 << 31) == -3
+    assert call(n=4) == -3 and call(rows=(1 << 28) + 1) == -3
+    for kw in [dict(k_stride_row=-256), dict(v_stride_row=-8), dict(k_stride_row=(1 << 24) + 8), dict(v_stride_row=1 << 40)]:
+        assert call(**kw) == -2, kw
     assert call(n=0, start=None) == 0 and call(max_rows=0, q=None) == 0
     if not torch.cuda.is_available():
-        assert call() == -6 and call(scale=0.0, lse=AT + 4) == -6 and call(rows=0, q=None, k=None, v=None, out=None) == -6
+        assert call() == -6 and call(scale=0.0, lse=AT + 4) == -6 and call(k_stride_row=0, v_stride_row=1 << 24, q_stride_row=-1024) == -6 and call(rows=0, q=None, k=None, v=None, out=None) == -6
 
 
 def test_advance_refused(lib):
