@@ -560,6 +560,14 @@ int kvc_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, dou
 int kvc_prompt_plan(const kvc_prompt_config *config, int32_t max_batch, kvc_prompt_plan_t **out);
 void kvc_prompt_plan_free(kvc_prompt_plan_t *plan);
 
+/*
+ * Rows that a workgroup of kvc_prompt_attend has in a call with these bounds (`rows` of the tensors): 64, 128 or 192, the size for which the time
+ * of such a call is estimated to be the least; *waves (or NULL): 4, or 8 where two sets of waves share them; 0 where there is nothing to do or the
+ * call is refused.  The lengths are on the device, so max_rows stands for them: with a bound far above the lengths blocks are taken that are
+ * large for the call (64 prompts of 100 tokens, 32 heads: 42 us with blocks of 64, 61 with 192).
+ */
+int32_t kvc_prompt_block_rows(const kvc_prompt_plan_t *plan, int32_t n, int32_t max_rows, int64_t rows, int32_t *waves);
+
 /* Queries and keys of `rows` rows.  Element d of head h of row r at q + r * q_stride_row + h * q_stride_head + d; strides are multiples of
  * 8.  q or k may be NULL (the other alone), and q_out = q, k_out = k with the same strides. */
 typedef struct {
@@ -597,7 +605,7 @@ typedef struct {
  *                       are held in 32 bits, weights enter the second product in the type (one rounding).  Rows of no sequence are left
  *                       as they are.  What a row does not see has no influence, whatever it holds; a row that sees a NaN, or an infinity
  *                       that its result depends on, has no finite result there (NaN or an infinity).  dev_status: n words, bits are OR-ed in.  Equal
- *                       inputs give equal bits
+ *                       inputs and bounds give equal bits
  */
 int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt_rows *rows, void *hip_stream);
 int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt_batch *batch, const kvc_prompt_heads *heads, int32_t *dev_status,

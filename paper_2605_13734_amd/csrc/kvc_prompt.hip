@@ -77,7 +77,7 @@ extern "C" int kvc_prompt_plan(const kvc_prompt_config *config, int32_t max_batc
     if (f.rotary_dim && !(f.amplitude > 0.0f && f.amplitude <= 1e30f)) return KVC_ERR_ARG;
     for (int i = 0; i < f.rotary_dim / 2; ++i)
         if (!(f.frequencies[i] >= -1e9 && f.frequencies[i] <= 1e9)) return KVC_ERR_ARG;
-    if (f.head_dim != kDim || f.rotary_dim % 16 || f.q_heads > 65536 || max_batch > 65535) return KVC_ERR_UNSUPPORTED;
+    if (f.head_dim != kDim || f.rotary_dim % 16 || f.q_heads > 65535 || max_batch > 65535) return KVC_ERR_UNSUPPORTED;
     kvc_prompt_plan_t *p = new (std::nothrow) kvc_prompt_plan_t();
     if (!p) return KVC_ERR_CAPACITY;
     p->config = f;
@@ -116,6 +116,23 @@ extern "C" int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt
     for (int i = 0; i < a.pairs; ++i) a.turns[i] = plan->turns[i];
     launch_rotate(f.dtype, f.layout == KVC_ROTARY_PAIRS, f.norm != 0, a, (hipStream_t)hip_stream);
     return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
+}
+
+extern "C" int32_t kvc_prompt_block_rows(const kvc_prompt_plan_t *plan, int32_t n, int32_t max_rows, int64_t rows, int32_t *waves)
+{
+    using namespace kvc;
+    if (waves) *waves = 0;
+    if (!plan || n < 1 || max_rows < 1 || rows < 1 || n > plan->max_batch || rows > kMostRows) return 0;
+    PromptArgs a = {};
+    a.n = n;
+    a.max_rows = max_rows;
+    a.rows = rows;
+    a.kv_heads = plan->config.kv_heads;
+    a.per_kv = plan->config.q_heads / plan->config.kv_heads;
+    int many;
+    const int block = prompt_block_rows(a, many);
+    if (waves) *waves = many;
+    return block;
 }
 
 extern "C" int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt_batch *batch, const kvc_prompt_heads *heads,
@@ -157,6 +174,6 @@ extern "C" int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt
     a.max_rows = batch->max_rows;
     a.kv_heads = f.kv_heads;
     a.per_kv = f.q_heads / f.kv_heads;
-    launch_prompt(f.dtype, a, prompt_shape(a), (hipStream_t)hip_stream);
+    launch_prompt(f.dtype, a, (hipStream_t)hip_stream);
     return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
 }

@@ -17,6 +17,8 @@
 #include "kvc_prompt_internal.h"
 #include "../../include/kvc.h"
 
+#include <math.h>
+
 namespace kvc {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -27,7 +29,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTile = 64;                    // tokens of K and V in LDS
 constexpr int kGroup = 32;                   // tokens of a product with values
 constexpr float kSlack = 7.0f, kBias = 8.0f;
 constexpr float kNone = -__builtin_inff();
@@ -88,13 +89,15 @@ struct Block {
     long long all;                           // blocks of the call, where that is known
 };
 
+// The workgroup that reports.
+__device__ __forceinline__ bool first_group() { return blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0; }
 // Rows of sequence s, none where its numbers do not fit (reported).
 __device__ __forceinline__ int rows_of(const PromptArgs &a, int s, int &row0)
 {
     row0 = a.start[s];
     const int rows = (int)((unsigned)a.start[s + 1] - (unsigned)row0);
     if (row0 >= 0 && (unsigned)rows <= (unsigned)a.max_rows && (long long)row0 + rows <= a.rows) return rows;
-    if (blockIdx.x == 0 && threadIdx.x < 64) atomicOr(a.status + s, KVC_DEV_BAD_ROW);
+    if (first_group() && threadIdx.x < 64) atomicOr(a.status + s, KVC_DEV_BAD_ROW);
     return 0;
 }
 
@@ -117,7 +120,8 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int s = 64 * i + lane;
-            rows[i] = row0[i] = 0;
+            blocks[i] = rows[i] = row0[i] = 0;
+            if (64 * i >= a.n) continue;
             if (s < a.n) rows[i] = rows_of(a, s, row0[i]);
             blocks[i] = (int)((unsigned)(rows[i] + size - 1) / (unsigned)size);
             all += blocks[i];
@@ -170,7 +174,7 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
             const int l = __ffsll(have) - 1;
             s = i + l;
             at = __builtin_amdgcn_readfirstlane((int)(before + __shfl(sum, l, 64) - 1 - number));
-            if (blockIdx.x) break;           // (the first workgroup looks at all sequences for its reports)
+            if (!first_group()) break;         // (the first workgroup looks at all sequences for its reports)
         }
         before += first_lane(__shfl(sum, 63, 64));
     }
@@ -225,27 +229,19 @@ __device__ __forceinline__ void wait_for_tiles()
     __syncthreads();
 }
 
-template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) void prompt_kernel(PromptArgs a, long long places)
+// TILES: of 16 rows per wave.  TOKENS: of a tile of K and V in LDS, 64 or 32.  TURNS: sets of kPromptWaves waves, each of which has all rows of the block and takes every TURNS-th tile;
+// the second set's results are joined to the first's in the end.
+template <int DT, int TILES, int TOKENS, int TURNS>
+__global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES == 1 ? 4 : TOKENS == 32 ? 3 : 2) void prompt_kernel(PromptArgs a)
 {
-    constexpr int kRows = 16 * TILES, kBlock = kRows * kPromptWaves, kPieces = kTile * 16;
+    constexpr int kRows = 16 * TILES, kBlock = kRows * kPromptWaves, kPieces = TOKENS * 16, kHalves = TOKENS / kGroup;
     constexpr int kLoads = kPieces / (64 * kPromptWaves);         // pieces of a tile that a lane brings
-    __shared__ __attribute__((aligned(256))) u32x4 keys[2 * kPieces], values[2 * kPieces];
-    const int lane = lane_id(), wave = wave_id(), i = lane & 15, g = lane >> 4;
-    const int q_heads = a.kv_heads * a.per_kv;
-    for (long long place = blockIdx.x;; place += places) {
-        // neighbouring workgroups, which run on different XCDs, have different KV heads; those of one KV head meet in an L2
-        int kv, head;
-        long long number;
-        if (place >> 32) {
-            kv = (int)(place % a.kv_heads);
-            head = kv * a.per_kv + (int)(place / a.kv_heads % a.per_kv);
-            number = place / q_heads;
-        } else {                             // (a division of 64-bit numbers takes ten times as long)
-            const unsigned low = (unsigned)place, rest = low / (unsigned)a.kv_heads;
-            number = rest / (unsigned)a.per_kv;
-            kv = (int)(low - rest * (unsigned)a.kv_heads);
-            head = kv * a.per_kv + (int)(rest - (unsigned)number * (unsigned)a.per_kv);
-        }
+    __shared__ __attribute__((aligned(256))) u32x4 room[TURNS * 4 * kPieces];
+    const int lane = lane_id(), turn = wave_id() / kPromptWaves, wave = wave_id() % kPromptWaves, i = lane & 15, g = lane >> 4;
+    u32x4 *keys = room + turn * 4 * kPieces, *values = keys + 2 * kPieces;       // two tiles of each
+    // neighbouring workgroups, which run on different XCDs, have different KV heads; those of one KV head meet in an L2
+    const int q_heads = a.kv_heads * a.per_kv, kv = blockIdx.x, head = kv * a.per_kv + blockIdx.y;
+    for (long long number = blockIdx.z;; number += gridDim.z) {
         Block b;
         if (!find_block(a, number, kBlock, b)) return;
         const int first = b.first + wave * kRows;                  // of the wave
@@ -253,29 +249,20 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
         const uint16_t *k_at = a.k + (long long)b.row0 * a.k_row + kv * a.k_head;
         const uint16_t *v_at = a.v + (long long)b.row0 * a.v_row + kv * a.v_head;
         const int tokens = b.first + kBlock < b.rows ? b.first + kBlock : b.rows;
-        const int tiles = (tokens + kTile - 1) / kTile;
-        u32x4 query[TILES][4];
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-            const int row = first + 16 * t + i < b.rows ? first + 16 * t + i : b.rows - 1;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                query[t][c] = *(const u32x4 *)(q_at + (long long)row * a.q_row + 32 * c + 8 * g);
-                query[t][c] = (query[t][c] & a.query_and) ^ a.query_xor;
-            }
-        }
+        const int tiles = (tokens + TOKENS - 1) / TOKENS;
         // A tile of keys or values into its half of LDS: the lane's places in LDS are fixed (64 lanes have 1 KB in a row), so the
         // octets are turned by what each lane asks for.  An address is one of the wave and an offset of the lane's that stays.  In place of
         // tokens behind the sequence there is the tile's first, which no row sees.
         const int place_in = wave * 4 + g;             // (of 16 tokens; lane g * 16 + i brings piece i)
         const uint32_t key_at = place_in * 2 * (uint32_t)a.k_row + 16 * (key_piece(place_in, i) & 15);
         const uint32_t value_at = place_in * 2 * (uint32_t)a.v_row + 16 * (value_piece(place_in, i) & 15);
-        auto bring = [&](u32x4 *room, const uint16_t *from, long long stride, uint32_t lane_at, int n) {
+        auto bring = [&](u32x4 *tile, const uint16_t *from, long long stride, uint32_t lane_at, int n) {
             if (n >= tiles) return;
-            const char *base = (const char *)(from + (long long)n * kTile * stride);
-            const int have = b.rows - n * kTile;
-            const uint32_t to = lds_address(room + (n & 1) * kPieces + wave * 64);
-            if (have >= kTile) {
+            const int half = n / TURNS & 1;
+            const char *base = (const char *)(from + (long long)n * TOKENS * stride);
+            const int have = b.rows - n * TOKENS;
+            const uint32_t to = lds_address(tile + half * kPieces + wave * 64);
+            if (have >= TOKENS) {
 #pragma unroll
                 for (int r = 0; r < kLoads; ++r) copy_to_lds(base + 32 * r * stride, lane_at, to + r * kPromptWaves * 1024);
             } else {
@@ -287,6 +274,23 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
                 }
             }
         };
+        auto bring_first = [&]() {
+            bring(keys, k_at, a.k_row, key_at, turn);
+            bring(values, v_at, a.v_row, value_at, turn);
+            bring(keys, k_at, a.k_row, key_at, turn + TURNS);
+        };
+        bring_first();
+        // (behind the first tiles, whose requests the compiler does not count: it waits for these, which come last)
+        u32x4 query[TILES][4];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+            const int row = first + 16 * t + i < b.rows ? first + 16 * t + i : b.rows - 1;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                query[t][c] = *(const u32x4 *)(q_at + (long long)row * a.q_row + 32 * c + 8 * g);
+                query[t][c] = (query[t][c] & a.query_and) ^ a.query_xor;
+            }
+        }
         f32x4 out[TILES][8];
         float top[TILES], shift[TILES], sum[TILES];
         // Tile n.  MIXED: some rows see some of its tokens only, or none.  AGAIN: with values that are not finite taken out where they are
@@ -296,15 +300,15 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
             constexpr bool MIXED = decltype(mixed_tile)::value, AGAIN = decltype(second_time)::value;
             // (turning an octet by a token's number is an exclusive or, and the tiles lie at multiples of their rows: all octets' addresses
             // are the first one's and an exclusive or with a constant)
-            const uint32_t key_lane = lds_address(keys + (n & 1) * kPieces) + 16 * key_piece(i, g);
-            const uint32_t value_lane = lds_address(values + (n & 1) * kPieces) + 16 * value_piece(4 * g + (i >> 2), (i & 3) >> 1) + 8 * (i & 1);
-            const int token = n * kTile;
-            const bool some = !MIXED || (first < b.rows && token < first + kRows), both = !MIXED || token + kGroup < first + kRows;
-            u32x4 weight[2][TILES];
+            const uint32_t key_lane = lds_address(keys + (n / TURNS & 1) * kPieces) + 16 * key_piece(i, g);
+            const uint32_t value_lane = lds_address(values + (n / TURNS & 1) * kPieces) + 16 * value_piece(4 * g + (i >> 2), (i & 3) >> 1) + 8 * (i & 1);
+            const int token = n * TOKENS;
+            const bool some = !MIXED || (first < b.rows && token < first + kRows && (TURNS == 1 || n < tiles)), both = !MIXED || token + kGroup < first + kRows;
+            u32x4 weight[kHalves][TILES];
             if (some) {
-                f32x4 score[4][TILES];
+                f32x4 score[2 * kHalves][TILES];
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
+                for (int h = 0; h < 2 * kHalves; ++h) {
 #pragma unroll
                     for (int t = 0; t < TILES; ++t) score[h][t] = f32x4{0, 0, 0, 0};
                     if (h >= 2 && !both) continue;
@@ -317,7 +321,7 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
                 }
                 if (MIXED) {
 #pragma unroll
-                    for (int h = 0; h < 4; ++h)
+                    for (int h = 0; h < 2 * kHalves; ++h)
 #pragma unroll
                         for (int t = 0; t < TILES; ++t)
 #pragma unroll
@@ -330,7 +334,7 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
                 for (int t = 0; t < TILES; ++t) {
                     most[t] = score[0][t][0];
 #pragma unroll
-                    for (int e = 1; e < 16; ++e) most[t] = fmaxf(most[t], score[e >> 2][t][e & 3]);
+                    for (int e = 1; e < 8 * kHalves; ++e) most[t] = fmaxf(most[t], score[e >> 2][t][e & 3]);
                     grown |= __builtin_fmaf(most[t], a.factor, -top[t]) > kSlack;
                 }
                 if (__any(grown)) {
@@ -349,7 +353,7 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
                     }
                 }
 #pragma unroll
-                for (int h = 0; h < 4; ++h)
+                for (int h = 0; h < 2 * kHalves; ++h)
 #pragma unroll
                     for (int t = 0; t < TILES; ++t) {
                         float w[4];
@@ -366,8 +370,8 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
             for (int t = 0; t < TILES; ++t) asm volatile("" : "+v"(sum[t]));   // (added up here, not held apart until the products are done)
             wait_for_tiles();                        // this tile's values, the next tile's keys
             // (what the next ones overwrite has no readers behind the barrier: this tile's keys, the last tile's values)
-            bring(values, v_at, a.v_row, value_at, n + 1);
-            bring(keys, k_at, a.k_row, key_at, n + 2);
+            bring(values, v_at, a.v_row, value_at, n + TURNS);
+            bring(keys, k_at, a.k_row, key_at, n + 2 * TURNS);
             // token 4 g + i / 4 of the lane's 16 (then 16 further), channels 16 d + 4 (i % 4) ... + 3; the lane gets tokens
             // 4 g ... 4 g + 3 of channel 16 d + i
             auto value_of = [&](int half, int d) {
@@ -383,7 +387,7 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
             };
             if (some) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
+                for (int half = 0; half < kHalves; ++half) {
                     if (half && !both) continue;
                     u32x4 seen[TILES];
                     if (MIXED && AGAIN) {
@@ -423,28 +427,58 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
 #pragma unroll
                 for (int d = 0; d < 8; ++d) out[t][d] = f32x4{0, 0, 0, 0};
             }
-            bring(keys, k_at, a.k_row, key_at, 0);
+            if (decltype(second_time)::value) bring_first();
             wait_for_tiles();
-            bring(values, v_at, a.v_row, value_at, 0);
-            bring(keys, k_at, a.k_row, key_at, 1);
-            const int whole = b.first / kTile;       // tiles of which all rows see all tokens
+            // (all sets pass the same barriers: a set may have a tile behind the last one, of which no row sees anything)
+            const int whole = b.first / TOKENS / TURNS * TURNS;       // tiles of which all rows see all tokens
             const int for_whole = here_only(lane);
-            for (int n = 0; n < whole; ++n) do_tile(n, for_whole, BoolConst<false>(), second_time);
+            for (int n = 0; n < whole; n += TURNS) do_tile(n + turn, for_whole, BoolConst<false>(), second_time);
             const int for_mixed = here_only(lane);
-            for (int n = whole; n < tiles; ++n) do_tile(n, for_mixed, BoolConst<true>(), second_time);
-            bool finite = true;
+            for (int n = whole; n < tiles; n += TURNS) do_tile(n + turn, for_mixed, BoolConst<true>(), second_time);
+            if constexpr (TURNS > 1) {
+                constexpr int kResults = TILES * 8 * kPromptWaves * 64, kStatistics = TILES * kPromptWaves * 64;       // of a set
+                static_assert((TURNS - 1) * (kResults * sizeof(f32x4) + kStatistics * sizeof(f32x2)) <= sizeof(room), "results go through the tiles' room");
+                f32x4 *results = (f32x4 *)room + wave * 64 + lane;
+                f32x2 *statistics = (f32x2 *)((f32x4 *)room + (TURNS - 1) * kResults) + wave * 64 + lane;
+                __syncthreads();
+                if (turn) {
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) {
+                        statistics[(turn - 1) * kStatistics + t * kPromptWaves * 64] = f32x2{top[t], sum[t]};
+#pragma unroll
+                        for (int d = 0; d < 8; ++d) results[(turn - 1) * kResults + (t * 8 + d) * kPromptWaves * 64] = out[t][d];
+                    }
+                }
+                __syncthreads();
+                if (turn) return true;
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                    for (int k = 0; k < TURNS - 1; ++k) {
+                        const f32x2 other = statistics[k * kStatistics + t * kPromptWaves * 64];
+                        const float now = fmaxf(top[t], other[0]), from = now == kNone ? 0.0f : now;
+                        const float by = __builtin_amdgcn_exp2f(top[t] - from), other_by = __builtin_amdgcn_exp2f(other[0] - from);
+                        top[t] = now;
+                        shift[t] = kBias - from;
+                        sum[t] = sum[t] * by + other[1] * other_by;
+#pragma unroll
+                        for (int d = 0; d < 8; ++d) out[t][d] = out[t][d] * by + results[k * kResults + (t * 8 + d) * kPromptWaves * 64] * other_by;
+                    }
+            }
+            f32x4 zero = {0, 0, 0, 0};               // times infinity, or NaN: NaN
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
 #pragma unroll
                 for (int d = 0; d < 8; ++d)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) finite &= out[t][d][e] - out[t][d][e] == 0.0f;
-            return finite || first >= b.rows;
+                    for (int e = 0; e < 4; ++e) zero[e] = __builtin_fmaf(out[t][d][e], 0.0f, zero[e]);
+            return zero[0] + zero[1] + (zero[2] + zero[3]) == 0.0f || first >= b.rows;
         };
         const bool finite = do_tiles(BoolConst<false>());
         if (__builtin_amdgcn_readfirstlane(__syncthreads_or(!finite))) do_tiles(BoolConst<true>());
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
+            if (turn) break;
             const int row = first + 16 * t + i;
             const float all = sum_of_row(sum[t]), by = 1.0f / all;
             if (row >= b.rows) continue;
@@ -455,36 +489,80 @@ template <int DT, int TILES> __global__ __launch_bounds__(64 * kPromptWaves, 2) 
             if (a.lse && g == 0)
                 a.lse[(long long)(b.row0 + row) * q_heads + head] = (__builtin_amdgcn_logf(all) - shift[t]) * 0.693147181f;
         }
-        if (place + places >= b.all * q_heads) return;
+        if (number + gridDim.z >= b.all) return;
         __syncthreads();
     }
 }
 
-PromptShape prompt_shape(const PromptArgs &a)
+// ---- which kernel ---------------------------------------------------------------------------------
+
+// The kernels, and what a call takes with each, us: the longest sequence's tiles one after the other (per 64 tokens), the products at the rate of a
+// full chip, what a workgroup takes apart from them, and the launch; fitted to 20 calls of 1 to 200 sequences of 30 to 32k tokens, 8 to 64 heads.
+//   64 rows    37 tokens x 64 heads 6.2 us, 64 x 100 x 32 42, 8 x 512 x 32 42, 1024 x 64 32      tiles of 32 tokens, four workgroups per compute unit
+//   64 shared  512 x 32 13.5 (one set of waves 16.4), 1024 x 32 21.2 (28.0), 4096 x 8 63 (93)   two sets of waves take turns: too few rows for the chip
+//   128 rows   2048 x 64 85 (64 rows: 99), 4096 x 32 157 (178), 8 x 1024 x 32 100 (105)            tiles of 32 tokens, three workgroups
+//   192 rows   8192 x 32 509 (128 rows: 511), 32768 x 64 15.1 ms (16.1)                              tiles of 64 tokens, two workgroups: K and V are read least
+struct Kernel {
+    int tiles, tokens, turns;
+    float per_64, rate, group, launch;       // us, TFLOP/s, us, us
+};
+constexpr Kernel kKernels[] = {{1, 32, 1, 1.38f, 910.0f, 0.0076f, 5.0f},
+                               {1, 32, 2, 0.82f, 860.0f, 0.0150f, 6.0f},
+                               {2, 32, 1, 1.80f, 1120.0f, 0.0160f, 5.0f},
+                               {3, 64, 1, 1.97f, 1190.0f, 0.0250f, 5.0f}};
+constexpr int kKinds = sizeof(kKernels) / sizeof(kKernels[0]);
+
+// Blocks of `size` rows that a call has at most: what the sequences' number and bound allow, or their rows in all.
+static long long most_blocks(const PromptArgs &a, int size)
 {
-    PromptShape s;
-#ifndef RT
-#define RT 2
-#endif
-    s.tiles = RT;
-    const long long size = 16 * s.tiles * kPromptWaves, each = (a.max_rows + size - 1) / size;
-    // blocks of all sequences: no more than what their number and bound allow, or their rows in all
-    long long blocks = each * a.n, most = a.rows / size + a.n;
-    blocks = blocks < most ? blocks : most;
-    s.places = blocks * a.kv_heads * a.per_kv;
-    const long long limit = 1 << 22;         // (further blocks are taken in turn, which also covers starts that overlap)
-    s.places = s.places < 1 ? 1 : s.places > limit ? limit : s.places;
-    return s;
+    const long long each = ((long long)a.max_rows + size - 1) / size * a.n, rows = a.rows / size + a.n;
+    return each < rows ? each : rows;
+}
+static int kernel_for(const PromptArgs &a)
+{
+    const double heads = (double)a.kv_heads * a.per_kv, longest = a.max_rows < a.rows ? a.max_rows : (double)a.rows;
+    const double rows = (double)a.max_rows * a.n < a.rows ? (double)a.max_rows * a.n : (double)a.rows;
+    int best = 0;
+    double least = 0.0;
+    for (int k = 0; k < kKinds; ++k) {
+        const Kernel &c = kKernels[k];
+        const double chain = c.per_64 * longest / 64, groups = heads * most_blocks(a, 16 * c.tiles * kPromptWaves);
+        const double work = 4.0 * kDim * heads * rows * longest / 2 / c.rate * 1e-6 + c.group * groups;
+        const double time = c.launch + sqrt(chain * chain + work * work);
+        if (k == 0 || time < least) {
+            best = k;
+            least = time;
+        }
+    }
+    return best;
 }
 
-template <int DT> static void launch_type(const PromptArgs &a, const PromptShape &s, hipStream_t stream)
+template <int DT, int KIND> static void launch_kind(const PromptArgs &a, hipStream_t stream)
 {
-    prompt_kernel<DT, RT><<<dim3((unsigned)s.places), 64 * kPromptWaves, 0, stream>>>(a, s.places);
+    constexpr Kernel c = kKernels[KIND];
+    // (a grid has 65535 places in this direction; further blocks are taken in turn, which also covers starts that overlap)
+    const long long blocks = most_blocks(a, 16 * c.tiles * kPromptWaves);
+    const dim3 grid(a.kv_heads, a.per_kv, (unsigned)(blocks < 1 ? 1 : blocks > 65535 ? 65535 : blocks));
+    prompt_kernel<DT, c.tiles, c.tokens, c.turns><<<grid, 64 * kPromptWaves * c.turns, 0, stream>>>(a);
 }
-void launch_prompt(int dtype, const PromptArgs &a, const PromptShape &s, hipStream_t stream)
+template <int DT> static void launch_type(const PromptArgs &a, int kind, hipStream_t stream)
 {
-    if (dtype == DT_F16) launch_type<DT_F16>(a, s, stream);
-    else launch_type<DT_BF16>(a, s, stream);
+    if (kind == 0) launch_kind<DT, 0>(a, stream);
+    else if (kind == 1) launch_kind<DT, 1>(a, stream);
+    else if (kind == 2) launch_kind<DT, 2>(a, stream);
+    else launch_kind<DT, 3>(a, stream);
+}
+void launch_prompt(int dtype, const PromptArgs &a, hipStream_t stream)
+{
+    if (dtype == DT_F16) launch_type<DT_F16>(a, kernel_for(a), stream);
+    else launch_type<DT_BF16>(a, kernel_for(a), stream);
+}
+
+int prompt_block_rows(const PromptArgs &a, int &waves)
+{
+    const Kernel &c = kKernels[kernel_for(a)];
+    waves = kPromptWaves * c.turns;
+    return 16 * c.tiles * kPromptWaves;
 }
 
 }  // namespace kvc

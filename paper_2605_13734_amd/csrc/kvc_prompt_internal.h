@@ -46,15 +46,11 @@ struct PromptArgs {
     int n, max_rows, kv_heads, per_kv;
 };
 
-// What the kernels have of a launch: rows of a block and workgroups.
-struct PromptShape {
-    int tiles;                     // of 16 rows per wave
-    long long places;
-};
-constexpr int kPromptWaves = 4;
+constexpr int kPromptWaves = 4;               // that divide the rows of a block
 
-PromptShape prompt_shape(const PromptArgs &a);
-void launch_prompt(int dtype, const PromptArgs &a, const PromptShape &s, hipStream_t stream);
+void launch_prompt(int dtype, const PromptArgs &a, hipStream_t stream);
+// rows of a block, and waves of a workgroup, in a call with these bounds
+int prompt_block_rows(const PromptArgs &a, int &waves);
 
 // ---- the pages' tables -----------------------------------------------------------------------------
 

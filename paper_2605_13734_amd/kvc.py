@@ -24,7 +24,7 @@ SYMBOLS = ["kvc_plan", "kvc_plan_free", "kvc_payload_size", "kvc_workspace_size"
            "kvc_trace", "kvc_selftest", "kvc_table_bytes", "kvc_workspace_init", "kvc_compress_static", "kvc_stream_probe", "kvc_profile_throughput", "kvc_benefit_threshold", "kvc_policy_build",
            "kvc_policy_lookup", "kvc_cache_plan", "kvc_cache_plan_free", "kvc_cache_page_bytes", "kvc_cache_workspace_size", "kvc_cache_block_rows",
            "kvc_cache_store", "kvc_cache_load", "kvc_cache_keep", "kvc_cache_attend", "kvc_cache_advance", "kvc_rotary_frequencies",
-           "kvc_prompt_plan", "kvc_prompt_plan_free", "kvc_prompt_rotate", "kvc_prompt_attend"]
+           "kvc_prompt_plan", "kvc_prompt_plan_free", "kvc_prompt_block_rows", "kvc_prompt_rotate", "kvc_prompt_attend"]
 
 
 class Strategy(C.Structure):
@@ -172,6 +172,7 @@ def load():
         L.kvc_prompt_plan.argtypes = [C.POINTER(PromptConfig), C.c_int32, C.POINTER(C.c_void_p)]
         L.kvc_prompt_plan_free.argtypes = [C.c_void_p]
         L.kvc_prompt_plan_free.restype = None
+        L.kvc_prompt_block_rows.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.POINTER(C.c_int32)]
         L.kvc_prompt_rotate.argtypes = [C.c_void_p, C.POINTER(PromptRows), C.c_void_p]
         L.kvc_prompt_attend.argtypes = [C.c_void_p, C.POINTER(PromptSequences), C.POINTER(PromptHeads), C.c_void_p, C.c_void_p]
         L.kvc_status_string.argtypes = [C.c_int]
@@ -642,6 +643,11 @@ class PromptPlan:
         if getattr(self, "_h", None) and _lib is not None:
             _lib.kvc_prompt_plan_free(self._h)
             self._h = None
+
+    def block_rows(self, n, max_rows, rows):
+        """kvc_prompt_block_rows: (rows, waves) of a workgroup of an attention with these bounds."""
+        waves = C.c_int32()
+        return load().kvc_prompt_block_rows(self._h, n, max_rows, rows, C.byref(waves)), waves.value
 
 
 class PromptBatch:

@@ -242,15 +242,17 @@ def test_layouts():
 
 @pytest.mark.parametrize("bf16", [False, True])
 def test_packed_is_as_alone(bf16):
-    """Equal inputs give equal bits: again, and each sequence in a call of its own."""
+    """Equal inputs and bounds give equal bits: again, and each sequence in a call of its own."""
     c = Case([300, 77, 1, 520], 2, 2, bf16, seed=5).run()
     first = c.out.clone(), c.lse.clone()
     c.run()
     assert torch.equal(c.out, first[0]) and torch.equal(c.lse, first[1])
+    block = c.prompt.plan.block_rows(4, 520, 898)
     for a, b in zip(c.starts, c.starts[1:]):
-        out = torch.empty_like(c.q[a:b])
-        c.prompt.attend(kvc.PromptBatch(i32(0, b - a), b - a), c.q[a:b], c.k[a:b], c.v[a:b], out, SCALE, None, stream())
-        assert torch.equal(out, c.out[a:b])
+        out = torch.full_like(c.q, 77.0)
+        assert c.prompt.plan.block_rows(1, 520, 898) == block
+        c.prompt.attend(kvc.PromptBatch(i32(a, b), 520), c.q, c.k, c.v, out, SCALE, None, stream())
+        assert torch.equal(out[a:b], c.out[a:b]) and (out[:a] == 77).all() and (out[b:] == 77).all()
 
 
 def test_bounds_above_the_lengths():

@@ -36,7 +36,7 @@ def test_plans(lib):
                dict(eps=-1e-6), dict(eps=math.nan), dict(eps=math.inf), dict(amplitude=0.0), dict(amplitude=math.nan), dict(head_dim=0),
                dict(frequencies=[math.nan] * 64), dict(frequencies=[math.inf] * 64), dict(frequencies=[1e10] * 64)]:
         assert status_of(lambda: plan(**kw)) == -1, kw
-    for kw in [dict(head_dim=256), dict(rotary_dim=24, frequencies=[1.0] * 12), dict(q_heads=2 * 65536), dict(max_batch=65536)]:
+    for kw in [dict(head_dim=256), dict(rotary_dim=24, frequencies=[1.0] * 12), dict(q_heads=65536), dict(max_batch=65536)]:
         assert status_of(lambda: plan(**kw)) == -2, kw
     with pytest.raises(ValueError):
         plan(frequencies=[1.0] * 63)
@@ -139,6 +139,24 @@ def test_attention_refused(lib):
     assert call(n=0, start=None) == 0 and call(max_rows=0, q=None) == 0
     if not torch.cuda.is_available():
         assert call() == -6 and call(scale=0.0, lse=AT + 4) == -6 and call(k_stride_row=0, v_stride_row=1 << 24, q_stride_row=-1024) == -6 and call(rows=0, q=None, k=None, v=None, out=None) == -6
+
+
+def test_block_rows(lib):
+    """Few rows: 64, shared by two sets of waves where they are long; many: 128; long ones: 192."""
+    p = plan(kv_heads=8, q_heads=64, max_batch=300)
+    assert p.block_rows(1, 37, 37) == (64, 4) and p.block_rows(200, 30, 6000) == (64, 4)
+    few = plan(kv_heads=8, q_heads=32)
+    assert few.block_rows(1, 1024, 1024) == few.block_rows(1, 2048, 2048) == (64, 8)
+    assert p.block_rows(1, 2048, 2048)[0] == 128 and p.block_rows(1, 32768, 32768) == (192, 4)
+    one = plan(kv_heads=1, q_heads=1)
+    assert one.block_rows(1, 8192, 8192) == (64, 8)
+    # (a bound beyond the tensors' rows means no more than those)
+    assert few.block_rows(1, 1 << 30, 1024) == (64, 8)
+    for args in ((0, 5, 5), (301, 5, 5), (1, 0, 5), (1, 5, 0), (-1, 5, 5), (1, 5, (1 << 28) + 1)):
+        assert p.block_rows(*args) == (0, 0), args
+    waves = C.c_int32(7)
+    assert lib.kvc_prompt_block_rows(None, 1, 5, 5, C.byref(waves)) == 0 and waves.value == 0
+    assert lib.kvc_prompt_block_rows(p._h, 1, 37, 37, None) == 64
 
 
 def test_advance_refused(lib):
