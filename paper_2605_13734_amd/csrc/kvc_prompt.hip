@@ -102,7 +102,8 @@ extern "C" int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt
         !aligned(r->k_weight, 16) || !aligned(r->positions, 4)) return KVC_ERR_ARG;
     if (!strides_ok(r->q_stride_row, r->q_stride_head) || !strides_ok(r->k_stride_row, r->k_stride_head) ||
         !strides_ok(r->q_out_stride_row, r->q_out_stride_head) || !strides_ok(r->k_out_stride_row, r->k_out_stride_head)) return KVC_ERR_ARG;
-    if (r->rows > 0x7fffffffll) return KVC_ERR_CAPACITY;
+    // (a workgroup has four waves of 4 heads at least)
+    if (r->rows > kMostRows || r->rows * (f.q_heads + f.kv_heads + 6) / 16 * 256 > 0xffffffffll) return KVC_ERR_CAPACITY;
     RotateArgs a = {};
     a.q = RotateTensor{(const uint16_t *)r->q, f.norm ? (const uint16_t *)r->q_weight : nullptr, (uint16_t *)r->q_out, r->q_stride_row,
                        r->q_stride_head, r->q_out_stride_row, r->q_out_stride_head, r->q ? f.q_heads : 0, 0};

@@ -27,6 +27,7 @@ struct RotateArgs {
     float eps, amplitude;
     int pairs;                     // rotated pairs of channels, a multiple of 8
     int chunk, chunks;             // heads of a row that a wave takes, waves per row
+    int past_caches, pad;          // rows are read past the caches
 };
 
 void launch_rotate(int dtype, bool neighbours, bool norm, const RotateArgs &a, hipStream_t stream);

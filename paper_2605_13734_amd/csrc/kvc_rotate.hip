@@ -5,7 +5,8 @@
 //
 // All in 32 bits, rounded once as it is stored.  Bound by HBM where there are many rows (every element is read and written once) and by
 // latency where there are few.  A wave has one row and a run of its heads, four heads at a time, 16 lanes per head and 8 channels
-// per lane: cosines and sines are made once per row and wave, the mean of a head inside a row of lanes.
+// per lane: cosines and sines are made once per row and wave, the mean of a head inside a row of lanes.  32k rows of 72 heads: 191 us, 6.3 TB/s (the fastest
+// copy found on this card 6.5); 32 rows 3.3 us in a graph, most of it the launch.
 //
 // Angles are fixed-point numbers of 2^-64 of a turn: a position times a frequency's part of a turn, modulo a turn, is one integer product
 // whose upper word is the angle, exact to 2^-32 of a turn wherever the position is (in 32-bit floating point a position of 10^6 would be
@@ -73,6 +74,11 @@ __device__ __forceinline__ u32x4 other_octet(const u32x4 &x, int other, bool opp
     return r;
 }
 
+constexpr int kAtOnce = 4;                    // groups of four heads that a wave requests together
+template <int N> struct Count {
+    static constexpr int value = N;
+};
+
 template <int DT, bool NEIGHBOURS, bool NORM> __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a)
 {
     const long long unit = (long long)blockIdx.x * 4 + wave_id();
@@ -126,49 +132,63 @@ template <int DT, bool NEIGHBOURS, bool NORM> __global__ __launch_bounds__(256) 
     }
     const uint16_t *in = x.in + row * x.in_row + 8 * col;
     uint16_t *out = x.out + row * x.out_row + 8 * col;
-    for (int h = first; h < end; h += 4) {
-        const int head = h + sub < end ? h + sub : end - 1;
-        const u32x4 r = *(const u32x4 *)(in + head * x.in_head);
-        const u32x4 p = NEIGHBOURS ? r : other_octet(r, partner, half == 8);
-        float mine[8], theirs[8], y[8];
+    // GROUPS of four heads at a time, all requested at once
+    auto do_heads = [&](int h, auto groups) {
+        constexpr int GROUPS = decltype(groups)::value;
+        u32x4 r[GROUPS];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            mine[e] = elem_f32<DT>(r, e);
-            theirs[e] = elem_f32<DT>(p, NEIGHBOURS ? e ^ 1 : e);
+        for (int u = 0; u < GROUPS; ++u) {
+            const int head = h + 4 * u + sub < end ? h + 4 * u + sub : end - 1;
+            const u32x4 *from = (const u32x4 *)(in + head * x.in_head);
+            r[u] = a.past_caches ? __builtin_nontemporal_load(from) : *from;
         }
-        float by = 1.0f;
-        if (NORM) {
-            float sum = 0.0f, eps = a.eps;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(mine[e], mine[e], sum);
-            sum = sum_of_row(sum);
-            // bf16 values whose squares leave 32 bits: all of the head times a power of two
-            const bool large = sum > 1e38f, small = sum < 1e-30f && eps < 1e-30f;
-            if (DT == DT_BF16 && __any(large || small)) {
-                const float f = large ? 0x1p-70f : small ? 0x1p80f : 1.0f;
-                sum = 0.0f;
+        for (int u = 0; u < GROUPS; ++u) {
+            const int head = h + 4 * u + sub;
+            const u32x4 p = NEIGHBOURS ? r[u] : other_octet(r[u], partner, half == 8);
+            float mine[8], theirs[8], y[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    mine[e] *= f;
-                    theirs[e] *= f;
-                    sum = __builtin_fmaf(mine[e], mine[e], sum);
-                }
-                sum = sum_of_row(sum);
-                eps = eps * f * f;               // (the square alone may leave 32 bits)
+            for (int e = 0; e < 8; ++e) {
+                mine[e] = elem_f32<DT>(r[u], e);
+                theirs[e] = elem_f32<DT>(p, NEIGHBOURS ? e ^ 1 : e);
             }
-            by = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, 1.0f / kDim, eps));
-        }
+            float by = 1.0f;
+            if (NORM) {
+                float sum = 0.0f, eps = a.eps;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            y[e] = mine[e] * own[e];
-            if (turns) y[e] = __builtin_fmaf(theirs[e], other[e], y[e]);
-            if (NORM) y[e] *= by;
+                for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(mine[e], mine[e], sum);
+                sum = sum_of_row(sum);
+                // bf16 values whose squares leave 32 bits: all of the head times a power of two
+                const bool large = sum > 1e38f, small = sum < 1e-30f && eps < 1e-30f;
+                if (DT == DT_BF16 && __any(large || small)) {
+                    const float f = large ? 0x1p-70f : small ? 0x1p80f : 1.0f;
+                    sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        mine[e] *= f;
+                        theirs[e] *= f;
+                        sum = __builtin_fmaf(mine[e], mine[e], sum);
+                    }
+                    sum = sum_of_row(sum);
+                    eps = eps * f * f;               // (the square alone may leave 32 bits)
+                }
+                by = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, 1.0f / kDim, eps));
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                y[e] = mine[e] * own[e];
+                if (turns) y[e] = __builtin_fmaf(theirs[e], other[e], y[e]);
+                if (NORM) y[e] *= by;
+            }
+            if (head < end) {
+                const u32x4 z = {round_pair<DT>(y[0], y[1]), round_pair<DT>(y[2], y[3]), round_pair<DT>(y[4], y[5]), round_pair<DT>(y[6], y[7])};
+                __builtin_nontemporal_store(z, (u32x4 *)(out + head * x.out_head));
+            }
         }
-        if (h + sub < end) {
-            const u32x4 z = {round_pair<DT>(y[0], y[1]), round_pair<DT>(y[2], y[3]), round_pair<DT>(y[4], y[5]), round_pair<DT>(y[6], y[7])};
-            *(u32x4 *)(out + head * x.out_head) = z;
-        }
-    }
+    };
+    int h = first;
+    for (; h + 4 * kAtOnce <= end; h += 4 * kAtOnce) do_heads(h, Count<kAtOnce>());
+    for (; h < end; h += 4) do_heads(h, Count<1>());
 }
 
 template <int DT, bool NEIGHBOURS> static void launch_layout(bool norm, const RotateArgs &a, dim3 grid, hipStream_t stream)
@@ -177,15 +197,23 @@ template <int DT, bool NEIGHBOURS> static void launch_layout(bool norm, const Ro
     else rotate_kernel<DT, NEIGHBOURS, false><<<grid, 256, 0, stream>>>(a);
 }
 
-// Heads of a row that a wave takes: all of a tensor's where the rows alone fill the chip, four where they do not.
-constexpr long long kManyRows = 8192;
+// Heads of a row that a wave takes: up to 16, which are 4 KB in a row for each of a workgroup's waves (32k rows of 72 heads: 191 us, with all of a row
+// in one wave 214, with 8 heads 225); fewer while there are not that many waves (1k rows of 40 heads: 5.5 us, with waves of 4 heads 7.9).
+constexpr int kMostHeads = 16;
+constexpr long long kLeastWaves = 4096;
+// Bytes read and written beyond which rows are read past the caches, which cannot hold them for anyone (32k rows of 72 heads, 1.2 GB: 191 instead of
+// 229 us; 8k rows of 40 heads, 168 MB: 30 instead of 29).
+constexpr double kCaches = 256e6;
 
 void launch_rotate(int dtype, bool neighbours, bool norm, const RotateArgs &args, hipStream_t stream)
 {
     RotateArgs a = args;
     const int most = a.q.heads > a.k.heads ? a.q.heads : a.k.heads;
-    a.chunk = a.rows >= kManyRows ? (most + 3) / 4 * 4 : 4;
-    a.chunks = (a.q.heads + a.chunk - 1) / a.chunk + (a.k.heads + a.chunk - 1) / a.chunk;
+    auto chunks = [&](int chunk) { return (a.q.heads + chunk - 1) / chunk + (a.k.heads + chunk - 1) / chunk; };
+    a.chunk = most < kMostHeads ? (most + 3) / 4 * 4 : kMostHeads;
+    while (a.chunk > 4 && a.rows * chunks(a.chunk) < kLeastWaves) a.chunk -= 4;
+    a.chunks = chunks(a.chunk);
+    a.past_caches = (double)a.rows * (a.q.heads + a.k.heads) * 4 * kDim > kCaches;
     const dim3 grid((unsigned)((a.rows * a.chunks + 3) / 4));
     if (dtype == DT_F16) neighbours ? launch_layout<DT_F16, true>(norm, a, grid, stream) : launch_layout<DT_F16, false>(norm, a, grid, stream);
     else neighbours ? launch_layout<DT_BF16, true>(norm, a, grid, stream) : launch_layout<DT_BF16, false>(norm, a, grid, stream);

@@ -561,6 +561,8 @@ class CachePages:
         self.free = torch.zeros(4 + num_pages, **i32)
         self.set_free(torch.arange(num_pages - 1, -1, -1, dtype=torch.int32))
         self._device = self.held.get_device() if self.held.is_cuda else None
+        self._n, self._stride, self._int32, self._int64 = n, self.table.shape[1], torch.int32, torch.int64
+        self._held, self._table, self._status, self._free = (x.data_ptr() for x in (self.held, self.table, self.status, self.free))
         self._plan, self._advance = plan._h, load().kvc_cache_advance
         if torch.cuda.device_count() > 1:
             self._advance = functools.partial(_on_device, self._device, self._advance)
@@ -587,23 +589,21 @@ class CachePages:
                 stream=None):
         """kvc_cache_advance.  new_start [n + 1], tokens [n]: int32, written; kept, fresh [n]: int32 or None; positions [rows] int32,
         slots [rows] int64: written, or None (then rows is the room that the new rows have, if it is bounded)."""
-        import torch
-        n = self.held.shape[0]
+        n = self._n
         for x, size in ((new_start, n + 1), (tokens, n), (kept, n), (fresh, n)):
-            if x is not None and (x.dtype is not torch.int32 or x.shape != (size,) or not x.is_contiguous() or x.get_device() != self._device):
+            if x is not None and (x.dtype is not self._int32 or x.shape != (size,) or not x.is_contiguous() or x.get_device() != self._device):
                 raise ValueError("new_start [n + 1], tokens, kept and fresh [n] are contiguous int32 tensors on the tables' device")
-        for x, dtype in ((positions, torch.int32), (slots, torch.int64)):
+        for x, dtype in ((positions, self._int32), (slots, self._int64)):
             if x is not None:
                 if x.dtype is not dtype or x.dim() != 1 or not x.is_contiguous() or x.get_device() != self._device or \
                         (rows is not None and rows != x.shape[0]):
                     raise ValueError("positions (int32) and slots (int64) are contiguous tensors of one length on the tables' device")
                 rows = x.shape[0]
         step = CacheStep(n, max_new, self.plan.max_tokens if max_tokens is None else max_tokens, 0x7fffffff if rows is None else rows,
-                         self.held.data_ptr(), kept.data_ptr() if kept is not None else None, fresh.data_ptr() if fresh is not None else None,
-                         self.free.data_ptr(), self.table.data_ptr(), self.table.shape[1], new_start.data_ptr(), tokens.data_ptr(),
-                         positions.data_ptr() if positions is not None else None, slots.data_ptr() if slots is not None else None,
-                         self.num_pages)
-        rc = self._advance(self._plan, step, self.status.data_ptr(), stream)
+                         self._held, kept.data_ptr() if kept is not None else None, fresh.data_ptr() if fresh is not None else None, self._free,
+                         self._table, self._stride, new_start.data_ptr(), tokens.data_ptr(), positions.data_ptr() if positions is not None else None,
+                         slots.data_ptr() if slots is not None else None, self.num_pages)
+        rc = self._advance(self._plan, step, self._status, stream)
         if rc != OK:
             raise KvcError("kvc_cache_advance", rc)
 
@@ -672,6 +672,7 @@ class Prompt:
         self.dtype = torch.float16 if plan.config.dtype == F16 else torch.bfloat16
         self.status = torch.zeros(plan.max_batch, dtype=torch.int32, device=device)
         self._device = self.status.get_device() if self.status.is_cuda else None
+        self._int32, self._float32 = torch.int32, torch.float32
         f, lib = plan.config, load()
         self._kv_heads, self._q_heads, self._dim, self._plan, self._norm = f.kv_heads, f.q_heads, f.head_dim, plan._h, bool(f.norm)
         self._rotate, self._attend = lib.kvc_prompt_rotate, lib.kvc_prompt_attend
@@ -683,34 +684,48 @@ class Prompt:
     def rotate(self, q, k, positions, q_out=None, k_out=None, q_weight=None, k_weight=None, stream=None):
         """kvc_prompt_rotate: q [rows, q_heads, 128], k [rows, kv_heads, 128], either may be None; positions [rows] int32; without q_out
         or k_out in place."""
-        import torch
-        u, seen = PromptRows(), None
-        for name, x, out, weight, heads in (("q", q, q_out, q_weight, self._q_heads), ("k", k, k_out, k_weight, self._kv_heads)):
-            if x is None:
-                continue
-            out = x if out is None else out
-            rows, strides = self._layout(x, heads)
-            out_rows, out_strides = self._layout(out, heads)
-            if out_rows != rows or seen not in (None, rows):
+        norm = self._norm
+        q_at = k_at = q_to = k_to = q_by = k_by = at = None
+        q_in = q_of = k_in = k_of = (0, 0)
+        rows = 0
+        if q is not None:
+            rows, q_in = self._layout(q, self._q_heads)
+            q_at = q_to = q.data_ptr()
+            q_of = q_in
+            if q_out is not None:
+                out_rows, q_of = self._layout(q_out, self._q_heads)
+                q_to = q_out.data_ptr()
+                if out_rows != rows:
+                    raise ValueError("q, k and their results have the same rows")
+            if norm:
+                q_by = self._weight(q_weight)
+        if k is not None:
+            k_rows, k_in = self._layout(k, self._kv_heads)
+            k_at = k_to = k.data_ptr()
+            k_of = k_in
+            if k_out is not None:
+                out_rows, k_of = self._layout(k_out, self._kv_heads)
+                k_to = k_out.data_ptr()
+            else:
+                out_rows = k_rows
+            if out_rows != k_rows or (q is not None and rows != k_rows):
                 raise ValueError("q, k and their results have the same rows")
-            if self._norm and (weight is None or weight.dtype is not self.dtype or weight.shape != (self._dim,) or not weight.is_contiguous() or
-                               weight.get_device() != self._device):
-                raise ValueError("weights are contiguous tensors [%d] of the plan's type on its device" % self._dim)
-            u.rows = seen = rows
-            setattr(u, name, x.data_ptr())
-            setattr(u, name + "_out", out.data_ptr())
-            setattr(u, name + "_weight", weight.data_ptr() if self._norm else None)
-            for prefix, pair in ((name, strides), (name + "_out", out_strides)):
-                setattr(u, prefix + "_stride_row", pair[0])
-                setattr(u, prefix + "_stride_head", pair[1])
+            rows = k_rows
+            if norm:
+                k_by = self._weight(k_weight)
         if positions is not None:
-            if positions.dtype is not torch.int32 or positions.shape != (u.rows,) or not positions.is_contiguous() or \
-                    positions.get_device() != self._device:
+            if positions.dtype is not self._int32 or positions.shape != (rows,) or not positions.is_contiguous() or positions.get_device() != self._device:
                 raise ValueError("positions are a contiguous int32 tensor [rows]")
-            u.positions = positions.data_ptr()
+            at = positions.data_ptr()
+        u = PromptRows(q_at, k_at, q_to, k_to, q_by, k_by, at, rows, q_in[0], q_in[1], k_in[0], k_in[1], q_of[0], q_of[1], k_of[0], k_of[1])
         rc = self._rotate(self._plan, u, stream)
         if rc != OK:
             raise KvcError("kvc_prompt_rotate", rc)
+
+    def _weight(self, w):
+        if w is None or w.dtype is not self.dtype or w.shape != (self._dim,) or not w.is_contiguous() or w.get_device() != self._device:
+            raise ValueError("weights are contiguous tensors [%d] of the plan's type on its device" % self._dim)
+        return w.data_ptr()
 
     def attend(self, batch, q, k, v, out, scale, lse=None, stream=None):
         """kvc_prompt_attend: q, out [rows, q_heads, 128], k, v [rows, kv_heads, 128]; lse: optional contiguous float32 [rows, q_heads]."""
@@ -721,8 +736,7 @@ class Prompt:
         if not rows == out_rows == k_rows == v_rows or batch.device != self._device:
             raise ValueError("q, k, v and out have the same rows, and the batch is on their device")
         if lse is not None:
-            import torch
-            if lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.get_device() != self._device:
+            if lse.dtype is not self._float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.get_device() != self._device:
                 raise ValueError("lse is a contiguous float32 tensor [rows, q_heads]")
         u = PromptHeads(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, rows,
                         q_strides[0], q_strides[1], k_strides[0], k_strides[1], v_strides[0], v_strides[1], out_strides[0], out_strides[1], scale)

@@ -132,6 +132,7 @@ def test_a_count_outside_the_pool():
     plan = kvc.CachePlan(kvc.F16, 1, 1, block_tokens=16, max_tokens=100, max_batch=2)
     p = kvc.CachePages(plan, 4, 2)
     p.free = torch.cat([p.free, i32(77, 77)])
+    p._free = p.free.data_ptr()
     p.free[0] = 1000
     start, tokens = i32(0, 0, 0), i32(0, 0)
     p.advance(start, tokens, None, i32(33, 30), 40, stream=stream())
