@@ -18,16 +18,21 @@ constexpr uint32_t kTop = 0x7fffffffu;       // the running sums stop here
 
 __device__ __forceinline__ uint32_t add_up(uint32_t a, uint32_t b) { return a + b < kTop ? a + b : kTop; }
 
+template <int CONTROL, int ROWS = 0xf> __device__ __forceinline__ uint32_t from_lane(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CONTROL, ROWS, 0xf, true);
+}
 // Sum of x over the workgroup's threads before this one; total: over all.
 template <int THREADS> __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t &total)
 {
-    uint32_t sum = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t up = __shfl_up(sum, d, 64);
-        if (lane_id() >= d) sum = add_up(sum, up);
-    }
-    const uint32_t up = __shfl_up(sum, 1, 64), mine = lane_id() ? up : 0;
+    uint32_t sum = x;                        // (lanes without a partner get zero)
+    sum = add_up(sum, from_lane<0x111>(sum));          // 1, 2, 4, 8 lanes before in the row of 16
+    sum = add_up(sum, from_lane<0x112>(sum));
+    sum = add_up(sum, from_lane<0x114>(sum));
+    sum = add_up(sum, from_lane<0x118>(sum));
+    sum = add_up(sum, from_lane<0x142, 0xa>(sum));     // the last lane of the first and third row for the rows behind them
+    sum = add_up(sum, from_lane<0x143, 0xc>(sum));     // that of the second for the third and fourth
+    const uint32_t mine = from_lane<0x138>(sum);       // one lane before in the wave
     if constexpr (THREADS == 64) {
         total = (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
         return mine;
