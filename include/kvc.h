@@ -568,7 +568,7 @@ void kvc_prompt_plan_free(kvc_prompt_plan_t *plan);
  */
 int32_t kvc_prompt_block_rows(const kvc_prompt_plan_t *plan, int32_t n, int32_t max_rows, int64_t rows, int32_t *waves);
 
-/* Queries and keys of `rows` rows.  Element d of head h of row r at q + r * q_stride_row + h * q_stride_head + d; strides are multiples of
+/* Queries and keys of `rows` rows, up to 2^28.  Element d of head h of row r at q + r * q_stride_row + h * q_stride_head + d; strides are multiples of
  * 8.  q or k may be NULL (the other alone), and q_out = q, k_out = k with the same strides. */
 typedef struct {
     const void *q, *k;                   /* DEVICE */

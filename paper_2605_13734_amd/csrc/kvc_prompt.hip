@@ -16,7 +16,8 @@ namespace kvc {
 constexpr long double kTwoPi = 6.283185307179586476925286766559L;
 
 constexpr int64_t kMostStride = 1 << 24;      // of rows of K and V, in elements
-constexpr int64_t kMostRows = 1 << 28;        // of an attention
+constexpr int64_t kMostRows = 1 << 28;        // of a call
+constexpr int64_t kMostThreads = 0xffffffffll;       // of a launch
 
 static bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 static bool strides_ok(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
@@ -102,8 +103,7 @@ extern "C" int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt
         !aligned(r->k_weight, 16) || !aligned(r->positions, 4)) return KVC_ERR_ARG;
     if (!strides_ok(r->q_stride_row, r->q_stride_head) || !strides_ok(r->k_stride_row, r->k_stride_head) ||
         !strides_ok(r->q_out_stride_row, r->q_out_stride_head) || !strides_ok(r->k_out_stride_row, r->k_out_stride_head)) return KVC_ERR_ARG;
-    // (a workgroup has four waves of 4 heads at least)
-    if (r->rows > kMostRows || r->rows * (f.q_heads + f.kv_heads + 6) / 16 * 256 > 0xffffffffll) return KVC_ERR_CAPACITY;
+    if (r->rows > kMostRows) return KVC_ERR_CAPACITY;
     RotateArgs a = {};
     a.q = RotateTensor{(const uint16_t *)r->q, f.norm ? (const uint16_t *)r->q_weight : nullptr, (uint16_t *)r->q_out, r->q_stride_row,
                        r->q_stride_head, r->q_out_stride_row, r->q_out_stride_head, r->q ? f.q_heads : 0, 0};
@@ -115,7 +115,9 @@ extern "C" int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt
     a.amplitude = f.rotary_dim ? f.amplitude : 1.0f;
     a.pairs = f.rotary_dim / 2;
     for (int i = 0; i < a.pairs; ++i) a.turns[i] = plan->turns[i];
-    launch_rotate(f.dtype, f.layout == KVC_ROTARY_PAIRS, f.norm != 0, a, (hipStream_t)hip_stream);
+    const long long groups = rotate_groups(a);
+    if (groups > kMostThreads / 256) return KVC_ERR_CAPACITY;
+    launch_rotate(f.dtype, f.layout == KVC_ROTARY_PAIRS, f.norm != 0, a, groups, (hipStream_t)hip_stream);
     return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
 }
 

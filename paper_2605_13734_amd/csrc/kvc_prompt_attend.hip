@@ -101,9 +101,54 @@ __device__ __forceinline__ int rows_of(const PromptArgs &a, int s, int &row0)
     return 0;
 }
 
+// Block `number` of up to 64 * EACH sequences, longest first (those with most tokens before them, over all sequences).
+template <int EACH> __device__ __forceinline__ bool find_sorted(const PromptArgs &a, int number, int size, Block &b)
+{
+    const int lane = lane_id();
+    int blocks[EACH], rows[EACH], row0[EACH], all = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int s = 64 * i + lane;
+        rows[i] = row0[i] = 0;
+        if (s < a.n) rows[i] = rows_of(a, s, row0[i]);
+        blocks[i] = (int)((unsigned)(rows[i] + size - 1) / (unsigned)size);
+        all += blocks[i];
+    }
+    all = sum_of_wave(all);
+    b.all = all;
+    if (number >= all) return false;
+    // the highest level (blocks before it in its sequence) at and above which there are more than `number` blocks
+    int low = 0, above = 0;                  // (low: more than `number`; the next that was tried: `above`, which is no more)
+    for (int step = 1 << (31 - __builtin_clz(((unsigned)a.max_rows + size - 1) / size | 1u)); step; step >>= 1) {
+        const int level = low + step;
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) sum += blocks[i] > level ? blocks[i] - level : 0;
+        sum = sum_of_wave(sum);
+        if (sum > number) low = level;
+        else above = sum;
+    }
+    // Of the last level tried above `low` no more than `number` blocks are there; of the sequences that have one at `low`, in their order:
+    int left = number - above;
+    b.first = low * size;
+    b.row0 = b.rows = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const unsigned long long have = __ballot(blocks[i] > low);
+        const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0));
+        const unsigned long long it = __ballot(blocks[i] > low && before == left);
+        if (it) {
+            const int l = __ffsll(it) - 1;
+            b.row0 = __builtin_amdgcn_readlane(row0[i], l);
+            b.rows = __builtin_amdgcn_readlane(rows[i], l);
+        }
+        left -= __popcll(have);
+    }
+    return true;
+}
+
 // Block `number` of all blocks of `size` rows, the same in all lanes; false where there are fewer.  The blocks of up to kSorted sequences
-// come longest first (those with most tokens before them, over all sequences), so that the last ones to run are short; those of more
-// sequences in the order of the sequences, each from its end.
+// come longest first, so that the last ones to run are short; those of more sequences in the order of the sequences, each from its end.
 __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number, int size, Block &b)
 {
     const int lane = lane_id();
@@ -114,50 +159,9 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
         b.first = (int)(b.all - 1 - number) * size;
         return number < b.all;
     }
-    if (a.n <= kSorted) {
-        constexpr int kEach = kSorted / 64;
-        int blocks[kEach], rows[kEach], row0[kEach], all = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int s = 64 * i + lane;
-            blocks[i] = rows[i] = row0[i] = 0;
-            if (64 * i >= a.n) continue;
-            if (s < a.n) rows[i] = rows_of(a, s, row0[i]);
-            blocks[i] = (int)((unsigned)(rows[i] + size - 1) / (unsigned)size);
-            all += blocks[i];
-        }
-        all = sum_of_wave(all);
-        b.all = all;
-        if (number >= all) return false;
-        // the highest level (blocks before it in its sequence) at and above which there are more than `number` blocks
-        int low = 0, above = 0;              // (low: more than `number`; the next that was tried: `above`, which is no more)
-        for (int step = 1 << (31 - __builtin_clz(((unsigned)a.max_rows + size - 1) / size | 1u)); step; step >>= 1) {
-            const int level = low + step;
-            int sum = 0;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) sum += blocks[i] > level ? blocks[i] - level : 0;
-            sum = sum_of_wave(sum);
-            if (sum > number) low = level;
-            else above = sum;
-        }
-        // Of the last level tried above `low` no more than `number` blocks are there; the sequences that have one at `low`, in their order:
-        int left = (int)number - above;
-        b.first = low * size;
-        b.row0 = b.rows = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            unsigned long long have = __ballot(blocks[i] > low);
-            const int many = __popcll(have);
-            if (left >= 0 && left < many) {
-                for (int k = 0; k < left; ++k) have &= have - 1;
-                const int l = __ffsll(have) - 1;
-                b.row0 = __builtin_amdgcn_readlane(row0[i], l);
-                b.rows = __builtin_amdgcn_readlane(rows[i], l);
-            }
-            left -= many;
-        }
-        return true;
-    }
+    // (2^30 blocks at most: rows are no more than 2^28, blocks no less than 64)
+    if (a.n <= 64) return find_sorted<1>(a, (int)number, size, b);
+    if (a.n <= kSorted) return find_sorted<kSorted / 64>(a, (int)number, size, b);
     b.all = INT64_MAX / 65536;
     int s = -1, at = 0, row0;
     long long before = 0;
@@ -256,28 +260,38 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
         const int place_in = wave * 4 + g;             // (of 16 tokens; lane g * 16 + i brings piece i)
         const uint32_t key_at = place_in * 2 * (uint32_t)a.k_row + 16 * (key_piece(place_in, i) & 15);
         const uint32_t value_at = place_in * 2 * (uint32_t)a.v_row + 16 * (value_piece(place_in, i) & 15);
-        auto bring = [&](u32x4 *tile, const uint16_t *from, long long stride, uint32_t lane_at, int n) {
-            if (n >= tiles) return;
-            const int half = n / TURNS & 1;
-            const char *base = (const char *)(from + (long long)n * TOKENS * stride);
-            const int have = b.rows - n * TOKENS;
-            const uint32_t to = lds_address(tile + half * kPieces + wave * 64);
+        struct Stream {
+            const char *at;                  // of its next tile
+            int n;
+        };
+        auto bring = [&](Stream &next, u32x4 *tile, long long stride, uint32_t lane_at) {
+            if (next.n >= tiles) return;
+            const int have = b.rows - next.n * TOKENS;
+            const uint32_t to = lds_address(tile + (next.n / TURNS & 1) * kPieces + wave * 64);
             if (have >= TOKENS) {
+                const char *at = next.at;
 #pragma unroll
-                for (int r = 0; r < kLoads; ++r) copy_to_lds(base + 32 * r * stride, lane_at, to + r * kPromptWaves * 1024);
+                for (int r = 0; r < kLoads; ++r, at += 32 * stride) copy_to_lds(at, lane_at, to + r * kPromptWaves * 1024);
             } else {
                 const uint32_t own = here_only(place_in), step = 32 * (uint32_t)stride;
 #pragma unroll
                 for (int r = 0; r < kLoads; ++r) {
                     const bool there = (int)own < have - r * 16;
-                    copy_to_lds(base, there ? lane_at + r * step : lane_at - own * 2 * (uint32_t)stride, to + r * kPromptWaves * 1024);
+                    copy_to_lds(next.at, there ? lane_at + r * step : lane_at - own * 2 * (uint32_t)stride, to + r * kPromptWaves * 1024);
                 }
             }
+            next.at += TURNS * TOKENS * 2 * stride;
+            next.n += TURNS;
         };
+        Stream next_key, next_value;
+        auto bring_key = [&]() { bring(next_key, keys, a.k_row, key_at); };
+        auto bring_value = [&]() { bring(next_value, values, a.v_row, value_at); };
         auto bring_first = [&]() {
-            bring(keys, k_at, a.k_row, key_at, turn);
-            bring(values, v_at, a.v_row, value_at, turn);
-            bring(keys, k_at, a.k_row, key_at, turn + TURNS);
+            next_key = {(const char *)(k_at + (long long)turn * TOKENS * a.k_row), turn};
+            next_value = {(const char *)(v_at + (long long)turn * TOKENS * a.v_row), turn};
+            bring_key();
+            bring_value();
+            bring_key();
         };
         bring_first();
         // (behind the first tiles, whose requests the compiler does not count: it waits for these, which come last)
@@ -370,8 +384,8 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
             for (int t = 0; t < TILES; ++t) asm volatile("" : "+v"(sum[t]));   // (added up here, not held apart until the products are done)
             wait_for_tiles();                        // this tile's values, the next tile's keys
             // (what the next ones overwrite has no readers behind the barrier: this tile's keys, the last tile's values)
-            bring(values, v_at, a.v_row, value_at, n + TURNS);
-            bring(keys, k_at, a.k_row, key_at, n + 2 * TURNS);
+            bring_value();
+            bring_key();
             // token 4 g + i / 4 of the lane's 16 (then 16 further), channels 16 d + 4 (i % 4) ... + 3; the lane gets tokens
             // 4 g ... 4 g + 3 of channel 16 d + i
             auto value_of = [&](int half, int d) {

@@ -30,7 +30,9 @@ struct RotateArgs {
     int past_caches, pad;          // rows are read past the caches
 };
 
-void launch_rotate(int dtype, bool neighbours, bool norm, const RotateArgs &a, hipStream_t stream);
+// Divides the rows (chunk, chunks, past_caches of the arguments) and returns the workgroups, of 256 threads.
+long long rotate_groups(RotateArgs &a);
+void launch_rotate(int dtype, bool neighbours, bool norm, const RotateArgs &a, long long groups, hipStream_t stream);
 
 // ---- attention over whole prompts ------------------------------------------------------------------
 

@@ -205,16 +205,20 @@ constexpr long long kLeastWaves = 4096;
 // 229 us; 8k rows of 40 heads, 168 MB: 30 instead of 29).
 constexpr double kCaches = 256e6;
 
-void launch_rotate(int dtype, bool neighbours, bool norm, const RotateArgs &args, hipStream_t stream)
+// How a call's rows are divided; workgroups.
+long long rotate_groups(RotateArgs &a)
 {
-    RotateArgs a = args;
     const int most = a.q.heads > a.k.heads ? a.q.heads : a.k.heads;
     auto chunks = [&](int chunk) { return (a.q.heads + chunk - 1) / chunk + (a.k.heads + chunk - 1) / chunk; };
     a.chunk = most < kMostHeads ? (most + 3) / 4 * 4 : kMostHeads;
     while (a.chunk > 4 && a.rows * chunks(a.chunk) < kLeastWaves) a.chunk -= 4;
     a.chunks = chunks(a.chunk);
     a.past_caches = (double)a.rows * (a.q.heads + a.k.heads) * 4 * kDim > kCaches;
-    const dim3 grid((unsigned)((a.rows * a.chunks + 3) / 4));
+    return (a.rows * a.chunks + 3) / 4;
+}
+void launch_rotate(int dtype, bool neighbours, bool norm, const RotateArgs &a, long long groups, hipStream_t stream)
+{
+    const dim3 grid((unsigned)groups);
     if (dtype == DT_F16) neighbours ? launch_layout<DT_F16, true>(norm, a, grid, stream) : launch_layout<DT_F16, false>(norm, a, grid, stream);
     else neighbours ? launch_layout<DT_BF16, true>(norm, a, grid, stream) : launch_layout<DT_BF16, false>(norm, a, grid, stream);
 }
