@@ -15,6 +15,8 @@ lowest bits of the base and of the offset, each by itself, and the compiler does
 kernel's arguments, indexed at run time, it took the address of a word apart into a base two bytes too far and an offset of -2, and the
 kernel read half of each of two pointers (and faulted).  A kernel's arguments have members of whole words only (CoderBatch).
 
+Kernels that copy to LDS with written-out instructions set m0 without the compiler's knowledge: nothing else in their unit may use it.
+
 A second check keeps kernels whose time depends on their waves (min_waves in kvc_quant.hip) within the
 registers that leave room for them, a third one looks for rows that are requested and waited for one at a time
 (rows_requested in kvc_tile.h).
@@ -87,6 +89,24 @@ def spilling_kernels(asm_path):
         if n:
             out.append((k, n))
     return out
+
+
+def other_m0_users(asm_path):
+    """[(kernel symbol, instruction)] that name m0 outside written-out copies to LDS, in a unit that has such copies: they set m0 and the compiler does
+    not know it."""
+    text = open(asm_path).read()
+    if "global_load_lds" not in text:
+        return []
+    hits, cur, written = [], None, False
+    for line in text.split("\n"):
+        m = re.match(r"^(\w+):", line)
+        if m:
+            cur = m.group(1)
+        if "#ASMSTART" in line or "#ASMEND" in line:
+            written = "#ASMSTART" in line
+        elif not written and re.search(r"\bm0\b", line.split(";")[0]):
+            hits.append((cur, line.strip()))
+    return hits
 
 
 # (kernel symbol, registers): six waves per SIMD for the compress kernels of one pass for bf16 rows that are not
@@ -179,6 +199,9 @@ def _compile(job):
     if off:
         raise RuntimeError("%s: scalar loads that are not at whole words (a kernel argument with a member of fewer than four "
                            "bytes?):\n%s" % (name, "\n".join("  %s: %s" % h for h in off[:20])))
+    m0 = other_m0_users(asm)
+    if m0:
+        raise RuntimeError("%s: m0 used beside written-out copies to LDS:\n%s" % (name, "\n".join("  %s: %s" % h for h in m0[:20])))
     over = over_budget(asm)
     if over:
         raise RuntimeError("%s: more registers than the kernel's waves leave room for:\n%s" % (

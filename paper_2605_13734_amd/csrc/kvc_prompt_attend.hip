@@ -8,7 +8,6 @@
 // sum belong to the lanes that hold its results.
 // Softmax: running maximum and sum per row in 32 bits, base 2.  Lanes look for a maximum of their own tokens only; the four lanes of a row
 // meet when one of them has found a score more than 2^kSlack above the maximum that the row's weights refer to (or none was there yet).
-// Weights are kept as 2^(kBias + score - maximum) <= 2^15, inside the half type, so that weights down to 2^-39 of the largest count.
 //
 // What a row does not see must not matter whatever it holds: scores are replaced (not added to) where tokens are behind the row, but a
 // weight of zero times a value that is NaN or infinite is NaN.  That is looked for once, in the results: a block that has one that is no
@@ -30,7 +29,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kGroup = 32;                   // tokens of a product with values
-constexpr float kSlack = 7.0f, kBias = 8.0f;
+constexpr float kSlack = 7.0f;
+// Weights are 2^(bias + score - maximum): fp16 ones as large as the type allows, so that those down to 2^-39 of the largest count; bf16 ones small,
+// so that sums of a million times the largest values stay inside 32 bits (values below 2^-106 lose bits for it).
+template <int DT> constexpr float kBias = DT == DT_F16 ? 8.0f : -20.0f;
 constexpr float kNone = -__builtin_inff();
 constexpr int kSorted = 256;                 // sequences of a call whose blocks are taken longest first
 
@@ -360,7 +362,7 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
                         const float from = now == kNone ? 0.0f : now;
                         const float by = __builtin_amdgcn_exp2f(top[t] - from);
                         top[t] = now;
-                        shift[t] = kBias - from;
+                        shift[t] = kBias<DT> - from;
                         sum[t] *= by;
 #pragma unroll
                         for (int d = 0; d < 8; ++d) out[t][d] *= by;
@@ -436,7 +438,7 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 top[t] = kNone;
-                shift[t] = kBias;
+                shift[t] = kBias<DT>;
                 sum[t] = 0.0f;
 #pragma unroll
                 for (int d = 0; d < 8; ++d) out[t][d] = f32x4{0, 0, 0, 0};
@@ -473,7 +475,7 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
                         const float now = fmaxf(top[t], other[0]), from = now == kNone ? 0.0f : now;
                         const float by = __builtin_amdgcn_exp2f(top[t] - from), other_by = __builtin_amdgcn_exp2f(other[0] - from);
                         top[t] = now;
-                        shift[t] = kBias - from;
+                        shift[t] = kBias<DT> - from;
                         sum[t] = sum[t] * by + other[1] * other_by;
 #pragma unroll
                         for (int d = 0; d < 8; ++d) out[t][d] = out[t][d] * by + results[k * kResults + (t * 8 + d) * kPromptWaves * 64] * other_by;

@@ -97,6 +97,19 @@ def test_weights_far_below_the_largest():
     assert c.out[-1].min() > 0.1
 
 
+@pytest.mark.parametrize("value", [3.3e38, -1e37, 1e30, 1e-30])
+def test_large_and_small_values(value):
+    """bf16: sums of thousands of the largest values, and of small ones, stay inside 32 bits; so do scores that rise."""
+    for rising in (False, True):
+        c = Case([5000], 1, 1, True, seed=6)
+        c.q[:] = 1
+        c.k[:] = 0 if not rising else (torch.linspace(0.0, 0.5, 5000, device=DEVICE)[:, None, None]).bfloat16()
+        c.v[:] = value
+        c.run()
+        assert ((c.out.double() / c.v.double() - 1).abs() <= 2.0 ** -7).all()
+        c.check()
+
+
 @pytest.mark.parametrize("bf16", [False, True])
 def test_equal_values_give_themselves(bf16):
     """A mean of equal numbers: weights and their sum have the same roundings but for half a step of each."""
