@@ -513,19 +513,21 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
 // ---- which kernel ---------------------------------------------------------------------------------
 
 // The kernels, and what a call takes with each, us: the longest sequence's tiles one after the other (per 64 tokens), the products at the rate of a
-// full chip, what a workgroup takes apart from them, and the launch; fitted to 20 calls of 1 to 200 sequences of 30 to 32k tokens, 8 to 64 heads.
-//   64 rows    37 tokens x 64 heads 6.2 us, 64 x 100 x 32 42, 8 x 512 x 32 42, 1024 x 64 32      tiles of 32 tokens, four workgroups per compute unit
-//   64 shared  512 x 32 13.5 (one set of waves 16.4), 1024 x 32 21.2 (28.0), 4096 x 8 63 (93)   two sets of waves take turns: too few rows for the chip
-//   128 rows   2048 x 64 85 (64 rows: 99), 4096 x 32 157 (178), 8 x 1024 x 32 100 (105)            tiles of 32 tokens, three workgroups
-//   192 rows   8192 x 32 509 (128 rows: 511), 32768 x 64 15.1 ms (16.1)                              tiles of 64 tokens, two workgroups: K and V are read least
+// full chip, what a workgroup takes apart from them, and the launch.  Times of calls in the sizes, us, tokens x heads:
+//   64 rows    37 x 64 6.2, 64 x 100 x 32 38, 1024 x 64 31                                          tiles of 32 tokens, four workgroups per compute unit
+//   64 shared  512 x 32 13.3 (one set of waves 16.4), 1024 x 32 21.3 (28.0), 4096 x 8 62 (93)   two sets of waves take turns: too few rows for the chip
+//   128 rows   2048 x 64 80 (64 rows: 99), 4096 x 32 152 (178), 8 x 1024 x 32 96 (105)             tiles of 32 tokens, three workgroups
+//   192 rows   8192 x 32 490 (128 rows: 500), 32768 x 64 14.8 ms (15.4)                              tiles of 64 tokens, two workgroups: K and V are read least
+// The numbers are fitted to the choice among 150 measured calls (1 to 128 sequences of 16 to 32k tokens, 8 to 64 heads, bf16): its
+// time is 0.4 % above the least in the mean, 8 % at worst; of 110 others (fp16) 0.6 and 12 % (profiles/prompt_block_rows.txt).
 struct Kernel {
     int tiles, tokens, turns;
     float per_64, rate, group, launch;       // us, TFLOP/s, us, us
 };
-constexpr Kernel kKernels[] = {{1, 32, 1, 1.38f, 910.0f, 0.0076f, 5.0f},
-                               {1, 32, 2, 0.82f, 860.0f, 0.0150f, 6.0f},
-                               {2, 32, 1, 1.80f, 1120.0f, 0.0160f, 5.0f},
-                               {3, 64, 1, 1.97f, 1190.0f, 0.0250f, 5.0f}};
+constexpr Kernel kKernels[] = {{1, 32, 1, 1.29f, 920.0f, 0.0069f, 5.0f},
+                               {1, 32, 2, 0.82f, 810.0f, 0.0116f, 5.6f},
+                               {2, 32, 1, 1.80f, 1150.0f, 0.0137f, 5.2f},
+                               {3, 64, 1, 1.80f, 1185.0f, 0.0244f, 6.5f}};
 constexpr int kKinds = sizeof(kKernels) / sizeof(kKernels[0]);
 
 // Blocks of `size` rows that a call has at most: what the sequences' number and bound allow, or their rows in all.
@@ -538,12 +540,14 @@ static int kernel_for(const PromptArgs &a)
 {
     const double heads = (double)a.kv_heads * a.per_kv, longest = a.max_rows < a.rows ? a.max_rows : (double)a.rows;
     const double rows = (double)a.max_rows * a.n < a.rows ? (double)a.max_rows * a.n : (double)a.rows;
+    // (of equal sequences; of ragged ones an estimate between those of the longest and of the mean)
+    const double pairs = rows * (longest + rows / a.n) / 4;
     int best = 0;
     double least = 0.0;
     for (int k = 0; k < kKinds; ++k) {
         const Kernel &c = kKernels[k];
         const double chain = c.per_64 * longest / 64, groups = heads * most_blocks(a, 16 * c.tiles * kPromptWaves);
-        const double work = 4.0 * kDim * heads * rows * longest / 2 / c.rate * 1e-6 + c.group * groups;
+        const double work = 4.0 * kDim * heads * pairs / c.rate * 1e-6 + c.group * groups;
         const double time = c.launch + sqrt(chain * chain + work * work);
         if (k == 0 || time < least) {
             best = k;

@@ -13,7 +13,7 @@ from prompt_util import DEVICE, DIM, check_attention, i32, own_type, stream, typ
 pytestmark = pytest.mark.gpu
 SCALE = DIM ** -0.5
 # (rows of a workgroup, waves): (KV heads, query heads per KV head, rows of the tensors)
-KERNELS = {(64, 4): (32, 2, 700), (64, 8): (1, 2, 900), (128, 4): (40, 2, 2000), (192, 4): (32, 2, 4000)}
+KERNELS = {(64, 4): (32, 2, 700), (64, 8): (1, 2, 900), (128, 4): (48, 2, 2600), (192, 4): (32, 2, 10000)}
 
 
 class Case:

@@ -146,7 +146,7 @@ def test_block_rows(lib):
     p = plan(kv_heads=8, q_heads=64, max_batch=300)
     assert p.block_rows(1, 37, 37) == (64, 4) and p.block_rows(200, 30, 6000) == (64, 4)
     few = plan(kv_heads=8, q_heads=32)
-    assert few.block_rows(1, 1024, 1024) == few.block_rows(1, 2048, 2048) == (64, 8)
+    assert few.block_rows(1, 512, 512) == few.block_rows(1, 1024, 1024) == (64, 8)
     assert p.block_rows(1, 2048, 2048)[0] == 128 and p.block_rows(1, 32768, 32768) == (192, 4)
     one = plan(kv_heads=1, q_heads=1)
     assert one.block_rows(1, 8192, 8192) == (64, 8)
