@@ -497,7 +497,7 @@ int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch,
  * KVC_DEV_BAD_ROW; or where it needs more pages and those left by the sequences before it (left out or not) are too few:
  * KVC_DEV_NO_PAGE.  A page outside [0, num_pages) in the stack or among the given ones is passed on as -1: KVC_DEV_BAD_BLOCK.
  * Up to KVC_MOST_ADVANCING sequences.  Arrays do not overlap; slots is 8-byte aligned.  Like the other calls it is enqueued on hip_stream
- * and may be captured.
+ * and may be captured; calls on the same tables and free pages must be in stream order.
  */
 #define KVC_MOST_ADVANCING 4096
 typedef struct {
@@ -574,7 +574,8 @@ typedef struct {
     const void *q, *k;                   /* DEVICE */
     void *q_out, *k_out;                 /* DEVICE */
     const void *q_weight, *k_weight;     /* DEVICE, head_dim values; not looked at where the plan does not norm */
-    const int32_t *positions;            /* DEVICE, rows; rows with a position below zero are left as they are */
+    const int32_t *positions;            /* DEVICE, rows (NULL where the plan does not rotate); rows with a position below zero are left as
+                                            they are */
     int64_t rows, q_stride_row, q_stride_head, k_stride_row, k_stride_head, q_out_stride_row, q_out_stride_head, k_out_stride_row,
         k_out_stride_head;
 } kvc_prompt_rows;
@@ -594,7 +595,7 @@ typedef struct {
     void *out;                           /* DEVICE */
     float *lse;                          /* DEVICE or NULL: log(sum of exp(scores)), for joining with other attention */
     int64_t rows, q_stride_row, q_stride_head, k_stride_row, k_stride_head, v_stride_row, v_stride_head, out_stride_row, out_stride_head;
-    float scale;                         /* of the scores, usually 1 / sqrt(head_dim); -1e38 to 1e38 */
+    float scale;                         /* of the scores, usually 1 / sqrt(head_dim); 0, or 1e-37 to 1e38 in magnitude */
 } kvc_prompt_heads;
 
 /*

@@ -153,7 +153,8 @@ extern "C" int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt
         !aligned(h.lse, 4)) return KVC_ERR_ARG;
     if (!strides_ok(h.q_stride_row, h.q_stride_head) || !strides_ok(h.k_stride_row, h.k_stride_head) ||
         !strides_ok(h.v_stride_row, h.v_stride_head) || !strides_ok(h.out_stride_row, h.out_stride_head)) return KVC_ERR_ARG;
-    if (!(h.scale >= -1e38f && h.scale <= 1e38f)) return KVC_ERR_ARG;
+    // (smaller factors are subnormal numbers, which may count as zero)
+    if (!(fabsf(h.scale) <= 1e38f) || (h.scale != 0.0f && fabsf(h.scale) < 1e-37f)) return KVC_ERR_ARG;
     // (offsets of the 64 rows of a tile are 32-bit numbers above zero)
     if (h.k_stride_row < 0 || h.v_stride_row < 0 || h.k_stride_row > kMostStride || h.v_stride_row > kMostStride) return KVC_ERR_UNSUPPORTED;
     PromptArgs a = {};

@@ -84,7 +84,7 @@ template <int DT, bool NEIGHBOURS, bool NORM> __global__ __launch_bounds__(256) 
     const long long unit = (long long)blockIdx.x * 4 + wave_id();
     const long long row = unit / a.chunks;
     if (row >= a.rows) return;
-    const int position = a.pairs ? __builtin_amdgcn_readfirstlane(a.positions[row]) : 0;
+    const int position = a.positions ? __builtin_amdgcn_readfirstlane(a.positions[row]) : 0;
     if (position < 0) return;
     const int q_chunks = (a.q.heads + a.chunk - 1) / a.chunk;
     const int part = (int)(unit - row * a.chunks);

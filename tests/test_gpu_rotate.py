@@ -93,6 +93,18 @@ def test_in_place_one_at_a_time_and_left_as_they_are(layout, eps):
     prompt.rotate(None, None, None, stream=stream())
 
 
+def test_norms_alone_leave_rows_too():
+    """Without a rotation positions are optional; given, they still say which rows are left as they are."""
+    prompt, q, k, w, _ = world(2, 2, False, 6, 5, rotary_dim=0, eps=1e-6)
+    at, outs = i32(3, -1, 0, -7, 9, 1), []
+    for positions in (None, at):
+        outs.append((torch.full_like(q, 77.0), torch.full_like(k, 77.0)))
+        prompt.rotate(q, k, positions, *outs[-1], *w, stream=stream())
+    check(*outs[0], q, k, w, at, False, rotary_dim=0, eps=1e-6)
+    for x, y in zip(*outs):
+        assert torch.equal(x[at >= 0], y[at >= 0]) and (y[at < 0] == 77).all()
+
+
 def test_layouts():
     """Heads before rows, in and out; nothing between the heads is written."""
     prompt, q, k, w, at = world(2, 2, False, 70, 6, eps=1e-6)

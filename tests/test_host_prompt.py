@@ -131,7 +131,7 @@ def test_attention_refused(lib):
     for kw in [dict(n=-1), dict(max_rows=-1), dict(rows=-1), dict(start=None), dict(status=None), dict(q=None), dict(k=None), dict(v=None),
                dict(out=None), dict(start=AT + 2), dict(status=AT + 1), dict(q=AT + 8), dict(k=AT + 8), dict(v=AT + 8), dict(out=AT + 8), dict(lse=AT + 2),
                dict(q_stride_row=1), dict(k_stride_head=12), dict(v_stride_row=2), dict(out_stride_head=4), dict(scale=math.nan),
-               dict(scale=math.inf), dict(scale=-2e38)]:
+               dict(scale=math.inf), dict(scale=-2e38), dict(scale=1e-38), dict(scale=-1e-44)]:
         assert call(**kw) == -1, kw
     assert call(n=4) == -3 and call(rows=(1 << 28) + 1) == -3
     for kw in [dict(k_stride_row=-256), dict(v_stride_row=-8), dict(k_stride_row=(1 << 24) + 8), dict(v_stride_row=1 << 40)]:
