@@ -564,7 +564,7 @@ void kvc_prompt_plan_free(kvc_prompt_plan_t *plan);
  * Rows that a workgroup of kvc_prompt_attend has in a call with these bounds (`rows` of the tensors): 64, 128 or 192, the size for which the time
  * of such a call is estimated to be the least; *waves (or NULL): 4, or 8 where two sets of waves share them; 0 where there is nothing to do or the
  * call is refused.  The lengths are on the device, so max_rows stands for them: with a bound far above the lengths blocks are taken that are
- * large for the call (64 prompts of 100 tokens, 32 heads: 42 us with blocks of 64, 61 with 192).
+ * large for the call (64 prompts of 100 tokens, 32 heads: 38 us with blocks of 64, 61 with 192).
  */
 int32_t kvc_prompt_block_rows(const kvc_prompt_plan_t *plan, int32_t n, int32_t max_rows, int64_t rows, int32_t *waves);
 

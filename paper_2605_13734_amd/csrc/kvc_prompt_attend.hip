@@ -1,6 +1,6 @@
 // Causal attention over whole prompts, packed one after the other: o_i = sum_{j <= i} softmax_j(scale * q_i . k_j) v_j.
 //
-// A workgroup has a block of rows of one query head, its waves divide the rows; tiles of 64 tokens of K and V go through LDS and are read
+// A workgroup has a block of rows of one query head, its waves divide the rows; tiles of 32 or 64 tokens of K and V go through LDS and are read
 // by all waves.  The scores' product has the keys as rows and the queries as columns (16 x 16 x 32): a lane then holds the scores of
 // one row and of the tokens 4 g ... 4 g + 3 of a tile of 16 (lane = 16 g + i, row i), two of which are, as weights, the operand that the
 // second product takes for 32 tokens: nothing moves between lanes.  The values' operand holds the same tokens, read from LDS with the
@@ -13,6 +13,9 @@
 // weight of zero times a value that is NaN or infinite is NaN.  That is looked for once, in the results: a block that has one that is no
 // finite number is done again with the values of the tiles that some rows see and others do not taken as zero where they are
 // not finite, and as NaN by the rows that see them.
+//
+// What bounds it: long prompts the matrix products beside the softmax's instructions (32k tokens, 64 heads: 14.8 ms, 1190 TFLOP/s; 8k, 32 heads: 0.50 ms,
+// 1110), many short ones the instructions that find a block and start and end it, single short ones latencies (37 tokens: 5.6 us in a graph).
 #include "kvc_prompt_internal.h"
 #include "../../include/kvc.h"
 
@@ -64,12 +67,6 @@ __device__ __forceinline__ float sum_of_row(float x)
     auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
-// The first lane's value, as one that the compiler knows to be the same in all lanes.
-__device__ __forceinline__ long long first_lane(long long x)
-{
-    const uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)x), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32));
-    return (long long)((uint64_t)high << 32 | low);
-}
 template <int N> __device__ __forceinline__ int turned_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, 0x120 + N, 0xf, 0xf, true); }
 __device__ __forceinline__ int sum_of_wave(int x)
 {
@@ -88,7 +85,7 @@ __device__ __forceinline__ int sum_of_wave(int x)
 struct Block {
     int row0, rows;                          // of the sequence
     int first;                               // of the block, in the sequence
-    long long all;                           // blocks of the call, where that is known
+    long long all;                           // blocks of the call
 };
 
 // The workgroup that reports.
@@ -164,31 +161,48 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
     // (2^30 blocks at most: rows are no more than 2^28, blocks no less than 64)
     if (a.n <= 64) return find_sorted<1>(a, (int)number, size, b);
     if (a.n <= kSorted) return find_sorted<kSorted / 64>(a, (int)number, size, b);
-    b.all = INT64_MAX / 65536;
-    int s = -1, at = 0, row0;
-    long long before = 0;
-    for (int i = 0; i < a.n; i += 64) {
-        const int mine = i + lane < a.n ? (int)((unsigned)(rows_of(a, i + lane, row0) + size - 1) / (unsigned)size) : 0;
-        long long sum = mine;
+    // kSorted sequences at a time, whose sum says whether the block is among them (300 prompts of 30 tokens, 32 heads: 70 us, 200: 42; 700: 216.  64
+    // sequences at a time: 72 and 247)
+    constexpr int kEach = kSorted / 64;
+    bool found = false;
+    b.row0 = b.rows = b.first = 0;
+    b.all = 0;
+    for (int begin = 0; begin < a.n; begin += kSorted) {
+        int blocks[kEach], rows[kEach], row0[kEach], all = 0;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const long long up = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += up;
+        for (int i = 0; i < kEach; ++i) {
+            const int s = begin + 64 * i + lane;
+            rows[i] = row0[i] = 0;
+            if (s < a.n) rows[i] = rows_of(a, s, row0[i]);
+            blocks[i] = (int)((unsigned)(rows[i] + size - 1) / (unsigned)size);
+            all += blocks[i];
         }
-        const unsigned long long have = __ballot(before + sum > number);
-        if (have && s < 0) {
-            const int l = __ffsll(have) - 1;
-            s = i + l;
-            at = __builtin_amdgcn_readfirstlane((int)(before + __shfl(sum, l, 64) - 1 - number));
-            if (!first_group()) break;         // (the first workgroup looks at all sequences for its reports)
+        all = sum_of_wave(all);
+        if (!found && number < b.all + all) {
+            int left = (int)(number - b.all);
+            found = true;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                int sum = blocks[i];         // of the sequences up to the lane's
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int up = __shfl_up(sum, d, 64);
+                    if (lane >= d) sum += up;
+                }
+                const unsigned long long behind = __ballot(sum > left);
+                const int many = __builtin_amdgcn_readlane(sum, 63);
+                if (left >= 0 && behind) {
+                    const int l = __ffsll(behind) - 1;
+                    b.row0 = __builtin_amdgcn_readlane(row0[i], l);
+                    b.rows = __builtin_amdgcn_readlane(rows[i], l);
+                    b.first = (__builtin_amdgcn_readlane(sum, l) - 1 - left) * size;
+                    left = -1;
+                } else if (left >= 0) left -= many;
+            }
         }
-        before += first_lane(__shfl(sum, 63, 64));
+        b.all += all;
     }
-    if (s < 0) return false;
-    b.rows = __builtin_amdgcn_readfirstlane(rows_of(a, s, row0));
-    b.row0 = __builtin_amdgcn_readfirstlane(row0);
-    b.first = at * size;
-    return true;
+    return found;
 }
 
 template <bool B> struct BoolConst {
@@ -235,8 +249,8 @@ __device__ __forceinline__ void wait_for_tiles()
     __syncthreads();
 }
 
-// TILES: of 16 rows per wave.  TOKENS: of a tile of K and V in LDS, 64 or 32.  TURNS: sets of kPromptWaves waves, each of which has all rows of the block and takes every TURNS-th tile;
-// the second set's results are joined to the first's in the end.
+// TILES: of 16 rows per wave.  TOKENS: of a tile of K and V in LDS, 64 or 32.  TURNS: sets of kPromptWaves waves, each of which has all rows of
+// the block and takes every TURNS-th tile; the second set's results are joined to the first's in the end.
 template <int DT, int TILES, int TOKENS, int TURNS>
 __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES == 1 ? 4 : TOKENS == 32 ? 3 : 2) void prompt_kernel(PromptArgs a)
 {

@@ -5,8 +5,8 @@
 //
 // All in 32 bits, rounded once as it is stored.  Bound by HBM where there are many rows (every element is read and written once) and by
 // latency where there are few.  A wave has one row and a run of its heads, four heads at a time, 16 lanes per head and 8 channels
-// per lane: cosines and sines are made once per row and wave, the mean of a head inside a row of lanes.  32k rows of 72 heads: 191 us, 6.3 TB/s (the fastest
-// copy found on this card 6.5); 32 rows 3.3 us in a graph, most of it the launch.
+// per lane: cosines and sines are made once per row and wave, the mean of a head inside a row of lanes.  32k rows of 72 heads: 192 us, 6.3 TB/s (the
+// fastest copy found on this card 6.5); 32 rows 3.3 us in a graph, most of it the launch.
 //
 // Angles are fixed-point numbers of 2^-64 of a turn: a position times a frequency's part of a turn, modulo a turn, is one integer product
 // whose upper word is the angle, exact to 2^-32 of a turn wherever the position is (in 32-bit floating point a position of 10^6 would be
@@ -197,11 +197,11 @@ template <int DT, bool NEIGHBOURS> static void launch_layout(bool norm, const Ro
     else rotate_kernel<DT, NEIGHBOURS, false><<<grid, 256, 0, stream>>>(a);
 }
 
-// Heads of a row that a wave takes: up to 16, which are 4 KB in a row for each of a workgroup's waves (32k rows of 72 heads: 191 us, with all of a row
+// Heads of a row that a wave takes: up to 16, which are 4 KB in a row for each of a workgroup's waves (32k rows of 72 heads: 192 us, with all of a row
 // in one wave 214, with 8 heads 225); fewer while there are not that many waves (1k rows of 40 heads: 5.5 us, with waves of 4 heads 7.9).
 constexpr int kMostHeads = 16;
 constexpr long long kLeastWaves = 4096;
-// Bytes read and written beyond which rows are read past the caches, which cannot hold them for anyone (32k rows of 72 heads, 1.2 GB: 191 instead of
+// Bytes read and written beyond which rows are read past the caches, which cannot hold them for anyone (32k rows of 72 heads, 1.2 GB: 192 instead of
 // 229 us; 8k rows of 40 heads, 168 MB: 30 instead of 29).
 constexpr double kCaches = 256e6;
 

@@ -57,9 +57,9 @@ def test_heads(kv_heads, per_kv, bf16):
 def test_many_sequences():
     """More sequences than are sorted by their lengths, empty ones among them."""
     g = np.random.default_rng(5)
-    for n in (255, 256, 257, 700):
+    for n in (63, 64, 65, 255, 256, 257, 512, 700, 1500):
         lengths = g.integers(0, 9, n).tolist()
-        lengths[n // 2], lengths[-1] = 150, 20
+        lengths[n // 2], lengths[-1], lengths[0] = 150, 20, 70
         Case(lengths, 1, 2, n % 2 == 0, seed=n, behind=1).run().check()
 
 
