@@ -161,46 +161,44 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
     // (2^30 blocks at most: rows are no more than 2^28, blocks no less than 64)
     if (a.n <= 64) return find_sorted<1>(a, (int)number, size, b);
     if (a.n <= kSorted) return find_sorted<kSorted / 64>(a, (int)number, size, b);
-    // kSorted sequences at a time, whose sum says whether the block is among them (300 prompts of 30 tokens, 32 heads: 70 us, 200: 42; 700: 216.  64
-    // sequences at a time: 72 and 247)
-    constexpr int kEach = kSorted / 64;
+    // kSorted sequences at a time, whose sum says whether the block is among them (300 prompts of 30 tokens, 32 heads: 75 us, 200: 42; 700: 231.  With
+    // the starts held in registers 70 and 216, but one prompt of 8k tokens 0.5 % more, for the registers)
     bool found = false;
     b.row0 = b.rows = b.first = 0;
     b.all = 0;
     for (int begin = 0; begin < a.n; begin += kSorted) {
-        int blocks[kEach], rows[kEach], row0[kEach], all = 0;
+        int sums = 0, row0;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int s = begin + 64 * i + lane;
-            rows[i] = row0[i] = 0;
-            if (s < a.n) rows[i] = rows_of(a, s, row0[i]);
-            blocks[i] = (int)((unsigned)(rows[i] + size - 1) / (unsigned)size);
-            all += blocks[i];
-        }
-        all = sum_of_wave(all);
-        if (!found && number < b.all + all) {
+        for (int i = 0; i < kSorted; i += 64)
+            if (begin + i + lane < a.n) sums += (unsigned)(rows_of(a, begin + i + lane, row0) + size - 1) / (unsigned)size;
+        sums = sum_of_wave(sums);
+        if (!found && number < b.all + sums) {
             int left = (int)(number - b.all);
             found = true;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                int sum = blocks[i];         // of the sequences up to the lane's
-#pragma unroll
+#pragma clang loop unroll(disable)
+            for (int i = 0; i < kSorted && left >= 0; i += 64) {
+                const int s = begin + i + lane;
+                int rows = 0;
+                row0 = 0;
+                if (s < a.n) rows = rows_of(a, s, row0);
+                int sum = (int)((unsigned)(rows + size - 1) / (unsigned)size);         // of the sequences up to the lane's
+#pragma clang loop unroll(disable)
                 for (int d = 1; d < 64; d <<= 1) {
                     const int up = __shfl_up(sum, d, 64);
                     if (lane >= d) sum += up;
                 }
                 const unsigned long long behind = __ballot(sum > left);
                 const int many = __builtin_amdgcn_readlane(sum, 63);
-                if (left >= 0 && behind) {
+                if (behind) {
                     const int l = __ffsll(behind) - 1;
-                    b.row0 = __builtin_amdgcn_readlane(row0[i], l);
-                    b.rows = __builtin_amdgcn_readlane(rows[i], l);
+                    b.row0 = __builtin_amdgcn_readlane(row0, l);
+                    b.rows = __builtin_amdgcn_readlane(rows, l);
                     b.first = (__builtin_amdgcn_readlane(sum, l) - 1 - left) * size;
                     left = -1;
-                } else if (left >= 0) left -= many;
+                } else left -= many;
             }
         }
-        b.all += all;
+        b.all += sums;
     }
     return found;
 }
