@@ -222,6 +222,10 @@ extern "C" int kvc_cache_advance(const kvc_cache_plan_t *plan, const kvc_cache_s
                           (const void *)t.new_start, (const void *)t.tokens, (const void *)t.positions, (const void *)dev_status})
         if (!aligned(p, 4)) return KVC_ERR_ARG;
     if (!aligned(t.slots, 8) || t.table_stride < (t.max_tokens + f.block_tokens - 1) / f.block_tokens) return KVC_ERR_ARG;
+    // (what is written at once is not what other workgroups still read)
+    for (const void *p : {(const void *)t.new_start, (const void *)t.tokens, (const void *)t.positions, (const void *)t.slots})
+        if (p && (p == t.held || p == t.kept || p == t.fresh)) return KVC_ERR_ARG;
+    if (t.new_start == t.tokens) return KVC_ERR_ARG;
     AdvanceArgs a = {};
     a.held = t.held;
     a.kept = t.kept;

@@ -21,6 +21,11 @@ constexpr int64_t kMostThreads = 0xffffffffll;       // of a launch
 
 static bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 static bool strides_ok(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
+// Results apart from the input, or in its place.
+static bool in_place_ok(const void *in, const void *out, int64_t rows, int64_t heads, int64_t row, int64_t head, int64_t out_row, int64_t out_head)
+{
+    return in != out || ((rows < 2 || row == out_row) && (heads < 2 || head == out_head));
+}
 
 // The part of a turn that a position adds, in 2^-64 of a turn.
 static uint64_t turns_of(double radians)
@@ -103,6 +108,10 @@ extern "C" int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt
         !aligned(r->k_weight, 16) || !aligned(r->positions, 4)) return KVC_ERR_ARG;
     if (!strides_ok(r->q_stride_row, r->q_stride_head) || !strides_ok(r->k_stride_row, r->k_stride_head) ||
         !strides_ok(r->q_out_stride_row, r->q_out_stride_head) || !strides_ok(r->k_out_stride_row, r->k_out_stride_head)) return KVC_ERR_ARG;
+    if ((r->q && (!in_place_ok(r->q, r->q_out, r->rows, f.q_heads, r->q_stride_row, r->q_stride_head, r->q_out_stride_row, r->q_out_stride_head) ||
+                  r->q_out == r->k)) ||
+        (r->k && (!in_place_ok(r->k, r->k_out, r->rows, f.kv_heads, r->k_stride_row, r->k_stride_head, r->k_out_stride_row, r->k_out_stride_head) ||
+                  r->k_out == r->q)) || (r->q && r->k && r->q_out == r->k_out)) return KVC_ERR_ARG;
     if (r->rows > kMostRows) return KVC_ERR_CAPACITY;
     RotateArgs a = {};
     a.q = RotateTensor{(const uint16_t *)r->q, f.norm ? (const uint16_t *)r->q_weight : nullptr, (uint16_t *)r->q_out, r->q_stride_row,
@@ -153,6 +162,8 @@ extern "C" int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt
         !aligned(h.lse, 4)) return KVC_ERR_ARG;
     if (!strides_ok(h.q_stride_row, h.q_stride_head) || !strides_ok(h.k_stride_row, h.k_stride_head) ||
         !strides_ok(h.v_stride_row, h.v_stride_head) || !strides_ok(h.out_stride_row, h.out_stride_head)) return KVC_ERR_ARG;
+    if (h.out && (h.out == h.k || h.out == h.v ||
+                  !in_place_ok(h.q, h.out, h.rows, f.q_heads, h.q_stride_row, h.q_stride_head, h.out_stride_row, h.out_stride_head))) return KVC_ERR_ARG;
     // (smaller factors are subnormal numbers, which may count as zero)
     if (!(fabsf(h.scale) <= 1e38f) || (h.scale != 0.0f && fabsf(h.scale) < 1e-37f)) return KVC_ERR_ARG;
     // (offsets of the 64 rows of a tile are 32-bit numbers above zero)

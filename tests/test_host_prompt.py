@@ -92,10 +92,11 @@ def test_frequencies_refused(lib):
 
 # Device addresses that nothing is read from: the calls below are refused before a launch, or end at the device that is not there.
 AT = 1 << 20
+ON, OFF = 2 * AT, 3 * AT                    # others
 
 
 def rows_of(**kw):
-    base = dict(q=AT, k=AT, q_out=AT, k_out=AT, q_weight=AT, k_weight=AT, positions=AT, rows=5, q_stride_row=1024, q_stride_head=128,
+    base = dict(q=AT, k=ON, q_out=AT, k_out=ON, q_weight=AT, k_weight=AT, positions=AT, rows=5, q_stride_row=1024, q_stride_head=128,
                 k_stride_row=256, k_stride_head=128, q_out_stride_row=1024, q_out_stride_head=128, k_out_stride_row=256, k_out_stride_head=128)
     return kvc.PromptRows(**{**base, **kw})
 
@@ -106,20 +107,23 @@ def test_rotation_refused(lib):
     assert lib.kvc_prompt_rotate(plain._h, None, None) == -1 and call(None) == -1
     for kw in [dict(rows=-1), dict(q_out=None), dict(k_out=None), dict(q_weight=None), dict(k_weight=None), dict(positions=None), dict(q=AT + 8),
                dict(k=AT + 2), dict(q_out=AT + 4), dict(k_out=AT + 8), dict(q_weight=AT + 2), dict(positions=AT + 2), dict(q_stride_row=1020),
-               dict(k_stride_head=4), dict(q_out_stride_head=129), dict(k_out_stride_row=-4)]:
+               dict(k_stride_head=4), dict(q_out_stride_head=129), dict(k_out_stride_row=-4),
+               # in place with other strides, over the other input, into one tensor
+               dict(q_out_stride_row=2048), dict(q_out_stride_head=256), dict(k_stride_row=512), dict(q_out=ON), dict(k_out=AT), dict(q_out=OFF, k_out=OFF)]:
         assert call(normed, **kw) == -1, kw
     assert call(normed, rows=1 << 31) == -3
     # nothing to do
     assert call(normed, rows=0) == 0 and call(plain, q=None, k=None) == 0
     if not torch.cuda.is_available():
         for p, kw in [(plain, dict(q_weight=None, k_weight=None)), (still, dict(positions=None)), (normed, dict(q=None, q_out=None, q_weight=None)),
-                      (normed, dict(k=None, k_out=None, k_weight=None)), (plain, dict(q_stride_row=-1024))]:
+                      (normed, dict(k=None, k_out=None, k_weight=None)), (plain, dict(q_stride_row=-1024, q_out_stride_row=-1024)),
+                      (plain, dict(q_out=OFF, q_out_stride_row=2048)), (plain, dict(rows=1, q_out_stride_row=2048))]:
             assert call(p, **kw) == -6, kw
 
 
 def test_attention_refused(lib):
     p = plan()
-    base = dict(q=AT, k=AT, v=AT, out=AT, lse=None, rows=9, q_stride_row=1024, q_stride_head=128, k_stride_row=256, k_stride_head=128,
+    base = dict(q=AT, k=AT, v=AT, out=ON, lse=None, rows=9, q_stride_row=1024, q_stride_head=128, k_stride_row=256, k_stride_head=128,
                 v_stride_row=256, v_stride_head=128, out_stride_row=1024, out_stride_head=128, scale=0.1)
 
     def call(n=2, max_rows=9, start=AT, status=AT, plan=p, **kw):
@@ -131,14 +135,16 @@ def test_attention_refused(lib):
     for kw in [dict(n=-1), dict(max_rows=-1), dict(rows=-1), dict(start=None), dict(status=None), dict(q=None), dict(k=None), dict(v=None),
                dict(out=None), dict(start=AT + 2), dict(status=AT + 1), dict(q=AT + 8), dict(k=AT + 8), dict(v=AT + 8), dict(out=AT + 8), dict(lse=AT + 2),
                dict(q_stride_row=1), dict(k_stride_head=12), dict(v_stride_row=2), dict(out_stride_head=4), dict(scale=math.nan),
-               dict(scale=math.inf), dict(scale=-2e38), dict(scale=1e-38), dict(scale=-1e-44)]:
+               dict(scale=math.inf), dict(scale=-2e38), dict(scale=1e-38), dict(scale=-1e-44),
+               # into keys or values; in place with other strides
+               dict(q=OFF, k=ON), dict(q=OFF, v=ON), dict(q=ON, out_stride_row=2048), dict(q=ON, q_stride_head=256)]:
         assert call(**kw) == -1, kw
     assert call(n=4) == -3 and call(rows=(1 << 28) + 1) == -3
     for kw in [dict(k_stride_row=-256), dict(v_stride_row=-8), dict(k_stride_row=(1 << 24) + 8), dict(v_stride_row=1 << 40)]:
         assert call(**kw) == -2, kw
     assert call(n=0, start=None) == 0 and call(max_rows=0, q=None) == 0
     if not torch.cuda.is_available():
-        assert call() == -6 and call(scale=0.0, lse=AT + 4) == -6 and call(k_stride_row=0, v_stride_row=1 << 24, q_stride_row=-1024) == -6 and call(rows=0, q=None, k=None, v=None, out=None) == -6
+        assert call() == -6 and call(scale=0.0, lse=AT + 4) == -6 and call(q=ON) == -6 and call(q=ON, rows=1, q_stride_row=0) == -6 and call(k_stride_row=0, v_stride_row=1 << 24, q_stride_row=-1024) == -6 and call(rows=0, q=None, k=None, v=None, out=None) == -6
 
 
 def test_block_rows(lib):
@@ -161,8 +167,8 @@ def test_block_rows(lib):
 
 def test_advance_refused(lib):
     p = kvc.CachePlan(1, 2, 8, block_tokens=32, max_tokens=1000, max_batch=6000)
-    base = dict(n=3, max_new=9, max_tokens=1000, rows=20, held=AT, kept=None, fresh=AT, free_pages=AT, block_table=AT, table_stride=32, new_start=AT,
-                tokens=AT, positions=AT, slots=AT, num_pages=50)
+    base = dict(n=3, max_new=9, max_tokens=1000, rows=20, held=AT, kept=None, fresh=AT, free_pages=AT, block_table=AT, table_stride=32, new_start=ON,
+                tokens=OFF, positions=4 * AT, slots=5 * AT, num_pages=50)
 
     def call(plan=p, status=AT, **kw):
         return lib.kvc_cache_advance(plan._h if plan else None, C.byref(kvc.CacheStep(**{**base, **kw})), status, None)
@@ -170,7 +176,9 @@ def test_advance_refused(lib):
     for kw in [dict(n=-1), dict(max_new=-1), dict(max_tokens=-1), dict(rows=-1), dict(num_pages=-1), dict(table_stride=31), dict(held=None),
                dict(free_pages=None), dict(block_table=None), dict(new_start=None), dict(tokens=None), dict(status=None), dict(held=AT + 2),
                dict(kept=AT + 1), dict(fresh=AT + 2), dict(free_pages=AT + 2), dict(block_table=AT + 2), dict(new_start=AT + 2), dict(tokens=AT + 2),
-               dict(positions=AT + 2), dict(slots=AT + 4), dict(status=AT + 2)]:
+               dict(positions=AT + 2), dict(slots=AT + 4), dict(status=AT + 2),
+               # written while others read them
+               dict(tokens=AT), dict(new_start=AT), dict(positions=AT), dict(slots=AT), dict(kept=OFF), dict(kept=ON), dict(tokens=ON)]:
         assert call(**kw) == -1, kw
     assert call(n=4097) == -3 and call(n=6001) == -3 and call(max_tokens=1001) == -3 and call(rows=1 << 31) == -3
     assert call(n=0, held=None) == 0
