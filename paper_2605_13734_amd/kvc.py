@@ -7,6 +7,7 @@ library has not been built (python __graft_entry__.py, or build.py in this direc
 import ctypes as C
 import functools
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libkvc.so")
@@ -102,6 +103,18 @@ class PromptHeads(C.Structure):
                                                "v_stride_head", "out_stride_row", "out_stride_head")] + [("scale", C.c_float)]
 
 
+def _packer(structure):
+    """What makes the bytes of such a structure from its fields in order (pointers as numbers, 0 for none), in a third of the structure's own
+    time: 0.25 instead of 0.75 us of a call that takes 6 on the host."""
+    letters = {C.c_void_p: "P", C.c_int64: "q", C.c_int32: "i", C.c_float: "f"}
+    packer = struct.Struct("@" + "".join(letters[t] for _, t in structure._fields_) + "0P")
+    assert packer.size == C.sizeof(structure)
+    return packer.pack
+
+
+_pack_step, _pack_rows, _pack_heads = _packer(CacheStep), _packer(PromptRows), _packer(PromptHeads)
+
+
 class KvcError(RuntimeError):
     def __init__(self, where, status):
         self.status = status
@@ -167,14 +180,14 @@ def load():
                                      C.c_void_p]
         L.kvc_cache_attend.argtypes = [C.c_void_p, C.POINTER(CacheSequences), C.POINTER(CacheQueries), C.c_void_p, C.c_void_p, C.c_void_p,
                                        C.c_void_p]
-        L.kvc_cache_advance.argtypes = [C.c_void_p, C.POINTER(CacheStep), C.c_void_p, C.c_void_p]
+        L.kvc_cache_advance.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]       # (a CacheStep, or its bytes)
         L.kvc_rotary_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_int64, C.c_void_p]
         L.kvc_prompt_plan.argtypes = [C.POINTER(PromptConfig), C.c_int32, C.POINTER(C.c_void_p)]
         L.kvc_prompt_plan_free.argtypes = [C.c_void_p]
         L.kvc_prompt_plan_free.restype = None
         L.kvc_prompt_block_rows.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.POINTER(C.c_int32)]
-        L.kvc_prompt_rotate.argtypes = [C.c_void_p, C.POINTER(PromptRows), C.c_void_p]
-        L.kvc_prompt_attend.argtypes = [C.c_void_p, C.POINTER(PromptSequences), C.POINTER(PromptHeads), C.c_void_p, C.c_void_p]
+        L.kvc_prompt_rotate.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
+        L.kvc_prompt_attend.argtypes = [C.c_void_p, C.POINTER(PromptSequences), C.c_void_p, C.c_void_p, C.c_void_p]
         L.kvc_status_string.argtypes = [C.c_int]
         L.kvc_status_string.restype = C.c_char_p
         _lib = L
@@ -599,10 +612,10 @@ class CachePages:
                         (rows is not None and rows != x.shape[0]):
                     raise ValueError("positions (int32) and slots (int64) are contiguous tensors of one length on the tables' device")
                 rows = x.shape[0]
-        step = CacheStep(n, max_new, self.plan.max_tokens if max_tokens is None else max_tokens, 0x7fffffff if rows is None else rows,
-                         self._held, kept.data_ptr() if kept is not None else None, fresh.data_ptr() if fresh is not None else None, self._free,
-                         self._table, self._stride, new_start.data_ptr(), tokens.data_ptr(), positions.data_ptr() if positions is not None else None,
-                         slots.data_ptr() if slots is not None else None, self.num_pages)
+        step = _pack_step(n, max_new, self.plan.max_tokens if max_tokens is None else max_tokens, 0x7fffffff if rows is None else rows,
+                         self._held, kept.data_ptr() if kept is not None else 0, fresh.data_ptr() if fresh is not None else 0, self._free,
+                          self._table, self._stride, new_start.data_ptr(), tokens.data_ptr(), positions.data_ptr() if positions is not None else 0,
+                          slots.data_ptr() if slots is not None else 0, self.num_pages)
         rc = self._advance(self._plan, step, self._status, stream)
         if rc != OK:
             raise KvcError("kvc_cache_advance", rc)
@@ -685,7 +698,7 @@ class Prompt:
         """kvc_prompt_rotate: q [rows, q_heads, 128], k [rows, kv_heads, 128], either may be None; positions [rows] int32; without q_out
         or k_out in place."""
         norm = self._norm
-        q_at = k_at = q_to = k_to = q_by = k_by = at = None
+        q_at = k_at = q_to = k_to = q_by = k_by = at = 0
         q_in = q_of = k_in = k_of = (0, 0)
         rows = 0
         if q is not None:
@@ -717,7 +730,7 @@ class Prompt:
             if positions.dtype is not self._int32 or positions.shape != (rows,) or not positions.is_contiguous() or positions.get_device() != self._device:
                 raise ValueError("positions are a contiguous int32 tensor [rows]")
             at = positions.data_ptr()
-        u = PromptRows(q_at, k_at, q_to, k_to, q_by, k_by, at, rows, q_in[0], q_in[1], k_in[0], k_in[1], q_of[0], q_of[1], k_of[0], k_of[1])
+        u = _pack_rows(q_at, k_at, q_to, k_to, q_by, k_by, at, rows, q_in[0], q_in[1], k_in[0], k_in[1], q_of[0], q_of[1], k_of[0], k_of[1])
         rc = self._rotate(self._plan, u, stream)
         if rc != OK:
             raise KvcError("kvc_prompt_rotate", rc)
@@ -738,7 +751,7 @@ class Prompt:
         if lse is not None:
             if lse.dtype is not self._float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.get_device() != self._device:
                 raise ValueError("lse is a contiguous float32 tensor [rows, q_heads]")
-        u = PromptHeads(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, rows,
+        u = _pack_heads(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else 0, rows,
                         q_strides[0], q_strides[1], k_strides[0], k_strides[1], v_strides[0], v_strides[1], out_strides[0], out_strides[1], scale)
         rc = self._attend(self._plan, batch._ref, u, self.status.data_ptr(), stream)
         if rc != OK:

@@ -286,3 +286,11 @@ def test_the_calls_go_to_their_device(lib, monkeypatch):
     prompt.attend(kvc.PromptBatch(words(0, 2), 2), q, k, k, q, 0.1)
     pages.advance(words(0, 0, 0), words(0, 0))
     assert seen == [("kvc_prompt_rotate", 1), ("kvc_prompt_attend", 1), ("kvc_cache_advance", 1)] and at == [0]
+
+
+def test_packed_arguments():
+    """The bytes that the calls are given are those of the structures."""
+    for structure, pack in ((kvc.CacheStep, kvc._pack_step), (kvc.PromptRows, kvc._pack_rows), (kvc.PromptHeads, kvc._pack_heads)):
+        values = [2.5 if t is C.c_float else (i + 1) * 0x10203 * (-1 if t is C.c_int64 else 1) for i, (_, t) in enumerate(structure._fields_)]
+        made = structure.from_buffer_copy(pack(*values))
+        assert [getattr(made, name) for name, _ in structure._fields_] == values
