@@ -603,7 +603,7 @@ typedef struct {
  *   kvc_prompt_rotate   in 32 bits, rounded once; angles are exact to 2^-31 of a turn at every position.  NaN and infinities stay in
  *                       their head, and in their pair where heads are not normed
  *   kvc_prompt_attend   out = softmax(scale * q k^T) v, where a row sees the rows of its sequence up to itself.  Scores, maxima and sums
- *                       are held in 32 bits, weights enter the second product in the type (one rounding).  Rows of no sequence are left
+ *                       are held in 32 bits (the weights' sums beyond 512 tokens in 64), weights enter the second product in the type (one rounding).  Rows of no sequence are left
  *                       as they are.  What a row does not see has no influence, whatever it holds; a row that sees a NaN, or an infinity
  *                       that its result depends on, has no finite result there (NaN or an infinity).  dev_status: n words, bits are OR-ed in.  Equal
  *                       inputs and bounds give equal bits
