@@ -33,6 +33,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kGroup = 32;                   // tokens of a product with values
 constexpr float kSlack = 7.0f;
+// A weight's exponent is score * factor + shift, one instruction, with the shift rounded to 32 bits: all weights of a row are off by one power of two, which
+// their sum has too, but which has to stay small.  Rows whose maximum is further from zero than this take it from the scores themselves (fp16 rows
+// with scores from 2^27 would leave the type, bf16 ones from 2^31).  (What the looking costs: 1 % at 8k tokens, 32 heads, 4 % at 1k.)
+constexpr float kFar = 65536.0f;
 // Weights are 2^(bias + score - maximum): fp16 ones as large as the type allows, so that those down to 2^-39 of the largest count; bf16 ones small,
 // so that sums of a million times the largest values stay inside 32 bits (values below 2^-106 lose bits for it).
 template <int DT> constexpr float kBias = DT == DT_F16 ? 8.0f : -20.0f;
@@ -325,7 +329,9 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
             }
         }
         f32x4 out[TILES][8];
-        float top[TILES], shift[TILES], sum[TILES];
+        float top[TILES], shift[TILES], sum[TILES];           // top: of the scores without the factor
+        bool far = false;                                     // some row of the wave is (kFar)
+        auto is_far = [&](float x) { return fabsf(x * a.factor) > kFar; };
         // Tile n.  MIXED: some rows see some of its tokens only, or none.  AGAIN: with values that are not finite taken out where they are
         // not seen.
         auto do_tile = [&](int n, int lane, auto mixed_tile, auto second_time) {
@@ -368,22 +374,33 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
                     most[t] = score[0][t][0];
 #pragma unroll
                     for (int e = 1; e < 8 * kHalves; ++e) most[t] = fmaxf(most[t], score[e >> 2][t][e & 3]);
-                    grown |= __builtin_fmaf(most[t], a.factor, -top[t]) > kSlack;
+                    grown |= (most[t] - top[t]) * a.factor > kSlack;
                 }
                 if (__any(grown)) {
+                    bool some_far = false;
 #pragma unroll
                     for (int t = 0; t < TILES; ++t) {
                         // (rows that have not grown stay as they are: a row's bits depend on what it sees alone)
                         const float highest = max_of_row(most[t]);
-                        const float now = __builtin_fmaf(highest, a.factor, -top[t]) > kSlack ? highest * a.factor : top[t];
+                        const float now = (highest - top[t]) * a.factor > kSlack ? highest : top[t];
                         const float from = now == kNone ? 0.0f : now;
-                        const float by = __builtin_amdgcn_exp2f(top[t] - from);
+                        const float by = __builtin_amdgcn_exp2f((top[t] - from) * a.factor);
                         top[t] = now;
-                        shift[t] = kBias<DT> - from;
+                        shift[t] = is_far(from) ? kBias<DT> : __builtin_fmaf(-from, a.factor, kBias<DT>);
+                        some_far |= is_far(from);
                         sum[t] *= by;
-                        sums_before[t][threadIdx.x] *= by;
+                        if (n >= kFold / TOKENS * TURNS) sums_before[t][threadIdx.x] *= by;
 #pragma unroll
                         for (int d = 0; d < 8; ++d) out[t][d] *= by;
+                    }
+                    far = __any(some_far);
+                }
+                if (__builtin_expect(far, false)) {
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) {
+                        const float off = top[t] != kNone && is_far(top[t]) ? top[t] : 0.0f;
+#pragma unroll
+                        for (int h = 0; h < 2 * kHalves; ++h) score[h][t] -= off;
                     }
                 }
                 float part[kHalves][TILES];
@@ -467,6 +484,7 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
                 top[t] = kNone;
                 shift[t] = kBias<DT>;
                 sum[t] = 0.0f;
+                far = false;
                 sums_before[t][threadIdx.x] = 0.0;
 #pragma unroll
                 for (int d = 0; d < 8; ++d) out[t][d] = f32x4{0, 0, 0, 0};
@@ -479,8 +497,10 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
             for (int n = 0; n < whole; n += TURNS) do_tile(n + turn, for_whole, BoolConst<false>(), second_time);
             const int for_mixed = here_only(lane);
             for (int n = whole; n < tiles; n += TURNS) do_tile(n + turn, for_mixed, BoolConst<true>(), second_time);
+            if (tiles > (kFold / TOKENS - 1) * TURNS) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) sum[t] = (float)(sums_before[t][threadIdx.x] + sum[t]);
+                for (int t = 0; t < TILES; ++t) sum[t] = (float)(sums_before[t][threadIdx.x] + sum[t]);
+            }
             if constexpr (TURNS > 1) {
                 constexpr int kResults = TILES * 8 * kPromptWaves * 64, kStatistics = TILES * kPromptWaves * 64;       // of a set
                 static_assert((TURNS - 1) * (kResults * sizeof(f32x4) + kStatistics * sizeof(f32x2)) <= sizeof(room), "results go through the tiles' room");
@@ -503,9 +523,9 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
                     for (int k = 0; k < TURNS - 1; ++k) {
                         const f32x2 other = statistics[k * kStatistics + t * kPromptWaves * 64];
                         const float now = fmaxf(top[t], other[0]), from = now == kNone ? 0.0f : now;
-                        const float by = __builtin_amdgcn_exp2f(top[t] - from), other_by = __builtin_amdgcn_exp2f(other[0] - from);
+                        const float by = __builtin_amdgcn_exp2f((top[t] - from) * a.factor), other_by = __builtin_amdgcn_exp2f((other[0] - from) * a.factor);
                         top[t] = now;
-                        shift[t] = kBias<DT> - from;
+                        shift[t] = is_far(from) ? kBias<DT> : __builtin_fmaf(-from, a.factor, kBias<DT>);
                         sum[t] = sum[t] * by + other[1] * other_by;
 #pragma unroll
                         for (int d = 0; d < 8; ++d) out[t][d] = out[t][d] * by + results[k * kResults + (t * 8 + d) * kPromptWaves * 64] * other_by;
@@ -533,7 +553,7 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
             for (int d = 0; d < 8; ++d)
                 *(u32x2 *)(to + 16 * d) = u32x2{round_pair<DT>(out[t][d][0] * by, out[t][d][1] * by), round_pair<DT>(out[t][d][2] * by, out[t][d][3] * by)};
             if (a.lse && g == 0)
-                a.lse[(long long)(b.row0 + row) * q_heads + head] = (__builtin_amdgcn_logf(all) - shift[t]) * 0.693147181f;
+                a.lse[(long long)(b.row0 + row) * q_heads + head] = (__builtin_amdgcn_logf(all) - shift[t] + (is_far(top[t]) ? top[t] * a.factor : 0.0f)) * 0.693147181f;
         }
         if (number + gridDim.z >= b.all) return;
         __syncthreads();

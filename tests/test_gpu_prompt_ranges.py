@@ -36,3 +36,44 @@ def test_sums_of_many_equal_weights(bf16, heads, rows):
         assert torch.equal(lse, lse[:, :1].expand(lse.shape)) and torch.equal(out, out[:, :1].expand(out.shape))
         error = (out[:, 0].double() - 1).abs().amax(1)
         assert (error <= 2.02 * half_step(bf16) + 2.0 ** -18 + count / 32 * 2.0 ** -24).all(), (b, error.max(), error.argmax())
+
+
+# (KV heads, query heads per KV head, rows of the tensors) of calls with blocks of 64 rows, of 64 shared by two sets of waves, of 128 and 192
+BLOCKS = {(64, 4): (32, 2, 700), (64, 8): (1, 2, 900), (128, 4): (48, 2, 2600), (192, 4): (32, 2, 10000)}
+
+
+@pytest.mark.parametrize("block", BLOCKS)
+@pytest.mark.parametrize("bf16,large,scale", [(False, 15, 2.0 ** -7), (False, 15, 2.0 ** -3), (False, 15, -2.0 ** -7), (True, 50, 2.0 ** -77), (True, 50, 2.0 ** -70),
+                                              (True, 50, 1.0), (True, 50, 1e30), (True, 50, -2.0 ** -77)])
+def test_scores_far_from_zero(block, bf16, large, scale):
+    """Scores that 32 bits hold, with differences that they hold too, and far larger than the differences that an exponential can tell.
+
+    Queries (2^large, 1 or 2^(large + 10)), keys (0, -2^large or 2^large, j): scores 0 or +-2^(2 large) and the steps of such numbers, exactly.  Weights
+    and the result are rounded to the type; 2^-17 allows for factors of up to 32 with two roundings (64 * 2^-24 is less) and the sums."""
+    kv, per, rows = BLOCKS[block]
+    dtype, n = typed(bf16), 640
+    plan = kvc.PromptPlan(own_type(bf16), kv, kv * per)
+    assert plan.block_rows(1, rows, rows) == block
+    g = torch.Generator().manual_seed(large)
+    step = 2.0 ** (2 * large - 23)           # of numbers from 2^(2 large)
+    q, k = torch.zeros(rows, 1, DIM, dtype=torch.float64), torch.zeros(rows, 1, DIM, dtype=torch.float64)
+    q[:, 0, 0], q[:, 0, 1] = 2.0 ** large, 1.0 if not bf16 else 2.0 ** (large + 10)
+    # a part near zero, one far below it, one far above it
+    k[100:250, 0, 0], k[250:, 0, 0] = -(2.0 ** large), 2.0 ** large
+    k[:, 0, 1] = torch.randint(0, 8, (rows,), generator=g) * step / q[0, 0, 1]
+    v = torch.randn(rows, 1, DIM, generator=g)
+    q, k, v = (x.to(dtype).to(DEVICE) for x in (q, k, v))
+    out, lse = torch.full((rows, kv * per, DIM), 77.0, dtype=dtype, device=DEVICE), torch.full((rows, kv * per), 77.0, device=DEVICE)
+    kvc.Prompt(plan).attend(kvc.PromptBatch(i32(0, n), rows), q.expand(rows, kv * per, DIM), k.expand(rows, kv, DIM), v.expand(rows, kv, DIM), out, scale,
+                            lse, stream())
+    scores = torch.where(torch.ones(n, n, device=DEVICE).tril() > 0, q[:n, 0].double() @ k[:n, 0].double().T, math.copysign(math.inf, -scale))
+    top = scores.amax(1, keepdim=True) if scale > 0 else scores.amin(1, keepdim=True)
+    weights = torch.exp((scores - top) * scale)
+    total = weights.sum(1, keepdim=True)
+    want, size = weights / total @ v[:n, 0].double(), weights / total @ v[:n, 0].double().abs()
+    u = half_step(bf16) * 1.01
+    assert ((out[:n, 0].double() - want).abs() <= want.abs() * u + size * (u + 2.0 ** -17) + n * 2.0 ** -33 * 6).all()
+    assert torch.equal(out[:n], out[:n, :1].expand(n, kv * per, DIM)) and (out[n:] == 77).all()
+    want = (top * scale + total.log())[:, 0]
+    off, some = (lse[:n, 0].double() - want).abs(), want.abs() < 3e38        # (others are beyond the logarithm's type)
+    assert (off[some] <= 2.0 ** -17 + want.abs()[some] * 2.0 ** -21).all() and some.any()
