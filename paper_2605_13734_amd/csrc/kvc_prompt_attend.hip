@@ -37,9 +37,10 @@ constexpr float kSlack = 7.0f;
 // their sum has too, but which has to stay small.  Rows whose maximum is further from zero than this take it from the scores themselves (fp16 rows
 // with scores from 2^27 would leave the type, bf16 ones from 2^31).  (What the looking costs: 1 % at 8k tokens, 32 heads, 4 % at 1k.)
 constexpr float kFar = 65536.0f;
-// Weights are 2^(bias + score - maximum): fp16 ones as large as the type allows, so that those down to 2^-39 of the largest count; bf16 ones small,
-// so that sums of a million times the largest values stay inside 32 bits (values below 2^-106 lose bits for it).
-template <int DT> constexpr float kBias = DT == DT_F16 ? 8.0f : -20.0f;
+// Weights are 2^(bias + score - maximum), where the maximum may be up to kSlack below the row's own: fp16 ones as large as the type allows (2^15 with the
+// slack), so that those down to 2^-32 of the largest count (2^-39 where all the slack is used), bf16 ones small (2^-20 with the slack), so that sums of
+// 2^20 times the largest values stay inside 32 bits (values below 2^-99 lose bits for it).
+template <int DT> constexpr float kBias = DT == DT_F16 ? 8.0f : -27.0f;
 constexpr float kNone = -__builtin_inff();
 // Weights of up to this many tokens are added up in 32 bits (a tile's as a tree, then tile by tile: 20 roundings at most), sums of these in 64
 // bits.  Added one by one over a long prompt, equal weights round the same way each time: 32k of them were off by 0.00012, 128k by 0.0005.  (8k tokens, 32 heads: 495 us, one by one 491.)

@@ -77,3 +77,24 @@ def test_scores_far_from_zero(block, bf16, large, scale):
     want = (top * scale + total.log())[:, 0]
     off, some = (lse[:n, 0].double() - want).abs(), want.abs() < 3e38        # (others are beyond the logarithm's type)
     assert (off[some] <= 2.0 ** -17 + want.abs()[some] * 2.0 ** -21).all() and some.any()
+
+
+@pytest.mark.parametrize("heads,rows,block", [(1, 20000, (64, 8)), (8, 12000, (64, 4)), (64, 30000, (192, 4)), (1, 1 << 20, (192, 4))])
+def test_sums_of_the_largest_values_behind_a_lower_maximum(heads, rows, block):
+    """bf16: a first tile of score 0, then scores just too low to become the maximum that weights refer to (6.9 in base 2, so each weighs 2^6.9): sums
+    of up to a million of the largest values stay inside 32 bits.  All values are equal: half a step for the weights, half a step for the result,
+    2^-18 for the sums, 2^-24 for each product of 32 tokens."""
+    plan = kvc.PromptPlan(kvc.BF16, heads, heads)
+    assert plan.block_rows(1, rows, rows) == block
+    q, k = torch.zeros(1, 1, DIM, dtype=torch.bfloat16, device=DEVICE), torch.zeros(rows, 1, DIM, dtype=torch.bfloat16, device=DEVICE)
+    q[:, :, 0] = 1.0
+    k[64:, :, 0] = 4.78
+    out = torch.empty(rows, heads, DIM, dtype=torch.bfloat16, device=DEVICE)
+    allowed = 2.02 * half_step(True) + 2.0 ** -18 + torch.arange(rows, device=DEVICE) / 32 * 2.0 ** -24
+    for value in (3.38e38, -3.38e38):
+        v = torch.full((1, 1, DIM), value, dtype=torch.bfloat16, device=DEVICE)
+        out.fill_(77.0)
+        kvc.Prompt(plan).attend(kvc.PromptBatch(i32(0, rows), rows), *(x.expand(rows, heads, DIM) for x in (q, k, v)), out, 1.0, None, stream())
+        got = out[:, 0].double() / v[0, 0, 0].double()
+        assert ((got - 1).abs().amax(1) <= allowed).all(), (value, (got - 1).abs().amax())
+        assert torch.equal(out, out[:, :1].expand(out.shape))
