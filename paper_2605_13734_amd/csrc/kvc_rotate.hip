@@ -94,7 +94,9 @@ template <int DT, bool NEIGHBOURS, bool NORM> __global__ __launch_bounds__(256) 
     const int end = first + a.chunk < x.heads ? first + a.chunk : x.heads;
     const int lane = lane_id(), col = lane & 15, sub = lane >> 4;
 
-    // factors of the lane's channels and of their partners'
+    // Factors of the lane's channels and of their partners'.  With norms of bf16 heads the amplitude is left for the head's own factor, and that
+    // comes first: a weight times a normed number stays inside 32 bits where the type's numbers times each other do not.
+    constexpr bool APART = NORM && DT == DT_BF16;
     float own[8], other[8];
     const int half = a.pairs / 8;            // octets of one half
     const bool turns = col < 2 * half, front = col < half;
@@ -111,8 +113,8 @@ template <int DT, bool NEIGHBOURS, bool NORM> __global__ __launch_bounds__(256) 
             const uint64_t each = f[NEIGHBOURS ? e / 2 : e];
             float c, s;
             turn(__umulhi((uint32_t)position, (uint32_t)each) + (uint32_t)position * (uint32_t)(each >> 32), c, s);
-            own[e] = c * a.amplitude;
-            other[e] = (NEIGHBOURS || front ? -s : s) * a.amplitude;
+            own[e] = APART ? c : c * a.amplitude;
+            other[e] = APART ? (NEIGHBOURS || front ? -s : s) : (NEIGHBOURS || front ? -s : s) * a.amplitude;
         }
     } else {
 #pragma unroll
@@ -174,11 +176,19 @@ template <int DT, bool NEIGHBOURS, bool NORM> __global__ __launch_bounds__(256) 
                 }
                 by = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, 1.0f / kDim, eps));
             }
+            if (APART) {
+                if (turns) by *= a.amplitude;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    mine[e] *= by;
+                    theirs[e] *= by;
+                }
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 y[e] = mine[e] * own[e];
                 if (turns) y[e] = __builtin_fmaf(theirs[e], other[e], y[e]);
-                if (NORM) y[e] *= by;
+                if (NORM && !APART) y[e] *= by;
             }
             if (head < end) {
                 const u32x4 z = {round_pair<DT>(y[0], y[1]), round_pair<DT>(y[2], y[3]), round_pair<DT>(y[4], y[5]), round_pair<DT>(y[6], y[7])};
