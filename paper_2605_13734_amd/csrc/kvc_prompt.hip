@@ -13,7 +13,7 @@ struct kvc_prompt_plan_s {
 
 namespace kvc {
 
-constexpr long double kTwoPi = 6.283185307179586476925286766559L;
+constexpr double kTwoPi = 6.283185307179586;
 
 constexpr int64_t kMostStride = 1 << 24;      // of rows of K and V, in elements
 constexpr int64_t kMostRows = 1 << 28;        // of a call
@@ -27,13 +27,21 @@ static bool in_place_ok(const void *in, const void *out, int64_t rows, int64_t h
     return in != out || ((rows < 2 || row == out_row) && (heads < 2 || head == out_head));
 }
 
-// The part of a turn that a position adds, in 2^-64 of a turn.
+// 1 / (2 pi) in 2^-128
+constexpr unsigned __int128 kTurnsPerRadian = (unsigned __int128)0x28be60db9391054aull << 64 | 0x7f09d5f47d4d3770ull;
+
+// The part of a turn that a position adds, in 2^-64 of a turn, rounded.  The product is made of whole numbers: of a frequency of 10^9 radians the turns
+// that are dropped have 28 bits, which a floating-point quotient would have in place of the last ones that a large position needs.
 static uint64_t turns_of(double radians)
 {
-    long double t = (long double)radians / kTwoPi;
-    t -= floorl(t);
-    // (t may be rounded up to 1: no turn)
-    return t >= 1.0L ? 0 : (uint64_t)(t * 18446744073709551616.0L);
+    int exponent;
+    const uint64_t mantissa = (uint64_t)ldexp(frexp(fabs(radians), &exponent), 53);       // times 2^(exponent - 53)
+    const unsigned __int128 low = (unsigned __int128)mantissa * (uint64_t)kTurnsPerRadian;
+    const unsigned __int128 high = (unsigned __int128)mantissa * (uint64_t)(kTurnsPerRadian >> 64) + (uint64_t)(low >> 64);       // in 2^(exponent - 117)
+    const int down = 53 - exponent;          // to 2^-64: 23 at least, since frequencies are no more than 10^9
+    if (down > 127) return 0;
+    const uint64_t turns = (uint64_t)(high >> down) + (uint64_t)(high >> (down - 1) & 1);
+    return radians < 0 ? 0 - turns : turns;
 }
 
 }  // namespace kvc
@@ -47,7 +55,7 @@ extern "C" int kvc_rotary_frequencies(int32_t rotary_dim, double base, int32_t s
     const bool windows = scaling == KVC_SCALE_BANDS || scaling == KVC_SCALE_RAMP;
     if (windows && (!(low > 0.0) || !(high > low) || !(high <= 1e9) || original_tokens < 1)) return KVC_ERR_ARG;
     if (scaling == KVC_SCALE_BASE && rotary_dim == 2) return KVC_ERR_ARG;
-    const double R = rotary_dim, two_pi = (double)kvc::kTwoPi, original = (double)original_tokens;
+    const double R = rotary_dim, two_pi = kvc::kTwoPi, original = (double)original_tokens;
     if (scaling == KVC_SCALE_BASE) base *= pow(factor, R / (R - 2.0));
     double first = 0.0, last = 0.0;
     if (scaling == KVC_SCALE_RAMP) {

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2605_13734_amd import kvc
-from prompt_util import DEVICE, DIM, check_rotation, heads, own_type, stream, typed
+from prompt_util import DEVICE, DIM, check_rotation, half_step, heads, smallest, stream
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +28,39 @@ def test_weights_of_norms_are_as_large_as_their_type(size, weight, amplitude, la
     for got, x, y in ((q_out, q, w[0]), (k_out, k, w[1])):
         assert got.isfinite().all()
         check_rotation(got, x, y, at.numpy(), f, layout == kvc.ROTARY_PAIRS, amplitude, eps, True)
+
+
+def turns(position, frequency):
+    """The part of a turn of an angle, from whole numbers: 1 / (2 pi) to 600 bits by pi = 16 arctan(1/5) - 4 arctan(1/239)."""
+    bits = 700
+
+    def arctan_of_one_by(x):
+        term, total, n, sign = (1 << bits) // x, 0, 1, 1
+        while term:
+            total, term, n, sign = total + sign * (term // n), term // (x * x), n + 2, -sign
+        return total
+    two_pi = 8 * (4 * arctan_of_one_by(5) - arctan_of_one_by(239))
+    top, bottom = frequency.as_integer_ratio()
+    part = (position * top << 2 * bits) // (bottom * two_pi) & ((1 << bits) - 1)
+    return (part >> (bits - 64)) / 2.0 ** 64
+
+
+@pytest.mark.parametrize("layout", [kvc.ROTARY_HALVES, kvc.ROTARY_PAIRS])
+def test_frequencies_of_many_turns_at_far_positions(layout):
+    """Frequencies up to the largest that a plan takes: the whole turns are dropped without a bit of what is left (a quotient of 64 bits is off by 2^-7
+    of a turn at the last of these).  2^-19 of the terms stands for 32-bit cosines (2^-21) and products; then the type's half step."""
+    f = [1e9, -1e9, 123456789.125, -87654321.1, 1e7, 1e6 + 0.1, 2.0 ** 29, 999999999.9999]
+    at = [2 ** 31 - 1, 2 ** 31 - 2, 10 ** 9 + 7, 2 ** 30 + 3, 10 ** 8 + 7, 123457, 1, 0]
+    prompt = kvc.Prompt(kvc.PromptPlan(kvc.F16, 2, 6, layout=layout, rotary_dim=16, frequencies=f))
+    q, k, _ = heads(len(at), 2, 3, False, 4)
+    q_out, k_out = torch.empty_like(q), torch.empty_like(k)
+    prompt.rotate(q, k, torch.tensor(at, dtype=torch.int32, device=DEVICE), q_out, k_out, stream=stream())
+    angle = 2 * np.pi * np.array([[turns(p, x) for x in f] for p in at])
+    c, s = np.cos(angle)[:, None], np.sin(angle)[:, None]
+    first, second = (slice(0, 16, 2), slice(1, 16, 2)) if layout == kvc.ROTARY_PAIRS else (slice(0, 8), slice(8, 16))
+    for x, got in ((q, q_out), (k, k_out)):
+        x, got = x.double().cpu().numpy(), got.double().cpu().numpy()
+        a, b = x[..., first], x[..., second]
+        for want, there in ((a * c - b * s, first), (a * s + b * c, second)):
+            assert (np.abs(got[..., there] - want) <= np.abs(want) * half_step(False) * 1.01 + (np.abs(a) + np.abs(b)) * 2.0 ** -19 + smallest(False)).all()
+        assert (got[..., 16:] == x[..., 16:]).all()
