@@ -14,9 +14,16 @@
 
 namespace kvc {
 
-constexpr uint32_t kTop = 0x7fffffffu;       // the running sums stop here
+// The running sums stop here: more than any number of rows or pages that a call may have, so that a sum that has stopped fits none.
+constexpr uint32_t kTop = 0x80000000u;
 
-__device__ __forceinline__ uint32_t add_up(uint32_t a, uint32_t b) { return a + b < kTop ? a + b : kTop; }
+__device__ __forceinline__ uint32_t add_up(uint32_t a, uint32_t b)
+{
+    const uint32_t sum = __builtin_elementwise_add_sat(a, b);
+    return sum < kTop ? sum : kTop;
+}
+// A sum as the largest word that callers have for it.
+__device__ __forceinline__ int word_of(uint32_t sum) { return sum < kTop ? (int)sum : 0x7fffffff; }
 
 template <int CONTROL, int ROWS = 0xf> __device__ __forceinline__ uint32_t from_lane(uint32_t x)
 {
@@ -114,7 +121,7 @@ template <int THREADS, int EACH> __global__ __launch_bounds__(THREADS) void adva
         const int s = tid * each + i;
         if (i < each && s < a.n) {
             start[s] = row;
-            if (first) a.new_start[s] = (int)row;
+            if (first) a.new_start[s] = word_of(row);
             row = add_up(row, (unsigned)mine[i].fresh <= (unsigned)a.max_new ? mine[i].fresh : 0);
             mine[i].fits = mine[i].fits && (long long)row <= a.rows;
             if (mine[i].fits) {
@@ -129,7 +136,7 @@ template <int THREADS, int EACH> __global__ __launch_bounds__(THREADS) void adva
         start[a.n] = total_rows;
         takes[a.n] = total_takes;
         gives[a.n] = total_gives;
-        if (first) a.new_start[a.n] = (int)total_rows;
+        if (first) a.new_start[a.n] = word_of(total_rows);
     }
     const uint32_t room = add_up((uint32_t)count, total_gives);
     int after[EACH];                         // tokens that are held afterwards
