@@ -569,7 +569,8 @@ void kvc_prompt_plan_free(kvc_prompt_plan_t *plan);
 int32_t kvc_prompt_block_rows(const kvc_prompt_plan_t *plan, int32_t n, int32_t max_rows, int64_t rows, int32_t *waves);
 
 /* Queries and keys of `rows` rows, up to 2^28.  Element d of head h of row r at q + r * q_stride_row + h * q_stride_head + d; strides are multiples of
- * 8.  q or k may be NULL (the other alone), and q_out = q, k_out = k with the same strides; tensors do not overlap otherwise. */
+ * 8.  q or k may be NULL (the other alone), and q_out = q, k_out = k with the same strides; tensors do not overlap otherwise, and heads of
+ * a result lie apart (strides that let two share a place, such as 0, are refused). */
 typedef struct {
     const void *q, *k;                   /* DEVICE */
     void *q_out, *k_out;                 /* DEVICE */
@@ -589,7 +590,7 @@ typedef struct {
 } kvc_prompt_batch;
 
 /* Queries, keys, values and results of `rows` rows, up to 2^28; strides are multiples of 8, those between rows of k and v 0 to 2^24.  lse: optional,
- * [rows][q_heads].  out may be q itself, with the same strides; results do not overlap anything else. */
+ * [rows][q_heads].  out may be q itself, with the same strides; results do not overlap anything else, and heads of out lie apart, as above. */
 typedef struct {
     const void *q, *k, *v;               /* DEVICE */
     void *out;                           /* DEVICE */

@@ -30,6 +30,20 @@ static bool in_place_ok(const void *in, const void *out, int64_t rows, int64_t h
 // 1 / (2 pi) in 2^-128
 constexpr unsigned __int128 kTurnsPerRadian = (unsigned __int128)0x28be60db9391054aull << 64 | 0x7f09d5f47d4d3770ull;
 
+// Heads of a result that lie apart: rows * row + heads * head comes nowhere within a head of itself.  (Two that share a place would race for it.)
+static bool apart(int64_t rows, int64_t heads, int64_t row, int64_t head)
+{
+    typedef __int128 wide;                   // (strides are any 64-bit numbers)
+    const wide r = row < 0 ? -(wide)row : row, h = head < 0 ? -(wide)head : head;
+    if ((rows > 1 && r < kDim) || (heads > 1 && h < kDim)) return false;
+    if (rows < 2 || heads < 2 || r >= (heads - 1) * h + kDim || h >= (rows - 1) * r + kDim) return true;
+    for (wide d = 1; d < heads; ++d) {       // (only layouts that are neither rows of heads nor heads of rows)
+        const wide below = d * h / r, off = d * h - below * r;
+        if ((below < rows && off < kDim) || (below + 1 < rows && r - off < kDim)) return false;
+    }
+    return true;
+}
+
 // The part of a turn that a position adds, in 2^-64 of a turn, rounded.  The product is made of whole numbers: of a frequency of 10^9 radians the turns
 // that are dropped have 28 bits, which a floating-point quotient would have in place of the last ones that a large position needs.
 static uint64_t turns_of(double radians)
@@ -121,6 +135,8 @@ extern "C" int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt
         (r->k && (!in_place_ok(r->k, r->k_out, r->rows, f.kv_heads, r->k_stride_row, r->k_stride_head, r->k_out_stride_row, r->k_out_stride_head) ||
                   r->k_out == r->q)) || (r->q && r->k && r->q_out == r->k_out)) return KVC_ERR_ARG;
     if (r->rows > kMostRows) return KVC_ERR_CAPACITY;
+    if ((r->q && !apart(r->rows, f.q_heads, r->q_out_stride_row, r->q_out_stride_head)) ||
+        (r->k && !apart(r->rows, f.kv_heads, r->k_out_stride_row, r->k_out_stride_head))) return KVC_ERR_ARG;
     RotateArgs a = {};
     a.q = RotateTensor{(const uint16_t *)r->q, f.norm ? (const uint16_t *)r->q_weight : nullptr, (uint16_t *)r->q_out, r->q_stride_row,
                        r->q_stride_head, r->q_out_stride_row, r->q_out_stride_head, r->q ? f.q_heads : 0, 0};
@@ -172,6 +188,7 @@ extern "C" int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt
         !strides_ok(h.v_stride_row, h.v_stride_head) || !strides_ok(h.out_stride_row, h.out_stride_head)) return KVC_ERR_ARG;
     if (h.out && (h.out == h.k || h.out == h.v ||
                   !in_place_ok(h.q, h.out, h.rows, f.q_heads, h.q_stride_row, h.q_stride_head, h.out_stride_row, h.out_stride_head))) return KVC_ERR_ARG;
+    if (!apart(h.rows, f.q_heads, h.out_stride_row, h.out_stride_head)) return KVC_ERR_ARG;
     // (smaller factors are subnormal numbers, which may count as zero)
     if (!(fabsf(h.scale) <= 1e38f) || (h.scale != 0.0f && fabsf(h.scale) < 1e-37f)) return KVC_ERR_ARG;
     // (offsets of the 64 rows of a tile are 32-bit numbers above zero)
