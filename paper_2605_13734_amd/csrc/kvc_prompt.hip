@@ -148,10 +148,24 @@ extern "C" int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt
     a.amplitude = f.rotary_dim ? f.amplitude : 1.0f;
     a.pairs = f.rotary_dim / 2;
     for (int i = 0; i < a.pairs; ++i) a.turns[i] = plan->turns[i];
-    const long long groups = rotate_groups(a);
-    if (groups > kMostThreads / 256) return KVC_ERR_CAPACITY;
-    launch_rotate(f.dtype, f.layout == KVC_ROTARY_PAIRS, f.norm != 0, a, groups, (hipStream_t)hip_stream);
-    return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_DEVICE;
+    divide_rows(a);
+    // one launch for as many rows as its threads can be (2^26, or 13 million with 64 + 8 heads), further ones behind it
+    const int64_t most = kMostThreads / 256 * 4 / a.chunks;
+    for (int64_t done = 0; done < r->rows; done += most) {
+        RotateArgs part = a;
+        part.rows = r->rows - done < most ? r->rows - done : most;
+        if (done) {
+            for (RotateTensor *x : {&part.q, &part.k}) {
+                if (!x->heads) continue;
+                x->in += done * x->in_row;
+                x->out += done * x->out_row;
+            }
+            if (part.positions) part.positions += done;
+        }
+        launch_rotate(f.dtype, f.layout == KVC_ROTARY_PAIRS, f.norm != 0, part, (part.rows * part.chunks + 3) / 4, (hipStream_t)hip_stream);
+        if (hipGetLastError() != hipSuccess) return KVC_ERR_DEVICE;
+    }
+    return KVC_OK;
 }
 
 extern "C" int32_t kvc_prompt_block_rows(const kvc_prompt_plan_t *plan, int32_t n, int32_t max_rows, int64_t rows, int32_t *waves)

@@ -30,8 +30,8 @@ struct RotateArgs {
     int past_caches, pad;          // rows are read past the caches
 };
 
-// Divides the rows (chunk, chunks, past_caches of the arguments) and returns the workgroups, of 256 threads.
-long long rotate_groups(RotateArgs &a);
+// Divides the rows (chunk, chunks, past_caches of the arguments): a wave has one row and one chunk, a workgroup four waves.
+void divide_rows(RotateArgs &a);
 void launch_rotate(int dtype, bool neighbours, bool norm, const RotateArgs &a, long long groups, hipStream_t stream);
 
 // ---- attention over whole prompts ------------------------------------------------------------------

@@ -215,8 +215,8 @@ constexpr long long kLeastWaves = 4096;
 // 229 us; 8k rows of 40 heads, 168 MB: 30 instead of 29).
 constexpr double kCaches = 256e6;
 
-// How a call's rows are divided; workgroups.
-long long rotate_groups(RotateArgs &a)
+// How a call's rows are divided.
+void divide_rows(RotateArgs &a)
 {
     const int most = a.q.heads > a.k.heads ? a.q.heads : a.k.heads;
     auto chunks = [&](int chunk) { return (a.q.heads + chunk - 1) / chunk + (a.k.heads + chunk - 1) / chunk; };
@@ -224,7 +224,6 @@ long long rotate_groups(RotateArgs &a)
     while (a.chunk > 4 && a.rows * chunks(a.chunk) < kLeastWaves) a.chunk -= 4;
     a.chunks = chunks(a.chunk);
     a.past_caches = (double)a.rows * (a.q.heads + a.k.heads) * 4 * kDim > kCaches;
-    return (a.rows * a.chunks + 3) / 4;
 }
 void launch_rotate(int dtype, bool neighbours, bool norm, const RotateArgs &a, long long groups, hipStream_t stream)
 {

@@ -64,3 +64,28 @@ def test_frequencies_of_many_turns_at_far_positions(layout):
         for want, there in ((a * c - b * s, first), (a * s + b * c, second)):
             assert (np.abs(got[..., there] - want) <= np.abs(want) * half_step(False) * 1.01 + (np.abs(a) + np.abs(b)) * 2.0 ** -19 + smallest(False)).all()
         assert (got[..., 16:] == x[..., 16:]).all()
+
+
+@pytest.mark.parametrize("rows,parts", [((1 << 26) + 1027, "q"), ((1 << 25) + 1, "qk")])
+def test_more_rows_than_a_launch_has(rows, parts):
+    """Rows that need more threads than one launch may have (17 GB): as calls of a quarter of them."""
+    plan = kvc.PromptPlan(kvc.F16, 1, 1, rotary_dim=32)
+    prompt, some = kvc.Prompt(plan), 4099
+    block = torch.randn(some, 1, DIM, generator=torch.Generator().manual_seed(3)).half().to(DEVICE)
+    at = torch.arange(rows, dtype=torch.int32, device=DEVICE)
+    at[-5:-3] = -1                           # (left as they are)
+    whole = []
+    for _ in parts:
+        x = torch.empty(rows, 1, DIM, dtype=torch.float16, device=DEVICE)
+        for a in range(0, rows, some):
+            x[a: a + some] = block[: rows - a]
+        whole.append(x)
+    q, k = whole[0], whole[1] if parts == "qk" else None
+    prompt.rotate(q, k, at, stream=stream())
+    piece = rows // 4 + 7
+    for a in range(0, rows, piece):
+        n = min(piece, rows - a)
+        want = block[torch.arange(a, a + n, device=DEVICE) % some]
+        prompt.rotate(want, None, at[a: a + n], stream=stream())
+        for x in whole:
+            assert torch.equal(x[a: a + n], want)

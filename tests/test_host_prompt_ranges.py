@@ -60,3 +60,11 @@ def test_expanded_results_are_refused(bad):
         with pytest.raises(kvc.KvcError) as e:
             call()
         assert e.value.status == ARG
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls that are taken end at the device that is not there")
+def test_all_rows_that_are_documented_are_taken():
+    for heads in (1, 16, 64, 1024):
+        stride = (heads * 128, 128)
+        assert rotate(heads, 1, 1 << 28, q=stride) == rotate(heads, heads, 1 << 28, q=stride, k=stride) == attend(heads, 1 << 28, stride) == DEVICE
+        assert rotate(heads, 1, (1 << 28) + 1, q=stride) == attend(heads, (1 << 28) + 1, stride) == CAPACITY
