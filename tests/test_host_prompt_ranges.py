@@ -15,7 +15,7 @@ OK, ARG, CAPACITY, DEVICE = 0, -1, -3, -6
 def rotate(q_heads, kv_heads, rows, q=None, k=None):
     """The status of a rotation into results with these (row, head) strides."""
     plan = kvc.PromptPlan(kvc.F16, kv_heads, q_heads)
-    a = dict(q=AT if q else None, q_out=ON, k=AT if k else None, k_out=ON, positions=AT, rows=rows, q_stride_row=0, q_stride_head=0, k_stride_row=0,
+    a = dict(q=AT if q else None, q_out=ON, k=AT if k else None, k_out=ON + AT, positions=AT, rows=rows, q_stride_row=0, q_stride_head=0, k_stride_row=0,
              k_stride_head=0)
     for name, strides in (("q", q), ("k", k)):
         a[name + "_out_stride_row"], a[name + "_out_stride_head"] = strides or (0, 0)
