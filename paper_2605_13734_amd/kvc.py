@@ -598,14 +598,19 @@ class CachePages:
         self.free[0] = pages.numel()
         self.free[4: 4 + pages.numel()] = pages.to(self.free.device)
 
-    def advance(self, new_start, tokens, kept=None, fresh=None, max_new=0, max_tokens=None, positions=None, slots=None, rows=None,
+    def advance(self, new_start, tokens, kept=None, fresh=None, max_new=None, max_tokens=None, positions=None, slots=None, rows=None,
                 stream=None):
-        """kvc_cache_advance.  new_start [n + 1], tokens [n]: int32, written; kept, fresh [n]: int32 or None; positions [rows] int32,
+        """kvc_cache_advance.  new_start [n + 1], tokens [n]: int32, written; kept, fresh [n]: int32 or None; max_new: the most that a number in
+        fresh may be (a sequence with more is left out), given with it; positions [rows] int32,
         slots [rows] int64: written, or None (then rows is the room that the new rows have, if it is bounded)."""
         n = self._n
         for x, size in ((new_start, n + 1), (tokens, n), (kept, n), (fresh, n)):
             if x is not None and (x.dtype is not self._int32 or x.shape != (size,) or not x.is_contiguous() or x.get_device() != self._device):
                 raise ValueError("new_start [n + 1], tokens, kept and fresh [n] are contiguous int32 tensors on the tables' device")
+        if max_new is None:
+            if fresh is not None:
+                raise ValueError("fresh needs max_new, the most that it may be")
+            max_new = 0
         for x, dtype in ((positions, self._int32), (slots, self._int64)):
             if x is not None:
                 if x.dtype is not dtype or x.dim() != 1 or not x.is_contiguous() or x.get_device() != self._device or \

@@ -68,3 +68,17 @@ def test_all_rows_that_are_documented_are_taken():
         stride = (heads * 128, 128)
         assert rotate(heads, 1, 1 << 28, q=stride) == rotate(heads, heads, 1 << 28, q=stride, k=stride) == attend(heads, 1 << 28, stride) == DEVICE
         assert rotate(heads, 1, (1 << 28) + 1, q=stride) == attend(heads, (1 << 28) + 1, stride) == CAPACITY
+
+
+def test_new_tokens_need_their_bound(monkeypatch):
+    """Without it every sequence that gets a token would be left out."""
+    pages = kvc.CachePages(kvc.CachePlan(1, 2, 8, max_tokens=100, max_batch=2), 7, 2, "cpu")
+    pages._device, calls = -1, []
+    monkeypatch.setattr(pages, "_advance", lambda plan, step, status, stream: calls.append(kvc.CacheStep.from_buffer_copy(step).max_new) or 0)
+    start, two = torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="max_new"):
+        pages.advance(start, two, fresh=two.clone())
+    pages.advance(start, two, fresh=two.clone(), max_new=0)
+    pages.advance(start, two, fresh=two.clone(), max_new=5)
+    pages.advance(start, two)
+    assert calls == [0, 5, 0]
