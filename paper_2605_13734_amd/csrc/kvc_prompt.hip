@@ -33,6 +33,7 @@ constexpr unsigned __int128 kTurnsPerRadian = (unsigned __int128)0x28be60db93910
 // Heads of a result that lie apart: rows * row + heads * head comes nowhere within a head of itself.  (Two that share a place would race for it.)
 static bool apart(int64_t rows, int64_t heads, int64_t row, int64_t head)
 {
+    if (rows < 1) return true;
     typedef __int128 wide;                   // (strides are any 64-bit numbers)
     const wide r = row < 0 ? -(wide)row : row, h = head < 0 ? -(wide)head : head;
     if ((rows > 1 && r < kDim) || (heads > 1 && h < kDim)) return false;

@@ -22,11 +22,11 @@ def rotate(q_heads, kv_heads, rows, q=None, k=None):
     return kvc.load().kvc_prompt_rotate(plan._h, C.byref(kvc.PromptRows(**a)), None)
 
 
-def attend(q_heads, rows, strides):
+def attend(q_heads, rows, strides, most=None):
     plan = kvc.PromptPlan(kvc.F16, 1, q_heads)
     heads = kvc.PromptHeads(q=AT, k=AT, v=AT, out=ON, rows=rows, q_stride_row=0, q_stride_head=0, k_stride_row=0, k_stride_head=0, v_stride_row=0,
                             v_stride_head=0, out_stride_row=strides[0], out_stride_head=strides[1], scale=0.1)
-    return kvc.load().kvc_prompt_attend(plan._h, C.byref(kvc.PromptSequences(1, rows, AT)), C.byref(heads), AT, None)
+    return kvc.load().kvc_prompt_attend(plan._h, C.byref(kvc.PromptSequences(1, most or rows, AT)), C.byref(heads), AT, None)
 
 
 def share(heads, rows, row, head):
@@ -47,6 +47,7 @@ def test_results_whose_heads_share_places_are_refused(heads, rows):
         assert rotate(heads, heads, rows, q=strides) == rotate(heads, heads, rows, k=strides) == attend(heads, rows, strides) == want, strides
         seen.add(want)
     assert len(seen) == 2 or heads == rows == 1
+    assert attend(heads, 0, (0, 0)) == OK and attend(heads, 0, (0, 0), 5) == DEVICE            # (no rows: nothing is written)
 
 
 @pytest.mark.parametrize("bad", [lambda x: x[:1].expand(4, 2, 128), lambda x: x[:, :1].expand(4, 2, 128)], ids=["rows", "heads"])
