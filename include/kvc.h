@@ -496,8 +496,9 @@ int kvc_cache_attend(const kvc_cache_plan_t *plan, const kvc_cache_batch *batch,
  * its numbers do not fit (0 <= kept <= held <= max_tokens, 0 <= fresh <= max_new, kept + fresh <= max_tokens, rows up to `rows`):
  * KVC_DEV_BAD_ROW; or where it needs more pages and those left by the sequences before it (left out or not) are too few:
  * KVC_DEV_NO_PAGE.  A page outside [0, num_pages) in the stack or among the given ones is passed on as -1: KVC_DEV_BAD_BLOCK.
- * Up to KVC_MOST_ADVANCING sequences.  Arrays do not overlap; slots is 8-byte aligned.  Like the other calls it is enqueued on hip_stream
- * and may be captured; calls on the same tables and free pages must be in stream order.
+ * Up to KVC_MOST_ADVANCING sequences; with none nothing is written.  New rows are 2^31 - 1 at most in all.  Arrays do not overlap; slots
+ * is 8-byte aligned.  Like the other calls it is enqueued on hip_stream and may be captured; calls on the same tables and free pages must be
+ * in stream order.
  */
 #define KVC_MOST_ADVANCING 4096
 typedef struct {
@@ -583,7 +584,8 @@ typedef struct {
 
 /* The prompts of a call: sequence s has rows start[s] ... start[s + 1] - 1.  max_rows bounds their rows and fixes the launch; a sequence
  * whose numbers do not fit (start below zero or descending, more than max_rows rows, rows outside the tensors) is left out: KVC_DEV_BAD_ROW
- * (behind descending starts two sequences may have the same rows, which then get the result of one of them). */
+ * (behind descending starts two sequences may have the same rows, which then get the result of one of them, or where out is q of neither).
+ * Where n or max_rows is 0 nothing is looked at. */
 typedef struct {
     int32_t n, max_rows;
     const int32_t *start;                /* DEVICE, n + 1 */
@@ -604,10 +606,10 @@ typedef struct {
  *   kvc_prompt_rotate   in 32 bits, rounded once; angles are exact to 2^-31 of a turn at every position.  NaN and infinities stay in
  *                       their head, and in their pair where heads are not normed
  *   kvc_prompt_attend   out = softmax(scale * q k^T) v, where a row sees the rows of its sequence up to itself.  Scores, maxima and sums
- *                       are held in 32 bits (the weights' sums beyond 512 tokens in 64), weights enter the second product in the type (one rounding).  Rows of no sequence are left
- *                       as they are.  What a row does not see has no influence, whatever it holds; a row that sees a NaN, or an infinity
- *                       that its result depends on, has no finite result there (NaN or an infinity).  dev_status: n words, bits are OR-ed in.  Equal
- *                       inputs and bounds give equal bits
+ *                       are held in 32 bits (the weights' sums beyond 512 tokens in 64), weights enter the second product in the type (one
+ *                       rounding).  Rows of no sequence are left as they are.  What a row does not see has no influence, whatever it
+ *                       holds; a row that sees a NaN, or an infinity that its result depends on, has no finite result there (NaN or an
+ *                       infinity).  dev_status: n words, bits are OR-ed in.  Equal inputs and bounds give equal bits
  */
 int kvc_prompt_rotate(const kvc_prompt_plan_t *plan, const kvc_prompt_rows *rows, void *hip_stream);
 int kvc_prompt_attend(const kvc_prompt_plan_t *plan, const kvc_prompt_batch *batch, const kvc_prompt_heads *heads, int32_t *dev_status,

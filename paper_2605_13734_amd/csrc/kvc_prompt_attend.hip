@@ -14,8 +14,8 @@
 // finite number is done again with the values of the tiles that some rows see and others do not taken as zero where they are
 // not finite, and as NaN by the rows that see them.
 //
-// What bounds it: long prompts the matrix products beside the softmax's instructions (32k tokens, 64 heads: 14.8 ms, 1190 TFLOP/s; 8k, 32 heads: 0.50 ms,
-// 1110), many short ones the instructions that find a block and start and end it, single short ones latencies (37 tokens: 5.6 us in a graph).
+// What bounds it: long prompts the matrix products beside the softmax's instructions (32k tokens, 64 heads: 15.0 to 15.5 ms, 1130 to 1170 TFLOP/s; 8k, 32
+// heads: 0.50 ms, 1110), many short ones the instructions that find a block and start and end it, single short ones latencies (37 tokens: 5.6 us in a graph).
 #include "kvc_prompt_internal.h"
 #include "../../include/kvc.h"
 
@@ -169,7 +169,7 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
     // (2^30 blocks at most: rows are no more than 2^28, blocks no less than 64)
     if (a.n <= 64) return find_sorted<1>(a, (int)number, size, b);
     if (a.n <= kSorted) return find_sorted<kSorted / 64>(a, (int)number, size, b);
-    // kSorted sequences at a time, whose sum says whether the block is among them (300 prompts of 30 tokens, 32 heads: 75 us, 200: 42; 700: 231.  With
+    // kSorted sequences at a time, whose sum says whether the block is among them (300 prompts of 30 tokens, 32 heads: 76 us, 200: 42; 700: 235.  With
     // the starts held in registers 70 and 216, but one prompt of 8k tokens 0.5 % more, for the registers)
     bool found = false;
     b.row0 = b.rows = b.first = 0;
@@ -565,12 +565,12 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
 
 // The kernels, and what a call takes with each, us: the longest sequence's tiles one after the other (per 64 tokens), the products at the rate of a
 // full chip, what a workgroup takes apart from them, and the launch.  Times of calls in the sizes, us, tokens x heads:
-//   64 rows    37 x 64 6.2, 64 x 100 x 32 38, 1024 x 64 31                                          tiles of 32 tokens, four workgroups per compute unit
-//   64 shared  512 x 32 13.3 (one set of waves 16.4), 1024 x 32 21.3 (28.0), 4096 x 8 62 (93)   two sets of waves take turns: too few rows for the chip
-//   128 rows   2048 x 64 80 (64 rows: 99), 4096 x 32 152 (178), 8 x 1024 x 32 96 (105)             tiles of 32 tokens, three workgroups
-//   192 rows   8192 x 32 490 (128 rows: 500), 32768 x 64 14.8 ms (15.4)                              tiles of 64 tokens, two workgroups: K and V are read least
+//   64 rows    37 x 64 5.8, 64 x 100 x 32 38, 1024 x 64 33                                          tiles of 32 tokens, four workgroups per compute unit
+//   64 shared  512 x 32 13.5 (one set of waves 17.0), 1024 x 32 22.3 (29.3), 4096 x 8 64 (98)   two sets of waves take turns: too few rows for the chip
+//   128 rows   2048 x 64 83 (64 rows: 97), 4096 x 32 155 (175), 8 x 1024 x 32 99 (106)             tiles of 32 tokens, three workgroups
+//   192 rows   8192 x 32 497 (128 rows: 504), 32768 x 64 15.2 ms (15.9)                              tiles of 64 tokens, two workgroups: K and V are read least
 // The numbers are fitted to the choice among 150 measured calls (1 to 128 sequences of 16 to 32k tokens, 8 to 64 heads, bf16): its
-// time is 0.4 % above the least in the mean, 8 % at worst; of 110 others (fp16) 0.6 and 12 % (profiles/prompt_block_rows.txt).
+// time is 0.5 % above the least in the mean, 9 % at worst; of 110 others (fp16) 0.6 and 14 % (profiles/prompt_block_rows.txt).
 struct Kernel {
     int tiles, tokens, turns;
     float per_64, rate, group, launch;       // us, TFLOP/s, us, us

@@ -5,8 +5,8 @@
 //
 // All in 32 bits, rounded once as it is stored.  Bound by HBM where there are many rows (every element is read and written once) and by
 // latency where there are few.  A wave has one row and a run of its heads, four heads at a time, 16 lanes per head and 8 channels
-// per lane: cosines and sines are made once per row and wave, the mean of a head inside a row of lanes.  32k rows of 72 heads: 192 us, 6.3 TB/s (the
-// fastest copy found on this card 6.5); 32 rows 3.3 us in a graph, most of it the launch.
+// per lane: cosines and sines are made once per row and wave, the mean of a head inside a row of lanes.  32k rows of 72 heads: 192 to 198 us, 6.1 to 6.3 TB/s
+// (cards differ; the fastest copy found 6.5); 32 rows 3.3 us in a graph, most of it the launch.
 //
 // Angles are fixed-point numbers of 2^-64 of a turn: a position times a frequency's part of a turn, modulo a turn, is one integer product
 // whose upper word is the angle, exact to 2^-32 of a turn wherever the position is (in 32-bit floating point a position of 10^6 would be
@@ -190,6 +190,8 @@ template <int DT, bool NEIGHBOURS, bool NORM> __global__ __launch_bounds__(256) 
                 if (turns) y[e] = __builtin_fmaf(theirs[e], other[e], y[e]);
                 if (NORM && !APART) y[e] *= by;
             }
+            // (Stored past the caches: alone 1k rows of 40 heads take 5.9 instead of 6.8 us, 32k rows of 72 heads 199 instead of 210; what reads them next
+            // pays where the caches had held them: 8k rows of 40 heads and their attention as prompts of 512 101 instead of 97, 1k rows 27.0 instead of 28.3.)
             if (head < end) {
                 const u32x4 z = {round_pair<DT>(y[0], y[1]), round_pair<DT>(y[2], y[3]), round_pair<DT>(y[4], y[5]), round_pair<DT>(y[6], y[7])};
                 __builtin_nontemporal_store(z, (u32x4 *)(out + head * x.out_head));
