@@ -42,8 +42,10 @@ constexpr float kFar = 65536.0f;
 // 2^20 times the largest values stay inside 32 bits (values below 2^-99 lose bits for it).
 template <int DT> constexpr float kBias = DT == DT_F16 ? 8.0f : -27.0f;
 constexpr float kNone = -__builtin_inff();
+template <int DT> constexpr float kLargest = DT == DT_F16 ? 65504.0f : 3.38953139e38f;       // of the type
 // Weights of up to this many tokens are added up in 32 bits (a tile's as a tree, then tile by tile: 20 roundings at most), sums of these in 64
-// bits.  Added one by one over a long prompt, equal weights round the same way each time: 32k of them were off by 0.00012, 128k by 0.0005.  (8k tokens, 32 heads: 495 us, one by one 491.)
+// bits.  Added one by one over a long prompt, equal weights round the same way each time: 32k of them were off by 0.00012, 128k by 0.0005.  (8k
+// tokens, 32 heads: 495 us, one by one 491.)
 constexpr int kFold = 512;
 constexpr int kSorted = 256;                 // sequences of a call whose blocks are taken longest first
 
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
             }
         }
         f32x4 out[TILES][8];
-        float top[TILES], shift[TILES], sum[TILES];           // top: of the scores without the factor
+        float top[TILES], shift[TILES], sum[TILES], size[TILES];       // top: of the scores without the factor; size: sum of the lane's results' magnitudes
         bool far = false;                                     // some row of the wave is (kFar)
         auto is_far = [&](float x) { return fabsf(x * a.factor) > kFar; };
         // Tile n.  MIXED: some rows see some of its tokens only, or none.  AGAIN: with values that are not finite taken out where they are
@@ -532,14 +534,18 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
                         for (int d = 0; d < 8; ++d) out[t][d] = out[t][d] * by + results[k * kResults + (t * 8 + d) * kPromptWaves * 64] * other_by;
                     }
             }
-            f32x4 zero = {0, 0, 0, 0};               // times infinity, or NaN: NaN
+            bool finite = true;
 #pragma unroll
-            for (int t = 0; t < TILES; ++t)
+            for (int t = 0; t < TILES; ++t) {
+                f32x4 sums = {0, 0, 0, 0};
 #pragma unroll
                 for (int d = 0; d < 8; ++d)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) zero[e] = __builtin_fmaf(out[t][d][e], 0.0f, zero[e]);
-            return zero[0] + zero[1] + (zero[2] + zero[3]) == 0.0f || first >= b.rows;
+                    for (int e = 0; e < 4; ++e) sums[e] += fabsf(out[t][d][e]);
+                size[t] = sums[0] + sums[1] + (sums[2] + sums[3]);
+                finite &= size[t] < -kNone;
+            }
+            return finite || first >= b.rows;
         };
         const bool finite = do_tiles(BoolConst<false>());
         if (__builtin_amdgcn_readfirstlane(__syncthreads_or(!finite))) do_tiles(BoolConst<true>());
@@ -549,10 +555,19 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
             const int row = first + 16 * t + i;
             const float all = sum_of_row(sum[t]), by = 1.0f / all;
             if (row >= b.rows) continue;
-            uint16_t *to = a.out + (long long)(b.row0 + row) * a.o_row + head * a.o_head + 4 * g;
 #pragma unroll
-            for (int d = 0; d < 8; ++d)
-                *(u32x2 *)(to + 16 * d) = u32x2{round_pair<DT>(out[t][d][0] * by, out[t][d][1] * by), round_pair<DT>(out[t][d][2] * by, out[t][d][3] * by)};
+            for (int d = 0; d < 8; ++d) out[t][d] *= by;
+            // A mean of numbers of the type that is beyond them is there by its weights' roundings.  (Looked at where the lane's sum of magnitudes is.)
+            if (__builtin_expect(__any(!(size[t] * by <= kLargest<DT>)), false)) {
+#pragma unroll
+                for (int d = 0; d < 8; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (fabsf(out[t][d][e]) < -kNone) out[t][d][e] = fminf(fmaxf(out[t][d][e], -kLargest<DT>), kLargest<DT>);
+            }
+            uint16_t *to = a.out + (long long)(b.row0 + row) * a.o_row + head * a.o_head + 4 * here_only(g);
+#pragma unroll
+            for (int d = 0; d < 8; ++d) *(u32x2 *)(to + 16 * d) = u32x2{round_pair<DT>(out[t][d][0], out[t][d][1]), round_pair<DT>(out[t][d][2], out[t][d][3])};
             if (a.lse && g == 0)
                 a.lse[(long long)(b.row0 + row) * q_heads + head] = (__builtin_amdgcn_logf(all) - shift[t] + (is_far(top[t]) ? top[t] * a.factor : 0.0f)) * 0.693147181f;
         }

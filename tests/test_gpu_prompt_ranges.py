@@ -98,3 +98,32 @@ def test_sums_of_the_largest_values_behind_a_lower_maximum(heads, rows, block):
         got = out[:, 0].double() / v[0, 0, 0].double()
         assert ((got - 1).abs().amax(1) <= allowed).all(), (value, (got - 1).abs().amax())
         assert torch.equal(out, out[:, :1].expand(out.shape))
+
+
+@pytest.mark.parametrize("block", BLOCKS)
+@pytest.mark.parametrize("bf16", [False, True])
+def test_means_of_the_largest_value_are_numbers(block, bf16):
+    """A mean is no more than the largest value, also where weights that are rounded up would take it beyond the type; an infinite value stays one.  Half
+    a step for the weights, half a step for the result, 2^-18 for the sums and 2^-24 for each product of 32 tokens."""
+    kv, per, rows = BLOCKS[block]
+    dtype, n = typed(bf16), 500
+    plan = kvc.PromptPlan(own_type(bf16), kv, kv * per)
+    assert plan.block_rows(1, rows, rows) == block
+    q, k = torch.zeros(1, 1, DIM, dtype=dtype, device=DEVICE), torch.zeros(rows, 1, DIM, dtype=dtype, device=DEVICE)
+    q[:, :, 0] = 1.0
+    top = torch.finfo(dtype).max
+    v = torch.full((rows, 1, DIM), top, dtype=dtype, device=DEVICE)
+    v[:, :, ::2] = -top
+    v[300, 0, 5], v[310, 0, 6] = math.inf, -math.inf
+    out = torch.empty(rows, kv * per, DIM, dtype=dtype, device=DEVICE)
+    allowed = 2.02 * half_step(bf16) + 2.0 ** -18 + n / 32 * 2.0 ** -24
+    for i in range(1, 40):
+        k[1:, :, 0] = -i / 16
+        kvc.Prompt(plan).attend(kvc.PromptBatch(i32(0, n), rows), q.expand(rows, kv * per, DIM), k.expand(rows, kv, DIM), v.expand(rows, kv, DIM), out, 1.0,
+                                None, stream())
+        bits = out[:n].view(torch.int16)     # (some are no numbers)
+        assert torch.equal(bits, bits[:, :1].expand(n, kv * per, DIM))
+        got = out[:n, 0].double() / v[0, 0].double()
+        assert not got[300:, 5].isfinite().any() and not got[310:, 6].isfinite().any()
+        got[300:, 5] = got[310:, 6] = 1.0
+        assert ((got - 1).abs() <= allowed).all(), (i, (got - 1).abs().max())
