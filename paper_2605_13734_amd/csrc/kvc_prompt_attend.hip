@@ -171,7 +171,7 @@ __device__ __forceinline__ bool find_block(const PromptArgs &a, long long number
     // (2^30 blocks at most: rows are no more than 2^28, blocks no less than 64)
     if (a.n <= 64) return find_sorted<1>(a, (int)number, size, b);
     if (a.n <= kSorted) return find_sorted<kSorted / 64>(a, (int)number, size, b);
-    // kSorted sequences at a time, whose sum says whether the block is among them (300 prompts of 30 tokens, 32 heads: 76 us, 200: 42; 700: 235.  With
+    // kSorted sequences at a time, whose sum says whether the block is among them (300 prompts of 30 tokens, 32 heads: 78 us, 200: 43; 700: 238.  With
     // the starts held in registers 70 and 216, but one prompt of 8k tokens 0.5 % more, for the registers)
     bool found = false;
     b.row0 = b.rows = b.first = 0;
@@ -583,9 +583,9 @@ __global__ __launch_bounds__(64 * kPromptWaves * TURNS, TOKENS == 32 && TILES ==
 //   64 rows    37 x 64 5.8, 64 x 100 x 32 38, 1024 x 64 33                                          tiles of 32 tokens, four workgroups per compute unit
 //   64 shared  512 x 32 13.5 (one set of waves 17.0), 1024 x 32 22.3 (29.3), 4096 x 8 64 (98)   two sets of waves take turns: too few rows for the chip
 //   128 rows   2048 x 64 83 (64 rows: 97), 4096 x 32 155 (175), 8 x 1024 x 32 99 (106)             tiles of 32 tokens, three workgroups
-//   192 rows   8192 x 32 497 (128 rows: 504), 32768 x 64 15.2 ms (15.9)                              tiles of 64 tokens, two workgroups: K and V are read least
+//   192 rows   8192 x 32 503 (128 rows: 517), 32768 x 64 15.1 ms (16.2)                              tiles of 64 tokens, two workgroups: K and V are read least
 // The numbers are fitted to the choice among 150 measured calls (1 to 128 sequences of 16 to 32k tokens, 8 to 64 heads, bf16): its
-// time is 0.5 % above the least in the mean, 9 % at worst; of 110 others (fp16) 0.6 and 14 % (profiles/prompt_block_rows.txt).
+// time is 0.6 % above the least in the mean, 13 % at worst; of 110 others (fp16) 0.7 and 15 % (profiles/prompt_block_rows.txt).
 struct Kernel {
     int tiles, tokens, turns;
     float per_64, rate, group, launch;       // us, TFLOP/s, us, us
